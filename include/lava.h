@@ -16,6 +16,8 @@
  * Around the path: lava_select_topk_batch / lava_compact_batch run tables of independent
  * selections / compactions in one launch each (the sequences of a ragged batch, the layers of a
  * stack), and lava_cascade_step is Algorithm 2 as a driver over a stack's compressed caches.
+ * lava_page_tables, lava_compact_paged, lava_rotary_append and lava_paged_decode keep compressed caches
+ * in pages, for sequences that come, grow and leave.
  *
  * Conventions common to all calls
  *   - "device" pointers are HIP device memory of the current device, "host" pointers are
@@ -509,6 +511,199 @@ int32_t lava_decode_attention(const lava_layer_desc* desc, int32_t batch, const 
                               const void* v_tail, int64_t tail_len, int64_t tail_capacity,
                               float* out, float* lse, void* workspace, size_t workspace_bytes,
                               void* hip_stream);
+
+/*
+ * ------------------------------------------------------------------------------------------
+ * The paged cache: compressed caches that grow by the tokens decoded and give their memory back.
+ *
+ * Heads of a layer keep different numbers of rows, so every KV head of every sequence owns pages of
+ * its own: fixed numbers of rows in one pool that all sequences (and all layers of a model, if the
+ * caller counts a layer's sequences as sequences of their own) share.  Row r of head g of sequence b is
+ * row r % page_rows of page block_table[b][g][r / page_rows].  A step is
+ *   lava_page_tables     pages for the rows the step adds (the survivors of a selection, or new
+ *                        tokens), block tables, the slots of the new rows, positions
+ *   lava_compact_paged   the survivors of an eviction, gathered into the pages of their heads, or
+ *   lava_rotary_append   new tokens: queries and keys rotated, keys and values written to their slots
+ *   lava_paged_decode    one new token per sequence attends to the pages
+ * Nothing is read back by any of them.  A slot is page * page_rows + row in the page; a negative one
+ * is no row.  Page numbers and slots are checked on the device against the pool before they are followed.
+ */
+typedef struct lava_page_pool {
+  int64_t n_pages;      /* 1 .. 2^31 - 1                                                      */
+  int32_t page_rows;    /* 16, 32, 64, 128 or 256                                             */
+  int32_t max_blocks;   /* entries of a head's block table; max_blocks * page_rows < 2^31     */
+  void* k;              /* device [n_pages][page_rows][d_h], dtype of the descriptor          */
+  void* v;
+  int32_t* pos;         /* device [n_pages][page_rows] token position of every row, or NULL   */
+} lava_page_pool;
+
+/* What lava_page_tables keeps between steps: device buffers owned by the caller.  The *_out buffers
+ * receive the counts after the step; each may be the buffer of the count itself (a step in place). */
+typedef struct lava_page_state {
+  int32_t* block_table;        /* [batch][H_kv][max_blocks] page numbers                             */
+  const int32_t* head_rows;    /* [batch][H_kv] rows every head holds                                */
+  const int32_t* seq_pos;      /* [batch] tokens every sequence has seen = position of its next one  */
+  int32_t* free_pages;         /* [n_pages] stack of unused pages, the first n_free[0] of them valid */
+  const int32_t* n_free;       /* [1]                                                                */
+  int32_t* head_rows_out;      /* [batch][H_kv]                                                      */
+  int32_t* seq_pos_out;        /* [batch]                                                            */
+  int32_t* n_free_out;         /* [1]                                                                */
+  int32_t* error;              /* [1] or NULL: LAVA_PAGES_* bits of steps that were refused on the
+                                  device are set in it (never cleared by the library)                */
+} lava_page_state;
+
+#define LAVA_PAGES_EXHAUSTED 1 /* more pages needed than are free                                     */
+#define LAVA_PAGES_BLOCKS 2    /* a head would need more than max_blocks pages                        */
+#define LAVA_PAGES_INVALID 4   /* a negative count (of a selection that gave up, say), a row count or
+                                  n_free out of range, more pages given back than the stack can hold  */
+#define LAVA_PAGES_TOKENS 8    /* more new tokens than max_tokens                                     */
+
+/* Bytes of device workspace lava_page_tables needs; 0 for invalid arguments. */
+size_t lava_page_tables_workspace_bytes(int32_t batch, int32_t n_kv_heads);
+
+/*
+ * Block tables and slot maps of one step.
+ *
+ *   pool         n_pages, page_rows and max_blocks are read; its buffers are not touched
+ *   n_new        device int32 [batch] or NULL (all zero): tokens sequence b sees in this step.  seq_pos grows by it
+ *   head_counts  device int32 [batch][H_kv] or NULL: rows head g of sequence b receives, as written by
+ *                lava_select_topk.  NULL: every head receives a row for every token, n_new[b]
+ *   release      device int32 [batch] or NULL: sequences with a non-zero word are over.  Their pages go
+ *                back before any are taken, in order of (sequence, head, block), and they start this
+ *                step without rows at position 0 (the place can be given to a new sequence at once)
+ *   max_tokens   entries of slots and positions; 0 (and both NULL) with head_counts
+ *   slots        device int64 [max_tokens][H_kv] or NULL: slot of every new row.  Tokens are numbered
+ *                through the sequences, n_new[0] of the first one first; entries behind the last are -1
+ *   positions    device int32 [max_tokens] or NULL: position of every new token, -1 behind the last
+ *
+ * New pages are taken from the top of the stack in order of (sequence, head, block); a head's row
+ * count rounded up to pages is what it owns.  Entries of block_table that get no page stay as they were.
+ * The free stack is written only where pages come back.  A step that cannot be carried out changes
+ * nothing: counts are copied unchanged, every slot and position is -1, and its bits appear in error.
+ * The same inputs give the same outputs bit for bit.  batch <= 65535, H_kv <= 64,
+ * batch * H_kv <= 2^20, max_tokens * H_kv < 2^31.
+ */
+int32_t lava_page_tables(const lava_page_pool* pool, int32_t batch, int32_t n_kv_heads,
+                         const lava_page_state* state, const int32_t* n_new, const int32_t* head_counts,
+                         const int32_t* release, int64_t max_tokens, int64_t* slots, int32_t* positions,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One eviction whose survivors go to pages; fields as in lava_compact_problem. */
+typedef struct lava_paged_compact_problem {
+  int64_t src_rows;             /* src_offsets != NULL: rows of the packed source pool;
+                                   src_offsets == NULL: rows per head of a dense [H_kv][n] source  */
+  const int64_t* src_offsets;
+  const void* k_src;
+  const void* v_src;
+  const int32_t* pos_src;       /* or NULL (the position is then the index itself)                 */
+  const int64_t* head_offsets;
+  const int32_t* kept_idx;
+  int64_t capacity;             /* entries of kept_idx; survivors beyond it are not written        */
+  const int32_t* block_table;   /* device [H_kv][max_blocks]: the sequence's rows of the table      */
+  const int32_t* first_rows;    /* device [H_kv] or NULL: rows every head held before (NULL: none)  */
+} lava_paged_compact_problem;
+
+/*
+ * The survivors of n_problems >= 1 evictions, bit for bit, into the pages of their heads: survivor t of
+ * head g becomes row first_rows[g] + t of that head, with its token position if the pool has positions.
+ * The pages come from a lava_page_tables call with the same head_counts.  Survivors whose source row
+ * is not in the head's segment, or whose page is not in the pool or behind max_blocks, are left out.
+ * Problems must not share pages.  One launch per 32 problems.
+ */
+int32_t lava_compact_paged(const lava_layer_desc* desc, int32_t n_problems,
+                           const lava_paged_compact_problem* problems, const lava_page_pool* pool,
+                           void* hip_stream);
+
+/*
+ * Rotary positions.  The first rotary_dim values of a head form rotary_dim / 2 pairs; pair i is turned by
+ * position * f_i and multiplied by `magnitude`; the other values pass unchanged.
+ *   f_i = base^(-2 i / rotary_dim) radians a token, for contexts longer than the model was trained on
+ *   divided by `factor`: all of them alike (original_context = 0), or by parts: with
+ *   r_i = original_context * f_i / (2 pi) turns in the original context and
+ *   c_i = clamp((r_i - low_turns) / (high_turns - low_turns), 0, 1),  f_i' = c_i f_i + (1 - c_i) f_i / factor.
+ */
+typedef struct lava_rotary_desc {
+  int32_t rotary_dim;        /* even, 2 .. head dimension                                         */
+  int32_t interleaved;       /* 0: pair i is values i and i + rotary_dim / 2; 1: values 2i, 2i + 1 */
+  float magnitude;           /* > 0; 0 selects 1                                                  */
+  int32_t original_context;  /* the fields from here on are read by lava_rotary_turns only        */
+  double base;               /* > 1                                                               */
+  double factor;             /* >= 1; 0 selects 1                                                 */
+  double low_turns, high_turns;   /* by parts: 0 <= low_turns < high_turns                        */
+} lava_rotary_desc;
+
+/* The angles of one token, host [rotary_dim / 2]: f_i in units of 2^-64 turns, rounded to nearest.  The
+ * kernels multiply them by the position modulo 2^64, which is exact, so a far position costs no accuracy.
+ * The caller copies the table to the device once.  Pure host arithmetic. */
+int32_t lava_rotary_turns(const lava_rotary_desc* rot, uint64_t* turns);
+
+/*
+ * Rotation of n_tokens x n_heads heads of any layout.
+ *
+ *   turns      device uint64 [rotary_dim / 2]
+ *   positions  device int32 [n_tokens]; a token with a negative one is left out (its output rows stay as they were)
+ *   x, out     device, head h of token t at element t * token_stride + h * head_stride, head_dim
+ *              values one after another; out == x is allowed where both strides agree, any other
+ *              overlap is not.  Strides are multiples of 16 bytes
+ *   transpose  non-zero: the transposed rotation, which is the gradient's way through it (the inverse, for
+ *              magnitude 1)
+ * dtype LAVA_F32 or LAVA_BF16, head_dim 64 or 128; 32-bit arithmetic, rounded once.
+ */
+int32_t lava_rotary(const lava_rotary_desc* rot, const uint64_t* turns, int32_t dtype, int32_t head_dim,
+                    int64_t n_tokens, int32_t n_heads, const int32_t* positions, const void* x,
+                    int64_t x_token_stride, int64_t x_head_stride, void* out, int64_t out_token_stride,
+                    int64_t out_head_stride, int32_t transpose, void* hip_stream);
+
+/*
+ * New tokens into the paged cache: queries rotated into q_out, keys rotated and values copied into the
+ * rows of the pool that `slots` names, positions written beside them if the pool has positions.
+ *
+ *   q, k, v        device, token t at element t * token_stride, its heads ([H][d_h], [H_kv][d_h]) one
+ *                  after another: three tensors, or three parts of one projection's output.  q may be NULL (with
+ *                  q_out NULL) if only the cache is to be written
+ *   q_out          device [n_tokens][H][d_h]; q itself is allowed where q_token_stride = H * d_h
+ *   slots          device int64 [n_tokens][H_kv] as written by lava_page_tables; a row whose slot is negative
+ *                  or not in the pool is not written.  No two rows may have the same slot
+ *   positions      device int32 [n_tokens]; a token with a negative one is left out altogether
+ */
+int32_t lava_rotary_append(const lava_layer_desc* desc, const lava_rotary_desc* rot, const uint64_t* turns,
+                           int64_t n_tokens, const int32_t* positions, const void* q, int64_t q_token_stride,
+                           const void* k, int64_t k_token_stride, const void* v, int64_t v_token_stride,
+                           void* q_out, const lava_page_pool* pool, const int64_t* slots, void* hip_stream);
+
+/* How lava_paged_decode changes logits, z = scale * <q, k> at first.  All zero: not at all. */
+typedef struct lava_decode_options {
+  float softcap;               /* > 0: z <- softcap * tanh(z / softcap)                                  */
+  int32_t window;              /* > 0: only rows at positions q_pos - window + 1 .. q_pos count           */
+  const float* slopes;         /* device [H] or NULL: z <- z - slopes[h] * (q_pos - position of the row)  */
+} lava_decode_options;
+
+/* Bytes of device workspace lava_paged_decode needs, whatever the batch and the lengths; 0 for an invalid descriptor. */
+size_t lava_paged_decode_workspace_bytes(const lava_layer_desc* desc);
+
+/*
+ * Attention of ONE new token per sequence over the pages of its heads:
+ *   out[h] = Softmax(z[h]) V_g,  g = h / G, over the head_rows[b][g] rows that head g of sequence b holds.
+ *
+ *   q            device [batch][H][d_h], dtype of the descriptor
+ *   pool         k, v; pos is read if the options have a window or slopes (INVALID_ARG if it is NULL then)
+ *   block_table  device int32 [batch][H_kv][max_blocks]; only the entries of rows that are held are read
+ *   head_rows    device int32 [batch][H_kv]
+ *   options      or NULL
+ *   q_pos        device int32 [batch] position of the new token; needed with a window or slopes (rows at later
+ *                positions do not count then), else NULL is allowed
+ *   out          device float [batch][H][d_h];  lse  device float [batch][H] natural-log log-sum-exp, or NULL
+ *
+ * A head without rows, or whose rows are all masked, gives zeros (lse = -inf); rows that are masked, and
+ * whatever pages hold behind a head's last row, may be infinite or NaN.  A head whose row count is negative or more
+ * than max_blocks * page_rows, or whose table names a page that is not in the pool, gives NaN.  fp32 accumulation,
+ * deterministic (fixed merge order).  Uses n_q_heads, n_kv_heads (G <= 8), head_dim, dtype and softmax_scale of the
+ * descriptor.  batch <= 65535, batch * H_kv <= 65536.
+ */
+int32_t lava_paged_decode(const lava_layer_desc* desc, int32_t batch, const void* q, const lava_page_pool* pool,
+                          const int32_t* block_table, const int32_t* head_rows, const lava_decode_options* options,
+                          const int32_t* q_pos, float* out, float* lse, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
 
 /*
  * Per-kernel timing for benchmarks.  When enabled, every kernel the library launches is

@@ -25,6 +25,10 @@ enum KernelId : int {
   KID_COMPACT,        // K/V row gather
   KID_BUDGETS,        // layer budgets on the device
   KID_DECODE,         // decode attention over the packed cache
+  KID_PAGE_PLAN,      // pages a step needs: sums over the heads (small steps: the whole step)
+  KID_PAGE_FILL,      // block tables, slots and positions of a step; pages given back
+  KID_ROTARY,         // rotary positions, keys and values to their slots
+  KID_PAGED_DECODE,   // decode attention over the pages
   KID_COUNT
 };
 
@@ -232,6 +236,62 @@ int32_t launch_decode(const lava_layer_desc& d, int32_t batch, const void* q, co
                       int64_t rows_capacity, const void* k_tail, const void* v_tail, int64_t tail_len,
                       int64_t tail_capacity, float* out, float* lse, void* ws, const DecodePlan& p,
                       hipStream_t s);
+
+// ---------------------------------------------------------------- paged cache
+// Descriptor checks every entry point shares; the decode steps' leave window and pool_kernel out (set to 1 in *out).
+int32_t check_desc(const lava_layer_desc* d);
+int32_t check_desc_decode(const lava_layer_desc* desc, lava_layer_desc* out);
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+struct PageTablesArgs {
+  lava_page_state st;
+  const int32_t* n_new;        // [batch] or null
+  const int32_t* head_counts;  // [batch][heads] or null
+  const int32_t* release;      // [batch] or null
+  long long n_pages, max_tokens;
+  long long* slots;
+  int32_t* positions;
+  int batch, heads, max_blocks, page_shift;
+  void* ws;
+};
+size_t page_tables_bytes(int32_t batch, int32_t n_kv_heads);
+int32_t launch_page_tables(const PageTablesArgs& a, hipStream_t s);
+int32_t launch_compact_paged(const lava_layer_desc& d, int n_problems, const lava_paged_compact_problem* problems,
+                             const lava_page_pool& pool, hipStream_t s);
+
+// One rotary launch: hq heads x -> out and, with a pool, hkv heads of k (rotated) and v to their slots.  Strides in bytes.
+struct RotaryArgs {
+  const unsigned long long* turns;
+  const int32_t* positions;
+  long long n_tokens;
+  const char *x, *k, *v;
+  long long x_token, x_head, k_token, v_token, out_token, out_head;
+  char* out;
+  char *k_pages, *v_pages;
+  int32_t* pos_pages;
+  const long long* slots;      // null: no pool
+  long long pool_rows;
+  int hq, hkv, rot, interleaved;
+  float cos_mul, sin_mul;      // magnitude, and magnitude or its negative (transposed)
+};
+int32_t launch_rotary(const RotaryArgs& a, int32_t dtype, int32_t head_dim, hipStream_t s);
+
+struct PagedDecodeArgs {
+  const char* q;
+  const char *k, *v;
+  const int32_t* pos;
+  const int32_t* block_table;  // [batch][H_kv][max_blocks]
+  const int32_t* head_rows;    // [batch][H_kv]
+  const int32_t* q_pos;        // [batch] or null
+  const float* slopes;         // [H] or null
+  long long n_pages;
+  int page_shift, max_blocks, batch, H, H_kv, G, window;
+  float scale, cap;
+  float* out;
+  float* lse;
+};
+size_t paged_decode_bytes(const lava_layer_desc& d);
+int32_t launch_paged_decode(const lava_layer_desc& d, const PagedDecodeArgs& a, void* ws, hipStream_t s);
 
 // ---------------------------------------------------------------- layer budgets
 // The host path runs the sequential allocation, the device kernel the same arithmetic spread over

@@ -21,7 +21,7 @@ struct ProfState {
 
 const char* const kKernelNames[KID_COUNT] = {
     "vnorm", "stats", "scores", "sweep", "prepass", "poolstat", "sel_init", "sel_fused", "sel_steps", "compact", "budgets",
-    "decode"};
+    "decode", "page_plan", "page_fill", "rotary", "paged_decode"};
 
 void prof_collect() {
   (void)hipDeviceSynchronize();
@@ -64,7 +64,7 @@ lava_tuning g_tuning = {};
 const lava_tuning& tuning() { return g_tuning; }
 
 // ------------------------------------------------------------------ descriptor checks
-static int32_t check_desc(const lava_layer_desc* d) {
+int32_t check_desc(const lava_layer_desc* d) {
   if (d == nullptr) return LAVA_ERR_INVALID_ARG;
   if (d->dtype != LAVA_F32 && d->dtype != LAVA_BF16) return LAVA_ERR_INVALID_ARG;
   if (d->n_q_heads < 1 || d->n_kv_heads < 1 || d->window < 1 || d->pool_kernel < 1)
@@ -79,6 +79,17 @@ static int32_t check_desc(const lava_layer_desc* d) {
   return LAVA_OK;
 }
 
+// Descriptor checks for the decode step: window and pool_kernel play no role there.
+int32_t check_desc_decode(const lava_layer_desc* desc, lava_layer_desc* out) {
+  if (desc == nullptr) return LAVA_ERR_INVALID_ARG;
+  *out = *desc;
+  out->window = 1;
+  out->pool_kernel = 1;
+  const int32_t st = check_desc(out);
+  if (st != LAVA_OK) return st;
+  return out->n_q_heads / out->n_kv_heads > 8 ? LAVA_ERR_SHAPE : LAVA_OK;   // the step's operand holds 8 heads of a group
+}
+
 int32_t check_select_problem(int32_t n_heads, const lava_select_problem& p) {
   if (p.scores == nullptr || p.head_counts == nullptr || p.head_offsets == nullptr || p.kept_idx == nullptr ||
       p.total_entries < 1)
@@ -90,8 +101,6 @@ int32_t check_select_problem(int32_t n_heads, const lava_select_problem& p) {
   if (p.primed != 0 && (p.seg_offsets != nullptr || p.in_offset_dev != nullptr)) return LAVA_ERR_INVALID_ARG;
   return LAVA_OK;
 }
-
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace lava
 
@@ -567,17 +576,6 @@ int32_t lava_cascade_step(const lava_layer_desc* desc, int32_t layer, int64_t n,
   if (st != LAVA_OK) return st;
   S.cur = b;
   return LAVA_OK;
-}
-
-// Descriptor checks for the decode step: window and pool_kernel play no role there.
-static int32_t check_desc_decode(const lava_layer_desc* desc, lava_layer_desc* out) {
-  if (desc == nullptr) return LAVA_ERR_INVALID_ARG;
-  *out = *desc;
-  out->window = 1;
-  out->pool_kernel = 1;
-  const int32_t st = check_desc(out);
-  if (st != LAVA_OK) return st;
-  return out->n_q_heads / out->n_kv_heads > 8 ? LAVA_ERR_SHAPE : LAVA_OK;   // the step's operand holds 8 heads of a group
 }
 
 size_t lava_decode_workspace_bytes(const lava_layer_desc* desc, int32_t batch, int64_t rows_capacity,

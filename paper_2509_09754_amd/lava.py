@@ -31,6 +31,8 @@ EXPORTS = [
     "lava_compact_kv", "lava_compact_packed", "lava_compact_batch",
     "lava_cascade_workspace_bytes", "lava_cascade_step",
     "lava_decode_workspace_bytes", "lava_decode_attention",
+    "lava_page_tables_workspace_bytes", "lava_page_tables", "lava_compact_paged", "lava_rotary_turns", "lava_rotary",
+    "lava_rotary_append", "lava_paged_decode_workspace_bytes", "lava_paged_decode",
     "lava_prof_kernel_count", "lava_prof_kernel_name", "lava_prof_enable", "lava_prof_reset",
     "lava_prof_read", "lava_probe_stream",
 ]
@@ -136,6 +138,22 @@ def _load() -> ctypes.CDLL:
     lib.lava_decode_workspace_bytes.argtypes = [dp, i32, i64, i64]
     lib.lava_decode_attention.restype = i32
     lib.lava_decode_attention.argtypes = [dp, i32, vp, vp, vp, vp, vp, i64, vp, vp, i64, i64, vp, vp, vp, sz, vp]
+    lib.lava_page_tables_workspace_bytes.restype = sz
+    lib.lava_page_tables_workspace_bytes.argtypes = [i32, i32]
+    lib.lava_page_tables.restype = i32
+    lib.lava_page_tables.argtypes = [vp, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.lava_compact_paged.restype = i32
+    lib.lava_compact_paged.argtypes = [dp, i32, vp, vp, vp]
+    lib.lava_rotary_turns.restype = i32
+    lib.lava_rotary_turns.argtypes = [vp, vp]
+    lib.lava_rotary.restype = i32
+    lib.lava_rotary.argtypes = [vp, vp, i32, i32, i64, i32, vp, vp, i64, i64, vp, i64, i64, i32, vp]
+    lib.lava_rotary_append.restype = i32
+    lib.lava_rotary_append.argtypes = [dp, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
+    lib.lava_paged_decode_workspace_bytes.restype = sz
+    lib.lava_paged_decode_workspace_bytes.argtypes = [dp]
+    lib.lava_paged_decode.restype = i32
+    lib.lava_paged_decode.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lava_prof_kernel_count.restype = i32
     lib.lava_prof_kernel_name.restype = ctypes.c_char_p
     lib.lava_prof_kernel_name.argtypes = [i32]
@@ -636,6 +654,285 @@ def lava_decode_attention(desc: LayerDesc, batch: int, q: torch.Tensor, k_hat, v
                                    _ptr(v_tail), int(tail_len), int(tail_capacity), _ptr(out), _ptr(lse),
                                    _ptr(workspace), workspace.numel(), _stream(stream))
     _check(st, "lava_decode_attention")
+    return out, lse
+
+
+# ------------------------------------------------------------------------------ the paged cache
+LAVA_PAGES_EXHAUSTED, LAVA_PAGES_BLOCKS, LAVA_PAGES_INVALID, LAVA_PAGES_TOKENS = 1, 2, 4, 8
+
+
+class PagePoolStruct(ctypes.Structure):
+    """Mirror of lava_page_pool."""
+    _fields_ = [("n_pages", ctypes.c_int64), ("page_rows", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
+
+
+class PagePool:
+    """A pool of pages over device tensors k, v [n_pages, page_rows, d_h] and pos [n_pages, page_rows] int32 or None
+    (the tensors are kept).  max_blocks: pages a head's block table has room for (not needed to append)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, pos: Optional[torch.Tensor] = None, max_blocks: int = 1):
+        _dev(k, "k"), _dev(v, "v", k.dtype)
+        if k.dim() != 3 or v.shape != k.shape:
+            raise ValueError("k and v must be [n_pages, page_rows, d_h]")
+        if pos is not None and tuple(_dev(pos, "pos", torch.int32).shape) != tuple(k.shape[:2]):
+            raise ValueError("pos must be [n_pages, page_rows]")
+        self.k, self.v, self.pos, self.max_blocks = k, v, pos, int(max_blocks)
+        self.c = PagePoolStruct(k.shape[0], k.shape[1], self.max_blocks, _ptr(k), _ptr(v), _ptr(pos))
+        self._ref = ctypes.byref(self.c)
+
+    def _check(self, desc: LayerDesc) -> None:
+        if self.k.dtype != desc.torch_dtype or self.k.shape[2] != desc.head_dim:
+            raise ValueError("the pool's pages have another type or head dimension than the descriptor")
+
+
+class PageStateStruct(ctypes.Structure):
+    """Mirror of lava_page_state."""
+    _fields_ = [(name, ctypes.c_void_p) for name in (
+        "block_table", "head_rows", "seq_pos", "free_pages", "n_free", "head_rows_out", "seq_pos_out", "n_free_out", "error")]
+
+
+class PageState:
+    """What lava_page_tables keeps between steps, over device tensors (all int32): block_table
+    [batch, H_kv, max_blocks], head_rows [batch, H_kv], seq_pos [batch], free_pages [n_pages] (a stack), n_free [1].
+    The *_out tensors receive the counts after a step; left out, a step is made in place."""
+
+    def __init__(self, block_table, head_rows, seq_pos, free_pages, n_free, page_rows: int, head_rows_out=None,
+                 seq_pos_out=None, n_free_out=None, error=None):
+        if block_table.dim() != 3:
+            raise ValueError("block_table must be [batch, H_kv, max_blocks]")
+        self.batch, self.n_kv_heads, self.max_blocks = block_table.shape
+        self.page_rows, self.n_pages = int(page_rows), free_pages.numel()
+        self.block_table, self.free_pages, self.error = block_table, free_pages, error
+        self.head_rows, self.seq_pos, self.n_free = head_rows, seq_pos, n_free
+        self.head_rows_out = head_rows if head_rows_out is None else head_rows_out
+        self.seq_pos_out = seq_pos if seq_pos_out is None else seq_pos_out
+        self.n_free_out = n_free if n_free_out is None else n_free_out
+        heads = self.batch * self.n_kv_heads
+        for name, t, n in (("block_table", block_table, None), ("free_pages", free_pages, None), ("head_rows", head_rows, heads),
+                           ("head_rows_out", self.head_rows_out, heads), ("seq_pos", seq_pos, self.batch),
+                           ("seq_pos_out", self.seq_pos_out, self.batch), ("n_free", n_free, 1), ("n_free_out", self.n_free_out, 1),
+                           ("error", error, 1)):
+            if t is None:
+                continue
+            _dev(t, name, torch.int32)
+            if n is not None and t.numel() != n:
+                raise ValueError(f"{name} must hold {n} values")
+        self.c = PageStateStruct(*(_ptr(t) for t in (block_table, head_rows, seq_pos, free_pages, n_free, self.head_rows_out,
+                                                     self.seq_pos_out, self.n_free_out, error)))
+        self._sizes = PagePoolStruct(self.n_pages, self.page_rows, self.max_blocks, None, None, None)
+        self._ref, self._sizes_ref = ctypes.byref(self.c), ctypes.byref(self._sizes)
+
+    @classmethod
+    def empty(cls, batch: int, n_kv_heads: int, max_blocks: int, n_pages: int, page_rows: int, device="cuda") -> "PageState":
+        """No sequence holds a row and every page is free; steps are made in place."""
+        new = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=device)
+        free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)     # page 0 is taken first
+        return cls(new(batch, n_kv_heads, max_blocks), new(batch, n_kv_heads), new(batch), free,
+                   torch.full((1,), n_pages, dtype=torch.int32, device=device), page_rows, error=new(1))
+
+
+def lava_page_tables_workspace_bytes(batch: int, n_kv_heads: int) -> int:
+    return int(lib.lava_page_tables_workspace_bytes(int(batch), int(n_kv_heads)))
+
+
+def lava_page_tables(state: PageState, n_new: Optional[torch.Tensor] = None, head_counts: Optional[torch.Tensor] = None,
+                     release: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                     positions: Optional[torch.Tensor] = None, workspace=None, stream=None):
+    """Pages, block tables and slots of one step; n_new / release [batch], head_counts [batch, H_kv] int32; slots
+    [max_tokens, H_kv] int64 and positions [max_tokens] int32 are written.  Returns (slots, positions)."""
+    for name, t, n in (("n_new", n_new, state.batch), ("release", release, state.batch),
+                       ("head_counts", head_counts, state.batch * state.n_kv_heads)):
+        if t is not None and _dev(t, name, torch.int32).numel() != n:
+            raise ValueError(f"{name} must hold {n} values")
+    max_tokens = 0
+    if slots is not None:
+        max_tokens = _dev(slots, "slots", torch.int64).numel() // state.n_kv_heads
+        if slots.numel() != max_tokens * state.n_kv_heads:
+            raise ValueError("slots must be [max_tokens, H_kv]")
+    if positions is not None:
+        _dev(positions, "positions", torch.int32)
+        if slots is not None and positions.numel() != max_tokens:
+            raise ValueError("slots and positions must be for the same number of tokens")
+        max_tokens = positions.numel()
+    if workspace is None:
+        need = lava_page_tables_workspace_bytes(state.batch, state.n_kv_heads)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=state.block_table.device)
+    st = lib.lava_page_tables(state._sizes_ref, state.batch, state.n_kv_heads, state._ref, _ptr(n_new), _ptr(head_counts),
+                              _ptr(release), max_tokens, _ptr(slots), _ptr(positions), _ptr(workspace), workspace.numel(),
+                              _stream(stream))
+    _check(st, "lava_page_tables")
+    return slots, positions
+
+
+class PagedCompactProblem(ctypes.Structure):
+    """Mirror of lava_paged_compact_problem."""
+    _fields_ = [
+        ("src_rows", ctypes.c_int64), ("src_offsets", ctypes.c_void_p), ("k_src", ctypes.c_void_p),
+        ("v_src", ctypes.c_void_p), ("pos_src", ctypes.c_void_p), ("head_offsets", ctypes.c_void_p),
+        ("kept_idx", ctypes.c_void_p), ("capacity", ctypes.c_int64), ("block_table", ctypes.c_void_p),
+        ("first_rows", ctypes.c_void_p),
+    ]
+
+
+def paged_compact_problem(desc: LayerDesc, src_rows, k_src, v_src, head_offsets, kept_idx, capacity, block_table,
+                          first_rows=None, src_offsets=None, pos_src=None) -> PagedCompactProblem:
+    """One row of the table of lava_compact_paged (dense source when src_offsets is None); block_table: the sequence's
+    [H_kv, max_blocks].  The caller keeps the tensors."""
+    for name, t in (("k_src", k_src), ("v_src", v_src)):
+        _dev(t, name, desc.torch_dtype)
+    _dev(head_offsets, "head_offsets", torch.int64), _dev(kept_idx, "kept_idx", torch.int32)
+    for name, t, dt in (("block_table", block_table, torch.int32), ("first_rows", first_rows, torch.int32),
+                        ("src_offsets", src_offsets, torch.int64), ("pos_src", pos_src, torch.int32)):
+        if t is not None:
+            _dev(t, name, dt)
+    if head_offsets.numel() != desc.n_kv_heads + 1 or kept_idx.numel() < int(capacity):
+        raise ValueError("head_offsets must hold H_kv + 1 values and kept_idx `capacity` ones")
+    rows = int(src_rows) * (1 if src_offsets is not None else desc.n_kv_heads)
+    if k_src.numel() != rows * desc.head_dim or v_src.numel() != rows * desc.head_dim:
+        raise ValueError("k_src / v_src hold a different number of rows than src_rows")
+    return PagedCompactProblem(int(src_rows), _addr(src_offsets), _addr(k_src), _addr(v_src), _addr(pos_src),
+                               _addr(head_offsets), _addr(kept_idx), int(capacity), _addr(block_table), _addr(first_rows))
+
+
+def lava_compact_paged(desc: LayerDesc, problems, pool: PagePool, stream=None) -> None:
+    """problems: sequence of PagedCompactProblem, or a ready (PagedCompactProblem * n) array."""
+    pool._check(desc)
+    table = problems if isinstance(problems, ctypes.Array) else (PagedCompactProblem * len(problems))(*problems)
+    st = lib.lava_compact_paged(ctypes.byref(desc), len(problems), ctypes.cast(table, ctypes.c_void_p), pool._ref, _stream(stream))
+    _check(st, "lava_compact_paged")
+
+
+class RotaryDesc(ctypes.Structure):
+    """Mirror of lava_rotary_desc."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("original_context", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("low_turns", ctypes.c_double), ("high_turns", ctypes.c_double)]
+
+    @classmethod
+    def make(cls, rotary_dim, interleaved=False, magnitude=1.0, base=10000.0, factor=1.0, original_context=0, low_turns=1.0,
+             high_turns=4.0):
+        return cls(int(rotary_dim), 1 if interleaved else 0, magnitude, int(original_context), base, factor, low_turns, high_turns)
+
+
+def lava_rotary_turns(rot: RotaryDesc, device=None) -> torch.Tensor:
+    """The angles of one token in 2^-64 turns [rotary_dim / 2]: the table lava_rotary takes, as int64 bit patterns."""
+    out = torch.empty(max(rot.rotary_dim // 2, 1), dtype=torch.int64)
+    _check(lib.lava_rotary_turns(ctypes.byref(rot), out.data_ptr()), "lava_rotary_turns")
+    return out if device is None else out.to(device)
+
+
+def _rows_of_heads(t: torch.Tensor, name: str, dtype=None) -> torch.Tensor:
+    """[tokens, heads, d_h] whose heads are contiguous rows (any strides between them)."""
+    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError(f"{name} must be a device tensor [tokens, heads, d_h] with contiguous heads")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype}")
+    return t
+
+
+def _check_turns(rot: RotaryDesc, turns: torch.Tensor, positions: torch.Tensor, tokens: int) -> None:
+    if _dev(turns, "turns", torch.int64).numel() < rot.rotary_dim // 2:
+        raise ValueError("turns must hold rotary_dim / 2 values")
+    if _dev(positions, "positions", torch.int32).numel() != tokens:
+        raise ValueError("positions must be [tokens]")
+
+
+def lava_rotary(rot: RotaryDesc, turns: torch.Tensor, positions: torch.Tensor, x: torch.Tensor,
+                out: Optional[torch.Tensor] = None, transpose: bool = False, stream=None) -> torch.Tensor:
+    """x [tokens, heads, d_h] turned by its tokens' positions into `out` (x itself, or any view of that shape)."""
+    dt = torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float32
+    _rows_of_heads(x, "x", dt)
+    tokens, heads, d = x.shape
+    _check_turns(rot, turns, positions, tokens)
+    if out is None:
+        out = torch.empty(x.shape, dtype=dt, device=x.device)
+    if _rows_of_heads(out, "out", dt).shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    st = lib.lava_rotary(ctypes.byref(rot), _ptr(turns), LAVA_BF16 if dt == torch.bfloat16 else LAVA_F32, d, tokens, heads,
+                         _ptr(positions), _ptr(x), x.stride(0), x.stride(1), _ptr(out), out.stride(0), out.stride(1),
+                         1 if transpose else 0, _stream(stream))
+    _check(st, "lava_rotary")
+    return out
+
+
+def lava_rotary_append(desc: LayerDesc, rot: RotaryDesc, turns: torch.Tensor, positions: torch.Tensor,
+                       q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pool: PagePool, slots: torch.Tensor,
+                       q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """New tokens into the paged cache; q [tokens, H, d_h] (or None), k, v [tokens, H_kv, d_h], parts of one projection's
+    output allowed.  Returns q_out, the rotated queries [tokens, H, d_h]."""
+    dt, d = desc.torch_dtype, desc.head_dim
+    tokens = k.shape[0]
+    for name, t, heads in (("q", q, desc.n_q_heads), ("k", k, desc.n_kv_heads), ("v", v, desc.n_kv_heads)):
+        if t is None:
+            continue
+        _rows_of_heads(t, name, dt)
+        if tuple(t.shape) != (tokens, heads, d) or (heads > 1 and t.stride(1) != d):
+            raise ValueError(f"{name} must be [tokens, {heads}, {d}], its heads one after another")
+    _check_turns(rot, turns, positions, tokens)
+    pool._check(desc)
+    if _dev(slots, "slots", torch.int64).numel() != tokens * desc.n_kv_heads:
+        raise ValueError("slots must be [tokens, H_kv]")
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(tokens, desc.n_q_heads, d, dtype=dt, device=q.device)
+        if q_out.data_ptr() != q.data_ptr():
+            _dev(q_out, "q_out", dt)
+        if q_out.numel() != tokens * desc.n_q_heads * d:
+            raise ValueError("q_out must be [tokens, H, d_h]")
+    st = lib.lava_rotary_append(ctypes.byref(desc), ctypes.byref(rot), _ptr(turns), tokens, _ptr(positions), _ptr(q),
+                                q.stride(0) if q is not None else 0, _ptr(k), k.stride(0), _ptr(v), v.stride(0),
+                                _ptr(q_out) if q is not None else None, pool._ref, _ptr(slots), _stream(stream))
+    _check(st, "lava_rotary_append")
+    return q_out
+
+
+class DecodeOptions(ctypes.Structure):
+    """Mirror of lava_decode_options."""
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p)]
+
+    @classmethod
+    def make(cls, softcap=0.0, window=0, slopes: Optional[torch.Tensor] = None) -> "DecodeOptions":
+        o = cls(softcap, int(window), _ptr(None if slopes is None else _dev(slopes, "slopes", torch.float32)))
+        o.tensor = slopes                                  # kept: the structure holds its address only
+        return o
+
+
+def lava_paged_decode_workspace_bytes(desc: LayerDesc) -> int:
+    return int(lib.lava_paged_decode_workspace_bytes(ctypes.byref(desc)))
+
+
+def lava_paged_decode(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_table: torch.Tensor, head_rows: torch.Tensor,
+                      options: Optional[DecodeOptions] = None, q_pos: Optional[torch.Tensor] = None, out=None, lse=None,
+                      workspace=None, stream=None):
+    """One new token per sequence, q [batch, H, d_h], attends to the pages of its heads; block_table
+    [batch, H_kv, pool.max_blocks], head_rows [batch, H_kv], q_pos [batch] int32.  Returns (out, lse)."""
+    _dev(q, "q", desc.torch_dtype), _dev(block_table, "block_table", torch.int32), _dev(head_rows, "head_rows", torch.int32)
+    batch = q.numel() // (desc.n_q_heads * desc.head_dim)
+    heads = batch * desc.n_kv_heads
+    if q.numel() != batch * desc.n_q_heads * desc.head_dim:
+        raise ValueError("q must be [batch, H, d_h]")
+    if head_rows.numel() != heads or block_table.numel() != heads * pool.max_blocks:
+        raise ValueError("head_rows must be [batch, H_kv] and block_table [batch, H_kv, max_blocks]")
+    pool._check(desc)
+    if q_pos is not None and _dev(q_pos, "q_pos", torch.int32).numel() != batch:
+        raise ValueError("q_pos must be [batch]")
+    slopes = getattr(options, "tensor", None)
+    if slopes is not None and slopes.numel() != desc.n_q_heads:
+        raise ValueError("slopes must be [H]")
+    if out is None:
+        out = torch.empty(batch, desc.n_q_heads, desc.head_dim, dtype=torch.float32, device=q.device)
+    if lse is None:
+        lse = torch.empty(batch, desc.n_q_heads, dtype=torch.float32, device=q.device)
+    for name, t, n in (("out", out, q.numel()), ("lse", lse, batch * desc.n_q_heads)):
+        if _dev(t, name, torch.float32).numel() != n:
+            raise ValueError(f"{name} must hold {n} values")
+    if workspace is None:
+        workspace = torch.empty(max(lava_paged_decode_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device)
+    st = lib.lava_paged_decode(ctypes.byref(desc), batch, _ptr(q), pool._ref, _ptr(block_table), _ptr(head_rows),
+                               ctypes.byref(options) if options is not None else None, _ptr(q_pos), _ptr(out), _ptr(lse),
+                               _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "lava_paged_decode")
     return out, lse
 
 
