@@ -138,6 +138,21 @@ struct TileDma {
     }
   }
 
+  // The two halves of a tile from two places: `b` is where the tile would begin if all of it lay with its second half.
+  __device__ __forceinline__ void issue_halves(const char* __restrict__ a, const char* __restrict__ b, u32x4* stage) const {
+#pragma unroll
+    for (int i = 0; i < T::kLoads; ++i) {
+      const char* src = (i < T::kLoads / 2 ? a : b) + (i / 4) * 4096 + loff[i % kVariants];
+      u32x4* dst = stage + (i / 4) * 256;
+      switch (i % 4) {
+        case 0: __builtin_amdgcn_global_load_lds((const LAVA_GLOBAL_AS void*)src, (LAVA_LDS_AS void*)dst, 16, 0, 0); break;
+        case 1: __builtin_amdgcn_global_load_lds((const LAVA_GLOBAL_AS void*)src, (LAVA_LDS_AS void*)dst, 16, 1024, 0); break;
+        case 2: __builtin_amdgcn_global_load_lds((const LAVA_GLOBAL_AS void*)src, (LAVA_LDS_AS void*)dst, 16, 2048, 0); break;
+        default: __builtin_amdgcn_global_load_lds((const LAVA_GLOBAL_AS void*)src, (LAVA_LDS_AS void*)dst, 16, 3072, 0); break;
+      }
+    }
+  }
+
   // rows at or beyond n are read from row n - 1 (callers mask or drop them)
   __device__ __forceinline__ void issue_clamped(const char* __restrict__ head_base, long long tile,
                                                 long long n, int lane, u32x4* stage) const {
