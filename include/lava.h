@@ -698,7 +698,7 @@ size_t lava_paged_decode_workspace_bytes(const lava_layer_desc* desc);
  * whatever pages hold behind a head's last row, may be infinite or NaN.  A head whose row count is negative or more
  * than max_blocks * page_rows, or whose table names a page that is not in the pool, gives NaN.  fp32 accumulation,
  * deterministic (fixed merge order).  Uses n_q_heads, n_kv_heads (G <= 8), head_dim, dtype and softmax_scale of the
- * descriptor.  batch <= 65535, batch * H_kv <= 65536.
+ * descriptor.  batch <= 65535, batch * H_kv <= 65536, batch * H_kv * max_blocks * page_rows < 2^35.
  */
 int32_t lava_paged_decode(const lava_layer_desc* desc, int32_t batch, const void* q, const lava_page_pool* pool,
                           const int32_t* block_table, const int32_t* head_rows, const lava_decode_options* options,

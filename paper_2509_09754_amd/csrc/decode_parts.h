@@ -80,6 +80,22 @@ __device__ __forceinline__ long long lane_value64(long long x, int lane) {
   return (long long)(((unsigned long long)lane_value((unsigned int)(u >> 32), lane) << 32) | lane_value((unsigned int)u, lane));
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned int dpp_add(unsigned int x) {
+  return x + (unsigned int)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+
+// Inclusive sum over the lanes.
+__device__ __forceinline__ unsigned int wave_incl(unsigned int x) {
+  x = dpp_add<0x111, 0xf>(x);
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  x = dpp_add<0x143, 0xc>(x);
+  return x;
+}
+
 int padded_group(int G) { return G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8; }
 
 int device_cus() {

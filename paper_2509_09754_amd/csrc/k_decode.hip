@@ -81,11 +81,6 @@ struct UnitMap {
   long long off, len;        // lane g: first packed row and number of packed rows of head g
 };
 
-template <int CTRL, int ROWS>
-__device__ __forceinline__ unsigned int dpp_add(unsigned int x) {
-  return x + (unsigned int)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
-}
-
 __device__ __forceinline__ UnitMap map_units(const long long* __restrict__ offs, int n_heads, long long capacity,
                                              int tiles_per_unit, long long tail_len, int lane) {
   UnitMap m;
@@ -100,13 +95,7 @@ __device__ __forceinline__ UnitMap map_units(const long long* __restrict__ offs,
   // usable lengths fit 31 bits (capacity and tail < 2^31)
   m.packed = ((unsigned int)m.len + kTileKeys - 1u) / kTileKeys;
   m.cnt = head && m.usable ? (m.packed + tail_tiles + (unsigned int)tiles_per_unit - 1u) / (unsigned int)tiles_per_unit : 0u;
-  unsigned int incl = m.cnt;                                 // inclusive sum over the lanes
-  incl = dpp_add<0x111, 0xf>(incl);
-  incl = dpp_add<0x112, 0xf>(incl);
-  incl = dpp_add<0x114, 0xf>(incl);
-  incl = dpp_add<0x118, 0xf>(incl);
-  incl = dpp_add<0x142, 0xa>(incl);
-  incl = dpp_add<0x143, 0xc>(incl);
+  const unsigned int incl = wave_incl(m.cnt);                // inclusive sum over the lanes
   m.incl = incl;
   m.total = lane_value(incl, 63);
   return m;

@@ -4,7 +4,7 @@
 // The work is one line of 32-row tiles, head after head through the whole batch.  It is cut into equal shares, one per workgroup
 // and as many workgroups as the device holds at a time, whatever the lengths: a ragged batch, a long sequence alone and a
 // padded one all end together, and the host needs to know no length.  A share is a run of tiles that may end in one head
-// and go on in the next; every workgroup finds its own with one pass over the row counts (an exclusive sum of 256 threads).
+// and go on in the next; every wavefront finds its workgroup's by itself, with one pass over the row counts (sums over its lanes).
 //
 // Inside a share's part of one head the wavefronts take tiles in turn.  K goes through a wavefront's own LDS ring with
 // direct-to-LDS loads, two tiles ahead, V straight into registers, one tile ahead (a lane owns the same columns of every row):
@@ -13,11 +13,13 @@
 //   output   acc[head][columns of this lane] += p[row][head] * V[row][columns], p broadcast through LDS in fp32; V is never
 //            rounded
 // Pages: the numbers of a wavefront's next 64 tiles are held by its lanes, one each (two for pages of half a tile), and become
-// scalars when their tile is requested, so that the table costs one trip to memory per 64 tiles.  With positions the same
-// lanes find out which rows of their tiles are seen: tiles without any are not requested.
+// scalars when their tile is requested, so that the table costs one trip to memory per 64 tiles, and the next head's first
+// is made while this head's tiles stream.  With positions it is the next 16 tiles: four lanes each find out which rows of
+// their tile are seen (tiles without any are not requested) and leave the distances in LDS for the bias.
 //
-// A head inside one share is finished there; otherwise each workgroup publishes its part (maximum, sum, output) and the one
-// that finds all parts of the head published merges them in order.  Flags and tags are those of the decode step over the packed cache
+// A head inside one share is finished there; otherwise each workgroup stores its part (maximum, sum, output), publishes its
+// parts (two at most: of its first and its last head) at its end, and the one that finds all parts of a head published
+// merges them in order.  Flags and tags are those of the decode step over the packed cache
 // (xblock.h): a flag counts only if it equals the call's tag, whoever merges a head clears its flags, nobody waits.
 //
 // Bound by HBM: 2 * d_h * elem bytes a row.
@@ -43,34 +45,18 @@ struct PagedArgs {
 
 // A workgroup's part of a head is stored in its first place if the head began before the workgroup's share, else in its
 // second: parts 0, 1, 2, ... of a head whose first workgroup is w0.
-__device__ __forceinline__ long long part_slot(long long w0, int u) { return u == 0 ? 2 * w0 + 1 : 2 * (w0 + u); }
+__device__ __forceinline__ int part_slot(int w0, int u) { return u == 0 ? 2 * w0 + 1 : 2 * (w0 + u); }
 
-// Tiles of head hb; -1: its row count is none.
+// x / y rounded up, y > 0.
+__device__ __forceinline__ unsigned int ceil_of(unsigned int x, unsigned int y) { return x / y + (x % y != 0u ? 1u : 0u); }
+
+// What a workgroup that changes heads loses, in tiles.
+constexpr unsigned int kHeadCost = 6u;
+
+// Tiles of a head with that many rows; -1: it cannot have them.
 __device__ __forceinline__ int head_tiles(const PagedDecodeArgs& a, int rows) {
-  if (rows < 0 || rows > (long long)a.max_blocks << a.page_shift) return -1;
-  return (int)(((long long)rows + kTileKeys - 1) / kTileKeys);
-}
-
-// Exclusive sum over the workgroup's threads and the sum over all.
-__device__ __forceinline__ long long share_scan(long long x, long long* s_part, long long* total) {
-  const int lane = threadIdx.x & 63, wave = wave_index();
-  long long incl = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const unsigned int lo = __shfl_up((unsigned int)incl, d), hi = __shfl_up((unsigned int)(incl >> 32), d);
-    if (lane >= d) incl += (long long)(((unsigned long long)hi << 32) | lo);
-  }
-  if (lane == 63) s_part[wave] = incl;
-  __syncthreads();
-  long long before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kDecWaves; ++w) {
-    const long long p = s_part[w];
-    if (w < wave) before += p;
-    all += p;
-  }
-  *total = all;
-  return before + incl - x;
+  if (rows < 0 || rows > a.max_blocks << a.page_shift) return -1;
+  return (int)(((unsigned int)rows + kTileKeys - 1u) / kTileKeys);
 }
 
 // cap * tanh(z / cap): near zero by its series (the quotient of exponentials would cancel), else from e^(-2 |z / cap|).
@@ -85,90 +71,56 @@ __device__ __forceinline__ float capped(float z, float cap, float inv_cap) {
   return cap * copysignf(a < 0.25f ? series : far, y);
 }
 
-// A value that is the same in every lane, as a scalar.
-__device__ __forceinline__ long long uniform64(long long x) { return lane_value64(x, 0); }
-
-// a / b for 0 <= a < 2^52, b > 0 (a quotient of doubles is off by less than one).
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  long long q = (long long)((double)a / (double)b);
-  if (q * b > a) --q;
-  if ((q + 1) * b <= a) ++q;
-  return q;
+// Two values of an output row from the maximum (log2 units), the sum and the weighted values; no row seen: zeros.
+template <int D>
+__device__ __forceinline__ void write_row(const PagedDecodeArgs& p, int b, int g, int t, int e, float M, float L, float2 sum) {
+  const long long row = (long long)b * p.H + (long long)g * p.G + t;
+  const bool none = L == 0.0f;
+  p.out[row * D + e] = none ? 0.0f : sum.x / L;
+  p.out[row * D + e + 1] = none ? 0.0f : sum.y / L;
+  if (p.lse != nullptr && e == 0) p.lse[row] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
-// The parts of one head, in order.
-constexpr int kPartChunk = 32;
+// The parts of one head, in order, eight loads of each kind in flight.
+constexpr int kPartLoads = 8;
 template <int D, int GP>
-__device__ __forceinline__ void merge_parts(const PagedArgs& a, int b, int g, long long w0, int parts, float2 (*s_ml)[GP]) {
-  constexpr int kPairs = GP * D / 2, kOut = (kPairs + kDecThreads - 1) / kDecThreads;
-  float M[kOut], L[kOut];
-  float2 sum[kOut];
+__device__ __forceinline__ void merge_parts(const PagedArgs& a, int b, int g, int w0, int parts) {
+  constexpr int kPairs = GP * D / 2;
+  for (int i = threadIdx.x; i < kPairs; i += kDecThreads) {
+    const int t = 2 * i / D, e = 2 * i % D;
+    float M = -INFINITY, L = 0.0f;
+    float2 sum = make_float2(0.0f, 0.0f);
+    for (int c0 = 0; c0 < parts; c0 += kPartLoads) {
+      const int nu = parts - c0 < kPartLoads ? parts - c0 : kPartLoads;
+      float2 ml[kPartLoads], pv[kPartLoads];
 #pragma unroll
-  for (int j = 0; j < kOut; ++j) { M[j] = -INFINITY; L[j] = 0.0f; sum[j] = make_float2(0.0f, 0.0f); }
-  for (int c0 = 0; c0 < parts; c0 += kPartChunk) {
-    const int nu = parts - c0 < kPartChunk ? parts - c0 : kPartChunk;
-    float2 pv[kOut][16];
-    auto load_parts = [&](int u0) {
-#pragma unroll
-      for (int j = 0; j < kOut; ++j) {
-        const int idx = 2 * ((int)threadIdx.x + kDecThreads * j);
-#pragma unroll
-        for (int u = 0; u < 16; ++u)
-          pv[j][u] = idx < GP * D && u0 + u < nu
-                         ? ld_dev_f2(reinterpret_cast<const float2*>(a.part_acc + part_slot(w0, c0 + u0 + u) * GP * D + idx))
-                         : make_float2(0.0f, 0.0f);
+      for (int u = 0; u < kPartLoads; ++u) {
+        const int slot = part_slot(w0, c0 + (u < nu ? u : 0));
+        ml[u] = ld_dev_f2(&a.part_ml[slot * GP + t]);
+        pv[u] = ld_dev_f2(reinterpret_cast<const float2*>(a.part_acc + (long long)slot * (GP * D) + 2 * i));
       }
-    };
-    load_parts(0);
-    for (int i = threadIdx.x; i < nu * GP; i += kDecThreads) s_ml[i / GP][i % GP] = ld_dev_f2(&a.part_ml[part_slot(w0, c0 + i / GP) * GP + i % GP]);
-    __syncthreads();
+      float m_new = M;
 #pragma unroll
-    for (int j = 0; j < kOut; ++j) {
-      const int t = 2 * ((int)threadIdx.x + kDecThreads * j) / D;
-      if (t >= GP) continue;
-      float mc = s_ml[0][t].x;
-      for (int u = 1; u < nu; ++u) mc = fmaxf(mc, s_ml[u][t].x);
-      const float m_new = fmaxf(M[j], mc), base = m_new == -INFINITY ? 0.0f : m_new;   // -inf: nothing seen so far
-      const float keep = fast_exp2(M[j] - base);
-      M[j] = m_new;
-      L[j] *= keep;
-      sum[j].x *= keep;
-      sum[j].y *= keep;
-    }
-    for (int u0 = 0; u0 < nu; u0 += 16) {
-      if (u0 > 0) load_parts(u0);
+      for (int u = 0; u < kPartLoads; ++u) m_new = fmaxf(m_new, ml[u].x);   // those beyond nu repeat the first
+      const float base = m_new == -INFINITY ? 0.0f : m_new;    // -inf: nothing seen so far
+      const float keep = fast_exp2(M - base);
+      M = m_new;
+      L *= keep;
+      sum.x *= keep;
+      sum.y *= keep;
 #pragma unroll
-      for (int j = 0; j < kOut; ++j) {
-        const int t = 2 * ((int)threadIdx.x + kDecThreads * j) / D;
-        if (t >= GP) continue;
-        const float base = M[j] == -INFINITY ? 0.0f : M[j];
-#pragma unroll
-        for (int u = 0; u < 16; ++u) {
-          if (u0 + u < nu) {
-            const float2 st = s_ml[u0 + u][t];
-            const float wgt = fast_exp2(st.x - base);
-            L[j] += wgt * st.y;
-            sum[j].x += wgt * pv[j][u].x;
-            sum[j].y += wgt * pv[j][u].y;
-          }
-        }
+      for (int u = 0; u < kPartLoads; ++u) {
+        const float wgt = u < nu ? fast_exp2(ml[u].x - base) : 0.0f;
+        L += u < nu ? wgt * ml[u].y : 0.0f;
+        sum.x += u < nu ? wgt * pv[u].x : 0.0f;
+        sum.y += u < nu ? wgt * pv[u].y : 0.0f;
       }
     }
-    __syncthreads();                                         // the next chunk overwrites s_ml
-  }
-#pragma unroll
-  for (int j = 0; j < kOut; ++j) {
-    const int idx = 2 * ((int)threadIdx.x + kDecThreads * j), t = idx / D, e = idx % D;
-    if (t >= a.p.G) continue;
-    const long long row = (long long)b * a.p.H + (long long)g * a.p.G + t;
-    const bool none = L[j] == 0.0f;                          // every row masked
-    a.p.out[row * D + e] = none ? 0.0f : sum[j].x / L[j];
-    a.p.out[row * D + e + 1] = none ? 0.0f : sum[j].y / L[j];
-    if (a.p.lse != nullptr && e == 0) a.p.lse[row] = none ? -INFINITY : (M[j] + log2f(L[j])) * 0.6931471805599453f;
+    if (t < a.p.G) write_row<D>(a.p, b, g, t, e, M, L, sum);
   }
 }
 
-template <int DT, int D, int GP, bool POS>
+template <int DT, int D, int GP, bool OPT>
 __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) {
   using S = DecShape<DT, D>;
   using T = Tile<DT, D>;
@@ -178,68 +130,94 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
   constexpr int kPs = GP < 4 ? 4 : GP;                      // floats per row in s_p (one or two 128-bit reads)
   __shared__ __attribute__((aligned(16))) float s_p[kDecWaves][kTileKeys + 1][kPs];   // probabilities; row 32: rescale factors
   __shared__ float s_m[kDecWaves][GP], s_l[kDecWaves][GP];
-  __shared__ long long s_part[kDecWaves], s_start;
-  __shared__ int s_head, s_flag, s_bad;
+  constexpr int kBlock = OPT ? 16 : 64;                     // tiles whose pages a wavefront holds
+  __shared__ __attribute__((aligned(16))) float s_back[OPT ? kDecWaves : 1][OPT ? 16 * kTileKeys : 4];   // distances to the rows
+  __shared__ int s_flag[2];
 
   const PagedDecodeArgs& p = a.p;
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int n_heads = p.batch * p.H_kv;
   const int shift = p.page_shift, page_mask = (1 << shift) - 1;
 
-  // ---------------- this workgroup's share
-  const int per = (n_heads + kDecThreads - 1) / kDecThreads;   // heads a thread adds up
-  long long mine = 0;
-  const int h_first = (int)threadIdx.x * per;
-  for (int i = 0; i < per; ++i) {
-    const int t = h_first + i < n_heads ? head_tiles(p, p.head_rows[h_first + i]) : 0;
-    mine += t > 0 ? t : 0;
-  }
-  if (threadIdx.x == 0) s_bad = 0;
-  long long total;
-  const long long before = share_scan(mine, s_part, &total);
-  total = uniform64(total);
-  // heads that hold nothing, or whose count is none, belong to nobody's share
-  for (int h0 = 0; h0 < n_heads; h0 += gridDim.x * 64) {
-    const int hb = h0 + (int)blockIdx.x + (int)gridDim.x * lane;
-    const int t = hb < n_heads ? head_tiles(p, p.head_rows[hb]) : 1;
-    unsigned long long todo = __ballot(t <= 0);
-    while (todo != 0ull) {
-      const int l = __builtin_ctzll(todo);
-      todo &= todo - 1ull;
-      const float x = (int)lane_value((unsigned int)t, l) < 0 ? NAN : 0.0f;
-      const int hx = h0 + (int)blockIdx.x + (int)gridDim.x * l, b = hx / p.H_kv;
-      const long long row0 = (long long)b * p.H + (long long)(hx - b * p.H_kv) * p.G;
-      for (int i = threadIdx.x; i < p.G * D; i += kDecThreads) p.out[row0 * D + i] = x;
-      if (p.lse != nullptr && (int)threadIdx.x < p.G) p.lse[row0 + threadIdx.x] = x == 0.0f ? -INFINITY : x;
+  // ---------------- this workgroup's share: sums over all heads, 64 at a time
+  constexpr int kHeld = 8;                                    // counts a lane holds at once: 512 heads in one trip to memory
+  int held[kHeld];
+  auto load_counts = [&](int h0) {
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c) {
+      const int h = h0 + 64 * c + lane;
+      held[c] = h < n_heads ? p.head_rows[h] : 0;
+    }
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c) held[c] = head_tiles(p, held[c]);
+  };
+  unsigned int mine = 0u, full = 0u;
+  bool empty = false;
+  for (int h0 = 0; h0 < n_heads; h0 += 64 * kHeld) {
+    load_counts(h0);
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c) {
+      mine += held[c] > 0 ? (unsigned int)held[c] : 0u;
+      full += held[c] > 0 ? 1u : 0u;
+      empty |= h0 + 64 * c + lane < n_heads && held[c] <= 0;
     }
   }
-  // a share is at least four tiles, one per wavefront, unless the heads are shorter than that
-  long long share = uniform64(quotient(total + gridDim.x - 1, gridDim.x));
-  if (share < 4) {
-    const long long least = total >= 4ll * n_heads ? 4 : total >= 3ll * n_heads ? 3 : total >= 2ll * n_heads ? 2 : 1;
-    if (share < least) share = least;
-  } else {
-    share = (share + 3) & ~3ll;
+  const unsigned int total = lane_value(wave_incl(mine), 63), n_full = lane_value(wave_incl(full), 63);
+  // Heads that hold nothing, or cannot hold what their count says, are in nobody's share: workgroup h % gridDim fills in.
+  if (__ballot(empty) != 0ull) {
+    for (int h = blockIdx.x; h < n_heads; h += gridDim.x) {
+      const int n = head_tiles(p, p.head_rows[h]);
+      if (n > 0) continue;                                    // uniform
+      const int b = h / p.H_kv;
+      const long long row0 = (long long)b * p.H + (long long)(h - b * p.H_kv) * p.G;
+      for (int i = threadIdx.x; i < p.G * D; i += kDecThreads) p.out[row0 * D + i] = n < 0 ? NAN : 0.0f;
+      if (p.lse != nullptr && (int)threadIdx.x < p.G) p.lse[row0 + threadIdx.x] = n < 0 ? NAN : -INFINITY;
+    }
   }
-  const long long t0 = (long long)blockIdx.x * share;
-  const long long t1 = t0 + share < total ? t0 + share : total;
-  if (t0 >= total) return;
-  if (mine > 0 && before <= t0 && t0 < before + mine) {      // one thread's heads hold the first tile
-    long long at = before;
-    for (int i = 0; i < per; ++i) {
-      const int t = h_first + i < n_heads ? head_tiles(p, p.head_rows[h_first + i]) : 0;
-      if (t <= 0) continue;
-      if (t0 < at + t) {
-        s_head = h_first + i;
-        s_start = at;
-        break;
+  if (total == 0u) return;
+  // Two ways to cut.  By heads: units of at most `share` tiles of one head, a workgroup each, if there are enough workgroups for
+  // all units.  Else through the line, where a head weighs kHeadCost tiles more than it has: what it costs to change heads.
+  const unsigned int wgs = gridDim.x, even = ceil_of(total, wgs), line = ceil_of(total + kHeadCost * n_full, wgs);
+  unsigned int share = 0u;
+  bool by_heads = false;
+#pragma unroll 1
+  for (int attempt = 0; attempt < 2 && !by_heads; ++attempt) {   // with shares as even as can be, then with those of the line
+    share = ((attempt == 0 ? even : line) + 3u) & ~3u;        // a tile for every wavefront
+    unsigned int units = 0u;
+    for (int h0 = 0; h0 < n_heads; h0 += 64 * kHeld) {
+      if (n_heads > 64 * kHeld) load_counts(h0);
+#pragma unroll
+      for (int c = 0; c < kHeld; ++c) units += held[c] > 0 ? ceil_of((unsigned int)held[c], share) : 0u;
+    }
+    by_heads = lane_value(wave_incl(units), 63) <= wgs;       // at most one unit a head more than tiles / share: no overflow
+  }
+  if (!by_heads) share = line;
+  const unsigned int weight = by_heads ? 0u : kHeadCost;
+  // t0: this workgroup's unit, or its first place in the line
+  const unsigned int t0 = by_heads ? blockIdx.x : blockIdx.x * share;
+  int hb = -1;
+  unsigned int head_start = 0u;                               // units, or places, before the head
+  {
+    unsigned int at = 0u;
+    for (int h0 = 0; h0 < n_heads && hb < 0; h0 += 64 * kHeld) {
+      if (n_heads > 64 * kHeld) load_counts(h0);
+#pragma unroll
+      for (int c = 0; c < kHeld; ++c) {
+        if (hb >= 0) continue;                                // uniform
+        const unsigned int k = held[c] > 0 ? (unsigned int)held[c] : 0u;
+        const unsigned int n = k == 0u ? 0u : by_heads ? ceil_of(k, share) : k + weight, incl = wave_incl(n);
+        const unsigned long long after = __ballot(at + incl > t0);
+        if (after != 0ull) {
+          const int l = __builtin_ctzll(after);
+          hb = h0 + 64 * c + l;
+          head_start = at + lane_value(incl, l) - lane_value(n, l);
+        } else {
+          at += lane_value(incl, 63);
+        }
       }
-      at += t;
     }
   }
-  __syncthreads();
-  int hb = (int)lane_value((unsigned int)s_head, 0);
-  long long head_start = uniform64(s_start);                 // tiles before this head
+  if (hb < 0) return;                                         // more workgroups than units
 
   using VRaw = typename RawBits<S::kBpl>::type;
   TileDma<DT, D> dma;
@@ -255,14 +233,44 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
   const float inv_cap = p.cap > 0.0f ? 1.0f / p.cap : 0.0f;
   const unsigned int window = p.window > 0 ? (unsigned int)p.window : 0x80000000u;
 
-  for (long long t = t0; t < t1;) {
-    const int rows = p.head_rows[hb];
-    const int tiles = head_tiles(p, rows);
-    if (tiles <= 0) { ++hb; continue; }                       // uniform
+  // Pages of tile0, tile0 + kDecWaves, ... of head h, kBlock of them, as far as there are `here`: a lane each, or four (OPT)
+  auto load_pages = [&](int h, int rows_h, int tile0, int here, int& page_a, int& page_b) {
+    const int i = OPT ? lane >> 2 : lane;
+    const int row0 = (tile0 + kDecWaves * i) * kTileKeys;
+    const int* table = p.block_table + (long long)h * p.max_blocks;
+    page_a = page_b = 0;
+    if (i < here) {
+      page_a = table[row0 >> shift];
+      page_b = shift == 4 && row0 + 16 < rows_h ? table[(row0 >> 4) + 1] : page_a;
+    }
+  };
+
+  // parts that wait to be published: of the first and the last head of the share
+  int pend_head[2] = {-1, -1}, pend_w0[2] = {0, 0}, pend_parts[2] = {0, 0};
+  int rows = p.head_rows[hb], tiles = head_tiles(p, rows);
+  int page_a, page_b;
+  bool pages_ready = false;
+  // In the line a head's tiles follow its weight: tile j is place head_start + weight + j.
+  const unsigned int t1 = t0 + share, line_end = total + weight * n_full;
+  unsigned int done = 0u;                                     // tiles of the share so far
+  for (;;) {
     const int b = hb / p.H_kv, g = hb - b * p.H_kv;
-    const int ta = (int)(t - head_start), tb = head_start + tiles < t1 ? tiles : (int)(t1 - head_start);   // tiles of the head
-    const int* __restrict__ table = p.block_table + (long long)hb * p.max_blocks;
-    const int q_pos = POS ? p.q_pos[b] : 0;
+    const unsigned int at = head_start + weight;              // place of the head's first tile
+    int ta, tb;                                               // its tiles that are this share's
+    if (by_heads) {
+      ta = (int)((t0 - head_start) * share);
+      tb = tiles - ta < (int)share ? tiles : ta + (int)share;
+    } else {
+      ta = t0 > at ? (int)(t0 - at) : 0;
+      tb = t1 <= at ? 0 : t1 - at < (unsigned int)tiles ? (int)(t1 - at) : tiles;
+    }
+    if (ta >= tb) return;                                     // the share ends inside the first head's weight
+    const bool last = by_heads || at + (unsigned int)tiles + weight >= t1 || at + (unsigned int)tiles >= line_end;
+    const int q_pos = OPT && p.pos != nullptr ? p.q_pos[b] : 0;
+    // wavefronts take turns through the whole share, so that each has as many tiles as the others
+    const int first = ta + (int)(((unsigned int)wave - done) & (kDecWaves - 1));
+    const int cnt = first < tb ? (tb - first + kDecWaves - 1) / kDecWaves : 0;   // this wavefront's tiles
+    if (!pages_ready) load_pages(hb, rows, first, cnt < kBlock ? cnt : kBlock, page_a, page_b);
 
     // the group's query rows as the 32-column operand: column t < G is head g * G + t
     u32x4 qf[T::kSteps];
@@ -273,7 +281,7 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
       qf[j] = x;
     }
     float slope = 0.0f;
-    if (POS && p.slopes != nullptr && col < p.G) slope = p.slopes[g * p.G + col] * kLog2e;
+    if (OPT && p.slopes != nullptr && col < p.G) slope = p.slopes[g * p.G + col] * kLog2e;
     float m_run = -INFINITY, l_run = 0.0f;                    // of head `col` (lanes col < G)
     float acc[GP][kDpl];
 #pragma unroll
@@ -281,46 +289,52 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
 #pragma unroll
       for (int e = 0; e < kDpl; ++e) acc[i][e] = 0.0f;
 
-    const int cnt = ta + wave < tb ? (tb - ta - wave + kDecWaves - 1) / kDecWaves : 0;   // this wavefront's tiles
-    for (int i0 = 0; i0 < cnt; i0 += 64) {
-      const int tile0 = ta + wave + kDecWaves * i0;           // of lane 0; lane j: tile0 + kDecWaves * j
-      const int here = cnt - i0 < 64 ? cnt - i0 : 64;
-      // ---------------- pages of the next 64 tiles
-      int page_a = 0, page_b = 0;
-      unsigned int seen = 0xffffffffu;                        // rows of the lane's tile that count (POS)
+    int next_head = hb, next_rows = 0, next_tiles = 0, next_a = 0, next_b = 0;
+    for (int i0 = 0; i0 == 0 || i0 < cnt; i0 += kBlock) {
+      const int tile0 = first + kDecWaves * i0;
+      const int here = cnt - i0 < kBlock ? cnt - i0 : kBlock;
+      if (i0 > 0) load_pages(hb, rows, tile0, here, page_a, page_b);
+      unsigned int seen = 0xffffffffu;                        // rows of the lane's tile that count (OPT)
       {
-        const int row0 = (tile0 + kDecWaves * lane) * kTileKeys;
-        const bool there = lane < here;
-        if (there) page_a = table[row0 >> shift];
-        page_b = page_a;
-        if (shift == 4 && there && row0 + 16 < rows) page_b = table[(row0 >> 4) + 1];
         const bool bad = page_a < 0 || page_a >= p.n_pages || page_b < 0 || page_b >= p.n_pages;
-        if (__ballot(bad) != 0ull) {
-          if (lane == 0) s_bad = 1;
+        if (__ballot(bad) != 0ull) {                          // the head's result is NaN: any page will do
+          l_run = NAN;
           if (bad) page_a = page_b = 0;
         }
-        if (POS) {
-          const long long at = ((long long)page_a << shift) + (row0 & page_mask);
-          const long long bt = shift == 4 ? (long long)page_b << 4 : at + 16;
+        if (OPT) {
+          const int i = lane >> 2, part = lane & 3;           // rows 8 part .. 8 part + 7 of tile i
+          const int row0 = (tile0 + kDecWaves * i) * kTileKeys;
           seen = 0u;
-          if (there) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              const int4 x = *reinterpret_cast<const int4*>(p.pos + (c < 4 ? at + 4 * c : bt + 4 * (c - 4)));
-              const int y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const unsigned int back = (unsigned int)(q_pos - y[e]);   // a later row: 2^31 and more
-                if (back < window && row0 + 4 * c + e < rows) seen |= 1u << (4 * c + e);
-              }
+          if (i < here) {
+            int4 x = make_int4(q_pos, q_pos, q_pos, q_pos), x2 = x;
+            if (p.pos != nullptr) {                            // uniform
+              const long long place = shift == 4 ? ((long long)(part < 2 ? page_a : page_b) << 4) + 8 * (part & 1)
+                                                 : ((long long)page_a << shift) + (row0 & page_mask) + 8 * part;
+              x = *reinterpret_cast<const int4*>(p.pos + place);
+              x2 = *reinterpret_cast<const int4*>(p.pos + place + 4);
             }
+            const int y[8] = {x.x, x.y, x.z, x.w, x2.x, x2.y, x2.z, x2.w};
+            float back[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const unsigned int d = (unsigned int)q_pos - (unsigned int)y[e];   // a later row: 2^31 and more
+              back[e] = (float)d;
+              if (d < window && row0 + 8 * part + e < rows) seen |= 1u << e;
+            }
+            float* dst = &s_back[wave][lane * 8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dst[e] = back[e];
           }
+          seen <<= 8 * part;
+          seen |= (unsigned int)__shfl_xor((int)seen, 1);
+          seen |= (unsigned int)__shfl_xor((int)seen, 2);
         }
       }
-      unsigned long long todo = POS ? __ballot(seen != 0u) : (here == 64 ? ~0ull : (1ull << here) - 1ull);
-      // place in the pool of the first rows of the two halves of lane j's tile
+      unsigned long long todo = OPT ? __ballot(seen != 0u) & 0x1111111111111111ull : here == 64 ? ~0ull : (1ull << here) - 1ull;
+      auto row_of = [&](int j) -> int { return (tile0 + kDecWaves * (OPT ? j >> 2 : j)) * kTileKeys; };   // first row of lane j's tile
+      // place in the pool of the first rows of the tile's two halves
       auto half_a = [&](int j) -> long long {
-        return ((long long)(int)lane_value((unsigned int)page_a, j) << shift) + (((tile0 + kDecWaves * j) * kTileKeys) & page_mask);
+        return ((long long)(int)lane_value((unsigned int)page_a, j) << shift) + (row_of(j) & page_mask);
       };
       auto half_b = [&](int j, long long at) -> long long {
         return shift == 4 ? (long long)(int)lane_value((unsigned int)page_b, j) << 4 : at + 16;
@@ -341,33 +355,36 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
         const long long at = half_a(j), bt = half_b(j, at);
         const char* va = p.v + at * T::kRowBytes;
         const char* vb = p.v + bt * T::kRowBytes - T::kTileBytes / 2;
-        const int left = rows - (tile0 + kDecWaves * j) * kTileKeys;
-        if (POS || left >= kTileKeys) {
 #pragma unroll
-          for (int kk = 0; kk < kTileKeys; ++kk)
-            dst[kk] = *reinterpret_cast<const VRaw*>((kk < kTileKeys / 2 ? va : vb) + kk * T::kRowBytes + v_lane);
-        } else {                                               // rows behind the last one repeat it
-#pragma unroll
-          for (int kk = 0; kk < kTileKeys; ++kk) {
-            const int r = kk < left ? kk : left - 1;
-            dst[kk] = *reinterpret_cast<const VRaw*>((r < kTileKeys / 2 ? va : vb) + r * T::kRowBytes + v_lane);
-          }
-        }
+        for (int kk = 0; kk < kTileKeys; ++kk)
+          dst[kk] = *reinterpret_cast<const VRaw*>((kk < kTileKeys / 2 ? va : vb) + kk * T::kRowBytes + v_lane);
       };
 
       // Vector-memory operations complete in issue order and the K ring is awaited by count, so the order below is part of the
-      // protocol:  K_0, K_1 | V_0 | then per tile i:  K_{i+2}, (positions of i+1,) V_{i+1}
+      // protocol:  K_0, K_1 | V_0 | then per tile i:  K_{i+2}, V_{i+1}  (other loads among them only make a wait longer)
       int j0 = next_tile(), j1 = next_tile(), j2 = next_tile();   // current tile, the next, the one after
       if (j0 >= 0) issue_k(j0, 0);
       if (j1 >= 0) issue_k(j1, 1);
       asm volatile("" ::: "memory");
       VRaw v0[kTileKeys], v1[kTileKeys];
       if (j0 >= 0) load_v(v0, j0);
+      if (i0 == 0 && !last) {                                  // the next head of the share, while this one streams
+        do {
+          ++next_head;
+          next_rows = p.head_rows[next_head];
+          next_tiles = head_tiles(p, next_rows);
+        } while (next_tiles <= 0);                             // ends: the share goes on
+        const unsigned int n_at = at + (unsigned int)tiles + weight;
+        const int n_tb = t1 - n_at < (unsigned int)next_tiles ? (int)(t1 - n_at) : next_tiles;
+        const int n_first = (int)(((unsigned int)wave - done - (unsigned int)(tb - ta)) & (kDecWaves - 1));
+        const int n_cnt = n_first < n_tb ? (n_tb - n_first + kDecWaves - 1) / kDecWaves : 0;
+        load_pages(next_head, next_rows, n_first, n_cnt < kBlock ? n_cnt : kBlock, next_a, next_b);
+      }
 
       auto step = [&](auto par, VRaw (&v_cur)[kTileKeys], VRaw (&v_next)[kTileKeys]) {
         constexpr int PAR = decltype(par)::value;              // ring stage of the current tile
-        const int left = rows - (tile0 + kDecWaves * j0) * kTileKeys;   // rows from this tile on (uniform)
-        const unsigned int mask = POS ? lane_value(seen, j0) : 0xffffffffu;
+        const int left = rows - row_of(j0);                    // rows from this tile on
+        const unsigned int mask = OPT ? lane_value(seen, j0) : left >= kTileKeys ? ~0u : (1u << left) - 1u;   // rows that count
         {
           // everything older than this tile's V (32 loads) and, if it was requested, the next K has landed
           if (j1 >= 0) wait_vmcnt<T::kLoads + kTileKeys>(); else wait_vmcnt<kTileKeys>();
@@ -382,33 +399,25 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
             x2 = mfma_chunk<DT>(kf[j + 1], qf[j + 1], x2);
           }
           x += x2;                                             // x[v]: row 8*(v/4) + 4*half + v%4, head col
-          if (p.cap > 0.0f) {                                  // uniform
+          if (OPT && p.cap > 0.0f) {                           // uniform
 #pragma unroll
             for (int v = 0; v < 16; ++v) x[v] = capped(x[v] * p.scale, p.cap, inv_cap) * kLog2e;
           } else {
 #pragma unroll
             for (int v = 0; v < 16; ++v) x[v] *= a.c2;
           }
-          if (POS) {
+          if (OPT) {
             if (p.slopes != nullptr) {                         // uniform
-              const long long at = half_a(j0), bt = half_b(j0, at);
+              u32x4 y[4];
+              lds_read128x4_strided<32>(lds_addr(&s_back[wave][0]) + (unsigned int)(((j0 >> 2) * kTileKeys + 4 * half) * 4), y[0], y[1], y[2], y[3]);
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const int4 y = *reinterpret_cast<const int4*>(p.pos + (c < 2 ? at + 8 * c : bt + 8 * (c - 2)) + 4 * half);
-                x[4 * c] -= slope * (float)(q_pos - y.x);
-                x[4 * c + 1] -= slope * (float)(q_pos - y.y);
-                x[4 * c + 2] -= slope * (float)(q_pos - y.z);
-                x[4 * c + 3] -= slope * (float)(q_pos - y.w);
-              }
+              for (int v = 0; v < 16; ++v) x[v] -= slope * __uint_as_float(y[v / 4][v % 4]);
             }
+          }
+          if (mask != ~0u) {                                   // uniform; whatever the other rows hold
             const unsigned int my = mask >> (4 * half);
 #pragma unroll
             for (int v = 0; v < 16; ++v) x[v] = my & (1u << (8 * (v / 4) + v % 4)) ? x[v] : -INFINITY;
-          } else if (left < kTileKeys) {                       // a partial tile
-            int h4 = 4 * half;
-            asm volatile("" : "+v"(h4));                       // keeps this path's temporaries out of the hot loop
-#pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] = h4 + 8 * (v / 4) + (v % 4) < left ? x[v] : -INFINITY;
           }
           float mt = x[0];
 #pragma unroll
@@ -434,6 +443,10 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
         {
           if (j1 >= 0) load_v(v_next, j1);
           asm volatile("" ::: "memory");
+          if (mask != ~0u) {
+#pragma unroll
+            for (int kk = 0; kk < kTileKeys; ++kk) v_cur[kk] = (mask >> kk) & 1u ? v_cur[kk] : VRaw{};
+          }
           u32x4 al[kPs / 4];
           static_for<kPs / 4>([&](auto cc) {
             constexpr int c = decltype(cc)::value;
@@ -455,11 +468,6 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
             for (int kk = 0; kk < 4; ++kk) {
               float vx[kDpl];
               unpack_v<DT, D>(v_cur[k4 + kk], vx);
-              if (POS) {                                       // a masked row may hold anything
-                const bool take = (mask >> (k4 + kk)) & 1u;    // uniform
-#pragma unroll
-                for (int e = 0; e < kDpl; ++e) vx[e] = take ? vx[e] : 0.0f;
-              }
 #pragma unroll
               for (int i = 0; i < GP; ++i) {
                 const float pw = __uint_as_float(pr[i / 4][kk][i % 4]);
@@ -500,9 +508,8 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
 #pragma unroll
       for (int e = 0; e < kDpl; ++e) s_acc[wave][i][lane * kDpl + e] = acc[i][e];
     __syncthreads();
-    const bool bad = s_bad != 0;
     const bool whole = ta == 0 && tb == tiles;
-    const long long slot = ta > 0 ? 2 * (long long)blockIdx.x : 2 * (long long)blockIdx.x + 1;
+    const int slot = 2 * (int)blockIdx.x + (ta > 0 ? 0 : 1);
     constexpr int kPairs = GP * D / 2;
 #pragma unroll
     for (int j = 0; j < (kPairs + kDecThreads - 1) / kDecThreads; ++j) {
@@ -521,47 +528,55 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
         sum.x += wgt * s_acc[w2][i][e];
         sum.y += wgt * s_acc[w2][i][e + 1];
       }
-      if (bad) L = NAN;                                       // a page that is not in the pool: the head's result is none
       if (!whole) {
-        st_dev_f2(reinterpret_cast<float2*>(a.part_acc + slot * GP * D + idx), sum.x, sum.y);
+        st_dev_f2(reinterpret_cast<float2*>(a.part_acc + (long long)slot * (GP * D) + idx), sum.x, sum.y);
         if (e == 0) st_dev_f2(&a.part_ml[slot * GP + i], M, L);
       } else if (i < p.G) {
-        const long long row = (long long)b * p.H + (long long)g * p.G + i;
-        const bool none = L == 0.0f;                          // every row masked
-        p.out[row * D + e] = none ? 0.0f : sum.x / L;
-        p.out[row * D + e + 1] = none ? 0.0f : sum.y / L;
-        if (p.lse != nullptr && e == 0) p.lse[row] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        write_row<D>(p, b, g, i, e, M, L, sum);
       }
     }
     if (!whole) {
-      // ---------------- publish the part; merge the head if all its parts are published
-      drain_vmem();
-      __syncthreads();                                        // every thread's share of the part is visible to the device
-      const long long w0 = uniform64(quotient(head_start, share));
-      const int parts = (int)(uniform64(quotient(head_start + tiles - 1, share)) - w0) + 1;
-      if (wave == 0) {
-        if (lane == 0) {
-          st_dev(&a.flags[slot], a.tag);
-          drain_vmem();
-        }
-        bool all = true;
-        for (int i = lane; i < parts; i += 64) all &= ld_dev(&a.flags[part_slot(w0, i)]) == a.tag;
-        const bool every = __ballot(!all) == 0ull;
-        if (lane == 0) s_flag = every ? 1 : 0;
-      }
-      __syncthreads();
-      if (s_flag != 0) {
-        for (int i = threadIdx.x; i < parts; i += kDecThreads) st_dev(&a.flags[part_slot(w0, i)], 0ull);
-        static_assert(sizeof(s_tile) >= kPartChunk * GP * sizeof(float2), "the ring is the merge's buffer");
-        merge_parts<D, GP>(a, b, g, w0, parts, reinterpret_cast<float2 (*)[GP]>(&s_tile[0][0][0]));
-      }
+      const int w0 = (int)(by_heads ? head_start : at / share);
+      const int parts = by_heads ? (int)ceil_of((unsigned int)tiles, share) : (int)((at + (unsigned int)tiles - 1u) / share) - w0 + 1;
+      if (ta > 0) { pend_head[0] = hb; pend_w0[0] = w0; pend_parts[0] = parts; }
+      else { pend_head[1] = hb; pend_w0[1] = w0; pend_parts[1] = parts; }
     }
-    __syncthreads();                                          // the ring, s_m and s_bad are free again
-    if (threadIdx.x == 0) s_bad = 0;
-    t = head_start + tb;
-    head_start += tiles;
-    ++hb;
-    __syncthreads();
+    if (last) break;
+    __syncthreads();                                          // the ring and s_m are free again
+    head_start = at + (unsigned int)tiles;
+    done += (unsigned int)(tb - ta);
+    hb = next_head;
+    rows = next_rows;
+    tiles = next_tiles;
+    page_a = next_a;
+    page_b = next_b;
+    pages_ready = true;
+  }
+
+  // ---------------- publish the parts; merge every head all of whose parts are published
+  if (pend_parts[0] == 0 && pend_parts[1] == 0) return;       // uniform
+  drain_vmem();
+  __syncthreads();                                            // every thread's share of the parts is visible to the device
+  if (wave == 0) {
+    if (lane < 2 && (lane == 0 ? pend_parts[0] : pend_parts[1]) > 0) {
+      st_dev(&a.flags[2 * blockIdx.x + lane], a.tag);
+      drain_vmem();
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      bool all = pend_parts[i] > 0;
+      for (int u = lane; u < pend_parts[i]; u += 64) all &= ld_dev(&a.flags[part_slot(pend_w0[i], u)]) == a.tag;
+      const bool every = __ballot(!all) == 0ull;
+      if (lane == 0) s_flag[i] = every ? 1 : 0;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (s_flag[i] == 0) continue;
+    for (int u = threadIdx.x; u < pend_parts[i]; u += kDecThreads) st_dev(&a.flags[part_slot(pend_w0[i], u)], 0ull);
+    const int b = pend_head[i] / p.H_kv;
+    merge_parts<D, GP>(a, b, pend_head[i] - b * p.H_kv, pend_w0[i], pend_parts[i]);
   }
 }
 
@@ -590,11 +605,11 @@ PagedLayout make_layout(const lava_layer_desc& d) {
   return l;
 }
 
-template <int DT, int D, int GP, bool POS>
+template <int DT, int D, int GP, bool OPT>
 int32_t launch_one(const PagedArgs& a, hipStream_t s) {
-  static const int wgs = resident(paged_decode_kernel<DT, D, GP, POS>);
+  static const int wgs = resident(paged_decode_kernel<DT, D, GP, OPT>);
   ProfScope ps(KID_PAGED_DECODE, s);
-  hipLaunchKernelGGL((paged_decode_kernel<DT, D, GP, POS>), dim3((unsigned)wgs), dim3(kDecThreads), 0, s, a);
+  hipLaunchKernelGGL((paged_decode_kernel<DT, D, GP, OPT>), dim3((unsigned)wgs), dim3(kDecThreads), 0, s, a);
   return launch_status();
 }
 
@@ -612,9 +627,10 @@ int32_t launch_paged_decode(const lava_layer_desc& d, const PagedDecodeArgs& p, 
   a.flags = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + l.off_flags);
   a.tag = next_tag();
   const int gp = padded_group(p.G);
+  const bool options = p.pos != nullptr || p.cap > 0.0f;
 #define LAVA_PAGED_CASE(DT, D, GP) \
   if (d.dtype == DT && d.head_dim == D && gp == GP)        \
-    return p.pos != nullptr ? launch_one<DT, D, GP, true>(a, s) : launch_one<DT, D, GP, false>(a, s);
+    return options ? launch_one<DT, D, GP, true>(a, s) : launch_one<DT, D, GP, false>(a, s);
 #define LAVA_PAGED_GROUPS(DT, D) LAVA_PAGED_CASE(DT, D, 1) LAVA_PAGED_CASE(DT, D, 2) LAVA_PAGED_CASE(DT, D, 4) LAVA_PAGED_CASE(DT, D, 8)
   LAVA_PAGED_GROUPS(LAVA_BF16, 128)
   LAVA_PAGED_GROUPS(LAVA_BF16, 64)
