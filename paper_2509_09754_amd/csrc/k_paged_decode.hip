@@ -49,9 +49,34 @@ __device__ __forceinline__ int part_slot(int w0, int u) { return u == 0 ? 2 * w0
 
 // x / y rounded up, y > 0.
 __device__ __forceinline__ unsigned int ceil_of(unsigned int x, unsigned int y) { return x / y + (x % y != 0u ? 1u : 0u); }
+// The same for many x: inv is 1.0 / y, so the product is off by less than one.
+__device__ __forceinline__ unsigned int ceil_by(unsigned int x, unsigned int y, double inv) {
+  unsigned int q = (unsigned int)((double)x * inv);
+  const int r = (int)(x - q * y);
+  q = r < 0 ? q - 1u : r >= (int)y ? q + 1u : q;
+  return q * y < x ? q + 1u : q;
+}
 
 // What a workgroup that changes heads loses, in tiles.
 constexpr unsigned int kHeadCost = 6u;
+
+// With a window the rows that count lie together, and a run of tiles would have all of them or none.  The tiles of a head then take
+// their places column by column of a matrix of kSpread rows (place x is tile (x % kSpread) * columns + x / kSpread, or none),
+// so that every share has its part of the window, and (kSpread is odd) every wavefront of it.
+constexpr int kSpread = 17;
+__device__ __forceinline__ int spread_columns(int tiles, bool spread) { return spread && tiles >= 4 * kSpread ? (tiles + kSpread - 1) / kSpread : 0; }
+__device__ __forceinline__ int places_of(int tiles, bool spread) {
+  const int columns = spread_columns(tiles, spread);
+  return columns > 0 ? columns * kSpread : tiles;
+}
+// With a window a place of the line is not one tile but `per` of them: about as many as hold one that counts if the head's rows are spread
+// over the sequence's positions (and no more than finding out costs).  An estimate: it moves cuts, not results.
+constexpr int kMostPer = 8;
+__device__ __forceinline__ int tiles_per_place(int q_pos, int window) {
+  const int n = window > 0 && q_pos >= 0 ? (int)(((unsigned int)q_pos + 1u) / (unsigned int)window) : 1;
+  return n < 1 ? 1 : n > kMostPer ? kMostPer : n;
+}
+__device__ __forceinline__ int tile_at(int place, int columns) { return columns > 0 ? (place % kSpread) * columns + place / kSpread : place; }
 
 // Tiles of a head with that many rows; -1: it cannot have them.
 __device__ __forceinline__ int head_tiles(const PagedDecodeArgs& a, int rows) {
@@ -140,6 +165,7 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
   const int shift = p.page_shift, page_mask = (1 << shift) - 1;
 
   // ---------------- this workgroup's share: sums over all heads, 64 at a time
+  const bool spread = OPT && p.window > 0;
   constexpr int kHeld = 8;                                    // counts a lane holds at once: 512 heads in one trip to memory
   int held[kHeld];
   auto load_counts = [&](int h0) {
@@ -149,7 +175,10 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
       held[c] = h < n_heads ? p.head_rows[h] : 0;
     }
 #pragma unroll
-    for (int c = 0; c < kHeld; ++c) held[c] = head_tiles(p, held[c]);
+    for (int c = 0; c < kHeld; ++c) {
+      held[c] = places_of(head_tiles(p, held[c]), spread);
+      if (spread && held[c] > 0) held[c] = (int)ceil_of((unsigned int)held[c], (unsigned int)tiles_per_place(p.q_pos[(h0 + 64 * c + lane) / p.H_kv], p.window));
+    }
   };
   unsigned int mine = 0u, full = 0u;
   bool empty = false;
@@ -183,11 +212,12 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
 #pragma unroll 1
   for (int attempt = 0; attempt < 2 && !by_heads; ++attempt) {   // with shares as even as can be, then with those of the line
     share = ((attempt == 0 ? even : line) + 3u) & ~3u;        // a tile for every wavefront
+    const double inv = 1.0 / (double)share;
     unsigned int units = 0u;
     for (int h0 = 0; h0 < n_heads; h0 += 64 * kHeld) {
       if (n_heads > 64 * kHeld) load_counts(h0);
 #pragma unroll
-      for (int c = 0; c < kHeld; ++c) units += held[c] > 0 ? ceil_of((unsigned int)held[c], share) : 0u;
+      for (int c = 0; c < kHeld; ++c) units += held[c] > 0 ? ceil_by((unsigned int)held[c], share, inv) : 0u;
     }
     by_heads = lane_value(wave_incl(units), 63) <= wgs;       // at most one unit a head more than tiles / share: no overflow
   }
@@ -198,6 +228,7 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
   int hb = -1;
   unsigned int head_start = 0u;                               // units, or places, before the head
   {
+    const double inv = 1.0 / (double)share;
     unsigned int at = 0u;
     for (int h0 = 0; h0 < n_heads && hb < 0; h0 += 64 * kHeld) {
       if (n_heads > 64 * kHeld) load_counts(h0);
@@ -205,7 +236,7 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
       for (int c = 0; c < kHeld; ++c) {
         if (hb >= 0) continue;                                // uniform
         const unsigned int k = held[c] > 0 ? (unsigned int)held[c] : 0u;
-        const unsigned int n = k == 0u ? 0u : by_heads ? ceil_of(k, share) : k + weight, incl = wave_incl(n);
+        const unsigned int n = k == 0u ? 0u : by_heads ? ceil_by(k, share, inv) : k + weight, incl = wave_incl(n);
         const unsigned long long after = __ballot(at + incl > t0);
         if (after != 0ull) {
           const int l = __builtin_ctzll(after);
@@ -234,12 +265,12 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
   const unsigned int window = p.window > 0 ? (unsigned int)p.window : 0x80000000u;
 
   // Pages of tile0, tile0 + kDecWaves, ... of head h, kBlock of them, as far as there are `here`: a lane each, or four (OPT)
-  auto load_pages = [&](int h, int rows_h, int tile0, int here, int& page_a, int& page_b) {
+  auto load_pages = [&](int h, int rows_h, int columns, int tile0, int here, int& page_a, int& page_b) {
     const int i = OPT ? lane >> 2 : lane;
-    const int row0 = (tile0 + kDecWaves * i) * kTileKeys;
+    const int row0 = tile_at(tile0 + kDecWaves * i, columns) * kTileKeys;
     const int* table = p.block_table + (long long)h * p.max_blocks;
     page_a = page_b = 0;
-    if (i < here) {
+    if (i < here && (!OPT || row0 < rows_h)) {
       page_a = table[row0 >> shift];
       page_b = shift == 4 && row0 + 16 < rows_h ? table[(row0 >> 4) + 1] : page_a;
     }
@@ -247,7 +278,9 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
 
   // parts that wait to be published: of the first and the last head of the share
   int pend_head[2] = {-1, -1}, pend_w0[2] = {0, 0}, pend_parts[2] = {0, 0};
-  int rows = p.head_rows[hb], tiles = head_tiles(p, rows);
+  // of a head: its rows, the columns of its tiles' order, the tiles in that order, how many make a place, its places
+  int rows = p.head_rows[hb], columns = spread_columns(head_tiles(p, rows), spread), order = places_of(head_tiles(p, rows), spread);
+  int per = spread ? tiles_per_place(p.q_pos[hb / p.H_kv], p.window) : 1, tiles = OPT ? (order + per - 1) / per : order;
   int page_a, page_b;
   bool pages_ready = false;
   // In the line a head's tiles follow its weight: tile j is place head_start + weight + j.
@@ -256,7 +289,7 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
   for (;;) {
     const int b = hb / p.H_kv, g = hb - b * p.H_kv;
     const unsigned int at = head_start + weight;              // place of the head's first tile
-    int ta, tb;                                               // its tiles that are this share's
+    int ta, tb;                                               // its places that are this share's
     if (by_heads) {
       ta = (int)((t0 - head_start) * share);
       tb = tiles - ta < (int)share ? tiles : ta + (int)share;
@@ -268,9 +301,10 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
     const bool last = by_heads || at + (unsigned int)tiles + weight >= t1 || at + (unsigned int)tiles >= line_end;
     const int q_pos = OPT && p.pos != nullptr ? p.q_pos[b] : 0;
     // wavefronts take turns through the whole share, so that each has as many tiles as the others
-    const int first = ta + (int)(((unsigned int)wave - done) & (kDecWaves - 1));
-    const int cnt = first < tb ? (tb - first + kDecWaves - 1) / kDecWaves : 0;   // this wavefront's tiles
-    if (!pages_ready) load_pages(hb, rows, first, cnt < kBlock ? cnt : kBlock, page_a, page_b);
+    const int pa = OPT ? ta * per : ta, pb = OPT ? (tb == tiles ? order : tb * per) : tb;   // in the order of the head's tiles
+    const int first = pa + (int)(((unsigned int)wave - done) & (kDecWaves - 1));
+    const int cnt = first < pb ? (pb - first + kDecWaves - 1) / kDecWaves : 0;   // this wavefront's tiles
+    if (!pages_ready) load_pages(hb, rows, columns, first, cnt < kBlock ? cnt : kBlock, page_a, page_b);
 
     // the group's query rows as the 32-column operand: column t < G is head g * G + t
     u32x4 qf[T::kSteps];
@@ -289,11 +323,11 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
 #pragma unroll
       for (int e = 0; e < kDpl; ++e) acc[i][e] = 0.0f;
 
-    int next_head = hb, next_rows = 0, next_tiles = 0, next_a = 0, next_b = 0;
+    int next_head = hb, next_rows = 0, next_columns = 0, next_order = 0, next_per = 1, next_tiles = 0, next_a = 0, next_b = 0;
     for (int i0 = 0; i0 == 0 || i0 < cnt; i0 += kBlock) {
       const int tile0 = first + kDecWaves * i0;
       const int here = cnt - i0 < kBlock ? cnt - i0 : kBlock;
-      if (i0 > 0) load_pages(hb, rows, tile0, here, page_a, page_b);
+      if (i0 > 0) load_pages(hb, rows, columns, tile0, here, page_a, page_b);
       unsigned int seen = 0xffffffffu;                        // rows of the lane's tile that count (OPT)
       {
         const bool bad = page_a < 0 || page_a >= p.n_pages || page_b < 0 || page_b >= p.n_pages;
@@ -303,9 +337,9 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
         }
         if (OPT) {
           const int i = lane >> 2, part = lane & 3;           // rows 8 part .. 8 part + 7 of tile i
-          const int row0 = (tile0 + kDecWaves * i) * kTileKeys;
+          const int row0 = tile_at(tile0 + kDecWaves * i, columns) * kTileKeys;
           seen = 0u;
-          if (i < here) {
+          if (i < here && row0 < rows) {
             int4 x = make_int4(q_pos, q_pos, q_pos, q_pos), x2 = x;
             if (p.pos != nullptr) {                            // uniform
               const long long place = shift == 4 ? ((long long)(part < 2 ? page_a : page_b) << 4) + 8 * (part & 1)
@@ -331,7 +365,7 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
         }
       }
       unsigned long long todo = OPT ? __ballot(seen != 0u) & 0x1111111111111111ull : here == 64 ? ~0ull : (1ull << here) - 1ull;
-      auto row_of = [&](int j) -> int { return (tile0 + kDecWaves * (OPT ? j >> 2 : j)) * kTileKeys; };   // first row of lane j's tile
+      auto row_of = [&](int j) -> int { return tile_at(tile0 + kDecWaves * (OPT ? j >> 2 : j), OPT ? columns : 0) * kTileKeys; };   // first row of lane j's tile
       // place in the pool of the first rows of the tile's two halves
       auto half_a = [&](int j) -> long long {
         return ((long long)(int)lane_value((unsigned int)page_a, j) << shift) + (row_of(j) & page_mask);
@@ -374,11 +408,17 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
           next_rows = p.head_rows[next_head];
           next_tiles = head_tiles(p, next_rows);
         } while (next_tiles <= 0);                             // ends: the share goes on
+        next_columns = spread_columns(next_tiles, spread);
+        next_tiles = next_order = places_of(next_tiles, spread);
+        if (spread) {
+          next_per = tiles_per_place(p.q_pos[next_head / p.H_kv], p.window);
+          next_tiles = (next_order + next_per - 1) / next_per;
+        }
         const unsigned int n_at = at + (unsigned int)tiles + weight;
-        const int n_tb = t1 - n_at < (unsigned int)next_tiles ? (int)(t1 - n_at) : next_tiles;
-        const int n_first = (int)(((unsigned int)wave - done - (unsigned int)(tb - ta)) & (kDecWaves - 1));
+        const int n_tb = t1 - n_at < (unsigned int)next_tiles ? (int)(t1 - n_at) * next_per : next_order;
+        const int n_first = (int)(((unsigned int)wave - done - (unsigned int)(pb - pa)) & (kDecWaves - 1));
         const int n_cnt = n_first < n_tb ? (n_tb - n_first + kDecWaves - 1) / kDecWaves : 0;
-        load_pages(next_head, next_rows, n_first, n_cnt < kBlock ? n_cnt : kBlock, next_a, next_b);
+        load_pages(next_head, next_rows, next_columns, n_first, n_cnt < kBlock ? n_cnt : kBlock, next_a, next_b);
       }
 
       auto step = [&](auto par, VRaw (&v_cur)[kTileKeys], VRaw (&v_next)[kTileKeys]) {
@@ -544,10 +584,13 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
     if (last) break;
     __syncthreads();                                          // the ring and s_m are free again
     head_start = at + (unsigned int)tiles;
-    done += (unsigned int)(tb - ta);
+    done += (unsigned int)(pb - pa);
     hb = next_head;
     rows = next_rows;
     tiles = next_tiles;
+    columns = next_columns;
+    order = next_order;
+    per = next_per;
     page_a = next_a;
     page_b = next_b;
     pages_ready = true;

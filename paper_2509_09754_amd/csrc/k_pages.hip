@@ -4,6 +4,10 @@
 // A step's tables are exclusive sums over the heads in order: head i needs ceil((old + add) / P) - ceil(old / P)
 // pages and pops them behind those of the heads before it.  Everything else follows from the sums: which page a
 // new block gets is one look-up in the stack, which slot a new row has is one look-up in the stack or the table.
+//
+// A step with little to write, as a decode step is, is one launch of one workgroup: a chain of four trips to memory.  For a large
+// one a first launch forms the sums, a workgroup for every 1024 heads, and every workgroup of the second adds up the
+// workgroups' totals for itself; that launch fills the device and is bound by the slots it writes, 8 bytes a row.
 #include "common.h"
 
 namespace lava {
@@ -13,59 +17,77 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / 64;
 
-// What the plan leaves in the workspace for the fill.
-struct PlanHeader {
-  int error;             // LAVA_PAGES_* bits; 0: the step is carried out
-  int top;               // pages on the stack once those given back are on it
-  int tokens;            // new tokens of all sequences
-  int pad;
+// What the sums' launch leaves in the workspace.  Heads, and sequences, are summed in chunks, at most kMaxChunks of them.
+constexpr int kMaxChunks = 256;
+struct ChunkTotals {
+  unsigned long long need, back;   // of a chunk of heads: pages needed, pages given back; of sequences: tokens, -
+  int error;                       // LAVA_PAGES_* bits
+  int n_free;                      // of the first chunk of heads: the stack's pages when the step began (n_free_out may be n_free)
 };
 struct PlanLayout {
-  size_t off_old;        // int [heads]      rows every head starts the step with (0 where it is over)
-  size_t off_need;       // int [heads + 1]  pages needed by the heads before
-  size_t off_back;       // int [heads + 1]  pages given back by the heads before
-  size_t off_tok;        // int [batch + 1]  new tokens of the sequences before
-  size_t off_pos;        // int [batch]      position of every sequence's first new token
-  size_t bytes;
+  size_t off_old;        // int [heads]   rows every head starts the step with (0 where it is over)
+  size_t off_need;       // int [heads]   pages needed by the heads of the chunk before
+  size_t off_back;       // int [heads]   pages given back by them
+  size_t off_tok;        // int [batch]   new tokens of the sequences of the chunk before
+  size_t off_pos;        // int [batch]   position of every sequence's first new token
+  size_t bytes;          // at 0: ChunkTotals [2][kMaxChunks], of the heads' chunks and of the sequences'
 };
 __host__ __device__ inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 __host__ __device__ inline PlanLayout plan_layout(int batch, int heads) {
   PlanLayout l;
-  l.off_old = 256;
+  l.off_old = up256(2 * kMaxChunks * sizeof(ChunkTotals));
   l.off_need = l.off_old + up256((size_t)heads * 4);
-  l.off_back = l.off_need + up256((size_t)(heads + 1) * 4);
-  l.off_tok = l.off_back + up256((size_t)(heads + 1) * 4);
-  l.off_pos = l.off_tok + up256((size_t)(batch + 1) * 4);
+  l.off_back = l.off_need + up256((size_t)heads * 4);
+  l.off_tok = l.off_back + up256((size_t)heads * 4);
+  l.off_pos = l.off_tok + up256((size_t)batch * 4);
   l.bytes = l.off_pos + up256((size_t)batch * 4);
   return l;
 }
 
-__device__ __forceinline__ long long shfl_up64(long long x, int d) {
-  const int lo = __shfl_up((int)(unsigned int)x, d), hi = __shfl_up((int)(x >> 32), d);
-  return ((long long)hi << 32) | (unsigned int)lo;
-}
-
-// Exclusive sum over the workgroup's threads; *total: the sum over all.
-__device__ __forceinline__ long long block_scan(long long x, long long* s_part, long long* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  long long incl = x;
+// Inclusive sum over the lanes of a wavefront.
+__device__ __forceinline__ unsigned int lane_sum(unsigned int x) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const long long y = shfl_up64(incl, d);
-    if (lane >= d) incl += y;
+    const unsigned int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
   }
-  if (lane == 63) s_part[wave] = incl;
-  __syncthreads();
-  long long before = 0, all = 0;
+  return x;
+}
+__device__ __forceinline__ unsigned long long wave_total(unsigned long long x) {
 #pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) {
-    const long long p = s_part[w];
-    if (w < wave) before += p;
-    all += p;
+  for (int d = 32; d > 0; d >>= 1) {
+    const unsigned int lo = __shfl_xor((unsigned int)x, d), hi = __shfl_xor((unsigned int)(x >> 32), d);
+    x += ((unsigned long long)hi << 32) | lo;
+  }
+  return x;
+}
+
+// Exclusive sums of a workgroup's values x[u] of items u * kPlanThreads + thread, in the order of the items.  32 bits: where they
+// could overflow the 64-bit totals refuse the step.
+template <int PER>
+__device__ __forceinline__ void plan_scan(unsigned int (&x)[PER], unsigned int* s_part) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned int incl[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    incl[u] = lane_sum(x[u]);
+    if (lane == 63) s_part[u * kPlanWaves + wave] = incl[u];
   }
   __syncthreads();
-  *total = all;
-  return before + incl - x;
+  if (wave == 0) {                                                 // sums of the wavefronts' sums, 64 at a time
+    unsigned int carry = 0u;
+    for (int i0 = 0; i0 < PER * kPlanWaves; i0 += 64) {
+      const int i = i0 + lane;
+      const unsigned int v = i < PER * kPlanWaves ? s_part[i] : 0u, s = lane_sum(v);
+      if (i < PER * kPlanWaves) s_part[i] = carry + s - v;
+      carry += __shfl(s, 63);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < PER; ++u) x[u] = s_part[u * kPlanWaves + wave] + incl[u] - x[u];
+  __syncthreads();
 }
 
 struct HeadStep {
@@ -94,151 +116,333 @@ __device__ __forceinline__ HeadStep head_step(const PageTablesArgs& a, int hb) {
   return h;
 }
 
-// The sums, by one workgroup.
-__global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PageTablesArgs a) {
-  __shared__ long long s_part[kPlanWaves];
-  __shared__ int s_error;
-  const int heads = a.batch * a.heads;
-  const PlanLayout l = plan_layout(a.batch, heads);
-  char* ws = static_cast<char*>(a.ws);
-  int* w_old = reinterpret_cast<int*>(ws + l.off_old);
-  int* w_need = reinterpret_cast<int*>(ws + l.off_need);
-  int* w_back = reinterpret_cast<int*>(ws + l.off_back);
-  int* w_tok = reinterpret_cast<int*>(ws + l.off_tok);
-  int* w_pos = reinterpret_cast<int*>(ws + l.off_pos);
-  if (threadIdx.x == 0) s_error = 0;
-  __syncthreads();
-  int error = 0;
-  long long need = 0, back = 0, tokens = 0;
-  for (int h0 = 0; h0 < heads; h0 += kPlanThreads) {
-    const int hb = h0 + (int)threadIdx.x;
-    HeadStep h = {0, 0, 0, 0, 0};
-    if (hb < heads) h = head_step(a, hb);
-    error |= h.error;
-    long long t_need, t_back;
-    const long long n0 = block_scan(h.need, s_part, &t_need), b0 = block_scan(h.back, s_part, &t_back);
-    if (hb < heads) {
-      w_old[hb] = h.old;
-      w_need[hb] = (int)(need + n0);       // read only if the step is carried out: the sum is below 2^31 then
-      w_back[hb] = (int)(back + b0);
-    }
-    need += t_need;
-    back += t_back;
-  }
-  for (int s0 = 0; s0 < a.batch; s0 += kPlanThreads) {
-    const int b = s0 + (int)threadIdx.x;
-    int n = 0;
-    if (b < a.batch) {
-      n = a.n_new != nullptr ? a.n_new[b] : 0;
-      const bool over = a.release != nullptr && a.release[b] != 0;
-      const int pos = over ? 0 : a.st.seq_pos[b];
-      if (n < 0 || pos < 0 || (long long)pos + n >= (long long)1 << 31) {
-        error |= LAVA_PAGES_INVALID;
-        n = 0;
-      }
-      w_pos[b] = pos;
-    }
-    long long t_tok;
-    const long long t0 = block_scan(n, s_part, &t_tok);
-    if (b < a.batch) w_tok[b] = (int)(tokens + t0);
-    tokens += t_tok;
-  }
-  const long long free_pages = a.st.n_free[0];
-  if (free_pages < 0 || free_pages + back > a.n_pages) error |= LAVA_PAGES_INVALID;
-  else if (need > free_pages + back) error |= LAVA_PAGES_EXHAUSTED;
-  if (a.slots != nullptr || a.positions != nullptr) {
-    if (tokens > a.max_tokens) error |= LAVA_PAGES_TOKENS;
-  }
-  if (error != 0) atomicOr(&s_error, error);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    w_need[heads] = (int)need;
-    w_back[heads] = (int)back;
-    w_tok[a.batch] = (int)tokens;
-    PlanHeader* hd = reinterpret_cast<PlanHeader*>(ws);
-    hd->error = s_error;
-    hd->top = (int)(free_pages + back);
-    hd->tokens = (int)tokens;
-    if (s_error != 0 && a.st.error != nullptr) atomicOr(a.st.error, s_error);
-  }
-}
+// The sums as the steps that use them see them: in LDS from the one workgroup (chunk = 31: one chunk of all), or in the workspace with
+// the sums of the chunks before in LDS.
+struct PlanSums {
+  const int *old, *need, *back, *tok, *pos;
+  const int *base_need, *base_back, *base_tok;   // [chunks]
+  int chunk;                                       // log2 of a chunk
+  int heads, batch, total_need, total_back, total_tok;
+  __device__ __forceinline__ int need_at(int hb) const { return hb < heads ? need[hb] + base_need[hb >> chunk] : total_need; }
+  __device__ __forceinline__ int back_at(int hb) const { return hb < heads ? back[hb] + base_back[hb >> chunk] : total_back; }
+  __device__ __forceinline__ int tok_at(int b) const { return b < batch ? tok[b] + base_tok[b >> chunk] : total_tok; }
+};
 
 // Pages of the sequences that are over, onto the stack: a wavefront per head.
-__global__ void __launch_bounds__(256) page_return_kernel(const PageTablesArgs a) {
-  const char* ws = static_cast<const char*>(a.ws);
-  if (reinterpret_cast<const PlanHeader*>(ws)->error != 0) return;
-  const int heads = a.batch * a.heads;
-  const PlanLayout l = plan_layout(a.batch, heads);
-  const int* w_back = reinterpret_cast<const int*>(ws + l.off_back);
-  const int lane = threadIdx.x & 63;
-  const int free_pages = reinterpret_cast<const PlanHeader*>(ws)->top - w_back[heads];
-  for (int hb = blockIdx.x * 4 + (threadIdx.x >> 6); hb < heads; hb += gridDim.x * 4) {
-    const int first = w_back[hb], n = w_back[hb + 1] - first;
+__device__ __forceinline__ void give_back(const PageTablesArgs& a, const PlanSums& w, int free_pages, int first, int step) {
+  const int lane = threadIdx.x & 63, heads = a.batch * a.heads;
+  for (int hb = first; hb < heads; hb += step) {
+    const int at = w.back_at(hb), n = w.back_at(hb + 1) - at;
     const int* table = a.st.block_table + (long long)hb * a.max_blocks;
-    for (int j = lane; j < n; j += 64) a.st.free_pages[free_pages + first + j] = table[j];
+    for (int j = lane; j < n; j += 64) a.st.free_pages[free_pages + at + j] = table[j];
   }
 }
 
-// Tables, counts, slots and positions.  The first `head_wgs` workgroups take the heads (a wavefront each), the others
-// the tokens.
-__global__ void __launch_bounds__(256) page_fill_kernel(const PageTablesArgs a, const int head_wgs) {
-  const char* ws = static_cast<const char*>(a.ws);
-  const PlanHeader hd = *reinterpret_cast<const PlanHeader*>(ws);
-  const int heads = a.batch * a.heads;
-  const PlanLayout l = plan_layout(a.batch, heads);
-  const int* w_old = reinterpret_cast<const int*>(ws + l.off_old);
-  const int* w_need = reinterpret_cast<const int*>(ws + l.off_need);
-  const int* w_tok = reinterpret_cast<const int*>(ws + l.off_tok);
-  const int* w_pos = reinterpret_cast<const int*>(ws + l.off_pos);
-  const int mask = (1 << a.page_shift) - 1;
-  const int lane = threadIdx.x & 63;
-  if ((int)blockIdx.x < head_wgs) {
-    for (int hb = blockIdx.x * 4 + (threadIdx.x >> 6); hb < heads; hb += head_wgs * 4) {
-      const int b = hb / a.heads;
-      if (hd.error != 0) {
-        if (lane == 0) a.st.head_rows_out[hb] = a.st.head_rows[hb];
-        continue;
-      }
-      const int old = w_old[hb], start = w_need[hb], need = w_need[hb + 1] - start;
-      const int first = (old + mask) >> a.page_shift;
-      int* table = a.st.block_table + (long long)hb * a.max_blocks + first;
-      for (int j = lane; j < need; j += 64) table[j] = a.st.free_pages[hd.top - 1 - start - j];
-      if (lane == 0) {
-        const int add = a.head_counts != nullptr ? a.head_counts[hb] : a.n_new != nullptr ? a.n_new[b] : 0;
-        a.st.head_rows_out[hb] = old + add;
-      }
+// Tables and counts of the heads: a thread per head, or a wavefront where heads may take many pages at once.
+template <bool WAVE>
+__device__ __forceinline__ void fill_heads(const PageTablesArgs& a, const PlanSums& w, int top, int first, int step) {
+  const int lane = WAVE ? threadIdx.x & 63 : 0, lanes = WAVE ? 64 : 1, heads = a.batch * a.heads, mask = (1 << a.page_shift) - 1;
+  for (int hb = first; hb < heads; hb += step) {
+    const int old = w.old[hb], start = w.need_at(hb), need = w.need_at(hb + 1) - start;
+    int* table = a.st.block_table + (long long)hb * a.max_blocks + ((old + mask) >> a.page_shift);
+    for (int j = lane; j < need; j += lanes) table[j] = a.st.free_pages[top - 1 - start - j];
+    if (lane == 0) {
+      const int add = a.head_counts != nullptr ? a.head_counts[hb] : a.n_new != nullptr ? a.n_new[hb / a.heads] : 0;
+      a.st.head_rows_out[hb] = old + add;
     }
-    for (int b = blockIdx.x * 256 + (int)threadIdx.x; b < a.batch; b += head_wgs * 256) {
-      const int pos = a.st.seq_pos[b], n = a.n_new != nullptr ? a.n_new[b] : 0;
-      const bool over = a.release != nullptr && a.release[b] != 0;
-      a.st.seq_pos_out[b] = hd.error != 0 ? pos : (over ? 0 : pos) + n;
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0)
-      a.st.n_free_out[0] = hd.error != 0 ? a.st.n_free[0] : hd.top - w_need[heads];
-    return;
   }
-  const int wg = blockIdx.x - head_wgs, wgs = gridDim.x - head_wgs;
-  const long long all = a.max_tokens * a.heads, real = hd.error != 0 ? 0 : (long long)hd.tokens * a.heads;
-  for (long long e = (long long)wg * 256 + (int)threadIdx.x; e < all; e += (long long)wgs * 256) {
-    const int t = (int)(e / a.heads), g = (int)(e - (long long)t * a.heads);
-    if (e >= real) {
+}
+
+// Slots and positions of `count` (token, head) places from place e on, `stride` apart; `tokens` of the tokens are real.
+__device__ __forceinline__ void fill_slots(const PageTablesArgs& a, const PlanSums& w, int top, int tokens, unsigned int e,
+                                           unsigned int stride, int count) {
+  const unsigned int all = (unsigned int)(a.max_tokens * a.heads), heads = (unsigned int)a.heads;
+  const int mask = (1 << a.page_shift) - 1;
+  const bool same_head = stride % heads == 0u;                       // uniform
+  unsigned int t = e / heads, g = e - t * heads;
+  int b = -1, end = 0, begin = 0, old = 0, start = 0, pos = 0, hb = 0;   // of the sequence (b >= 0) and its head
+  for (int i = 0; i < count && e < all; ++i, e += stride) {
+    if (i > 0) {
+      if (same_head) {
+        t += stride / heads;
+      } else {
+        t = e / heads;
+        g = e - t * heads;
+      }
+    }
+    if ((int)t >= tokens) {
       if (a.slots != nullptr) a.slots[e] = -1;
-      if (a.positions != nullptr && g == 0) a.positions[t] = -1;
+      if (a.positions != nullptr && g == 0u) a.positions[t] = -1;
       continue;
     }
-    int lo = 0, hi = a.batch - 1;                             // the sequence: the last one that starts at or before t
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (w_tok[mid] <= t) lo = mid; else hi = mid - 1;
+    if (b < 0 || (int)t >= end || !same_head) {
+      if (b < 0) {                                                   // the last sequence that starts at or before t
+        int lo = 0, hi = a.batch - 1;
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (w.tok_at(mid) <= (int)t) lo = mid; else hi = mid - 1;
+        }
+        b = lo;
+      } else {
+        while ((int)t >= w.tok_at(b + 1)) ++b;                       // ends: t < tokens = tok_at(batch)
+      }
+      begin = w.tok_at(b);
+      end = w.tok_at(b + 1);
+      hb = b * a.heads + (int)g;
+      old = w.old[hb];
+      start = w.need_at(hb);
+      pos = w.pos[b];
     }
-    const int i = t - w_tok[lo];
-    if (a.positions != nullptr && g == 0) a.positions[t] = w_pos[lo] + i;
+    if (a.positions != nullptr && g == 0u) a.positions[t] = pos + (int)t - begin;
     if (a.slots == nullptr) continue;
-    const int hb = lo * a.heads + g, old = w_old[hb], r = old + i;
-    const int block = r >> a.page_shift, first = (old + mask) >> a.page_shift;
-    const int page = block < first ? a.st.block_table[(long long)hb * a.max_blocks + block]
-                                   : a.st.free_pages[hd.top - 1 - w_need[hb] - (block - first)];
+    const int r = old + (int)t - begin, block = r >> a.page_shift, owned = (old + mask) >> a.page_shift;
+    const int page = block < owned ? a.st.block_table[(long long)hb * a.max_blocks + block]
+                                   : a.st.free_pages[top - 1 - start - (block - owned)];
     a.slots[e] = ((long long)page << a.page_shift) + (r & mask);
+  }
+}
+
+// What sequence b does: its tokens (0 where it cannot be), its first position.
+__device__ __forceinline__ int seq_step(const PageTablesArgs& a, int b, int& pos, int& error) {
+  const int n = a.n_new != nullptr ? a.n_new[b] : 0;
+  pos = a.release != nullptr && a.release[b] != 0 ? 0 : a.st.seq_pos[b];
+  if (n >= 0 && pos >= 0 && (long long)pos + n < (long long)1 << 31) return n;
+  error |= LAVA_PAGES_INVALID;
+  return 0;
+}
+
+// May the step be carried out?
+__device__ __forceinline__ int verdict(const PageTablesArgs& a, int error, long long free_pages, unsigned long long need,
+                                       unsigned long long back, unsigned long long tokens) {
+  if (free_pages < 0 || free_pages + (long long)back > a.n_pages) error |= LAVA_PAGES_INVALID;
+  else if ((long long)need > free_pages + (long long)back) error |= LAVA_PAGES_EXHAUSTED;
+  if (a.max_tokens > 0 && tokens > (unsigned long long)a.max_tokens) error |= LAVA_PAGES_TOKENS;
+  return error;
+}
+
+// A whole step by one workgroup.
+constexpr int kOnePer = 2, kOneHeads = kOnePer * kPlanThreads;
+__global__ void __launch_bounds__(kPlanThreads) page_step_kernel(const PageTablesArgs a) {
+  __shared__ unsigned int s_part[kOnePer * kPlanWaves];
+  __shared__ unsigned long long s_total[3];                          // pages needed, pages given back, tokens
+  __shared__ int s_error, s_zero;
+  __shared__ int s_old[kOneHeads], s_need[kOneHeads], s_back[kOneHeads], s_tok[kOneHeads], s_pos[kOneHeads];
+  const int heads = a.batch * a.heads;
+  if (threadIdx.x == 0) s_error = s_zero = 0;
+  if (threadIdx.x < 3) s_total[threadIdx.x] = 0ull;
+  int error = 0;
+  unsigned int need[kOnePer], back[kOnePer], tok[kOnePer];
+  unsigned long long all_need = 0ull, all_back = 0ull, all_tok = 0ull;
+#pragma unroll
+  for (int u = 0; u < kOnePer; ++u) {
+    const int hb = u * kPlanThreads + (int)threadIdx.x;
+    HeadStep h = {0, 0, 0, 0, 0};
+    if (hb < heads) {
+      h = head_step(a, hb);
+      s_old[hb] = h.old;
+    }
+    int n = 0, pos = 0;
+    if (hb < a.batch) {
+      n = seq_step(a, hb, pos, error);
+      s_pos[hb] = pos;
+    }
+    error |= h.error;
+    all_need += need[u] = (unsigned int)h.need;
+    all_back += back[u] = (unsigned int)h.back;
+    all_tok += tok[u] = (unsigned int)n;
+  }
+  __syncthreads();                                                   // the totals are zero
+  all_need = wave_total(all_need);
+  all_tok = wave_total(all_tok);
+  if (a.release != nullptr) all_back = wave_total(all_back);         // uniform
+  if ((threadIdx.x & 63) == 0) {
+    if (all_need != 0ull) atomicAdd(&s_total[0], all_need);
+    if (a.release != nullptr && all_back != 0ull) atomicAdd(&s_total[1], all_back);
+    if (all_tok != 0ull) atomicAdd(&s_total[2], all_tok);
+  }
+  if (error != 0) atomicOr(&s_error, error);
+  plan_scan<kOnePer>(need, s_part);
+  if (a.release != nullptr) plan_scan<kOnePer>(back, s_part);
+  if (a.max_tokens > 0) plan_scan<kOnePer>(tok, s_part);
+#pragma unroll
+  for (int u = 0; u < kOnePer; ++u) {
+    const int hb = u * kPlanThreads + (int)threadIdx.x;
+    s_need[hb] = (int)need[u];
+    s_back[hb] = (int)back[u];
+    s_tok[hb] = (int)tok[u];
+  }
+  const long long free_pages = a.st.n_free[0];
+  __syncthreads();                                                   // every thread has read n_free, which n_free_out may be
+  error = verdict(a, s_error, free_pages, s_total[0], s_total[1], s_total[2]);   // the same in every thread
+  const int top = (int)(free_pages + (long long)s_total[1]);
+  if (threadIdx.x == 0 && error != 0 && a.st.error != nullptr) atomicOr(a.st.error, error);
+  const PlanSums w = {s_old, s_need, s_back, s_tok, s_pos, &s_zero, &s_zero, &s_zero, 31, heads, a.batch, (int)s_total[0], (int)s_total[1], (int)s_total[2]};
+  const int wave = threadIdx.x >> 6;
+  if (error == 0 && a.release != nullptr) {
+    give_back(a, w, (int)free_pages, wave, kPlanWaves);
+    __syncthreads();                                                 // the stack's new pages, for this workgroup to read
+  }
+  if (a.max_tokens > 0) {
+    const unsigned int places = (unsigned int)(a.max_tokens * a.heads);
+    fill_slots(a, w, top, error != 0 ? 0 : w.total_tok, threadIdx.x, kPlanThreads, (int)((places + kPlanThreads - 1) / kPlanThreads));
+  }
+  if (error == 0) {
+    fill_heads<false>(a, w, top, threadIdx.x, kPlanThreads);
+  } else {
+    for (int hb = threadIdx.x; hb < heads; hb += kPlanThreads) a.st.head_rows_out[hb] = a.st.head_rows[hb];
+  }
+  for (int b = threadIdx.x; b < a.batch; b += kPlanThreads)
+    a.st.seq_pos_out[b] = error != 0 ? a.st.seq_pos[b] : s_pos[b] + (a.n_new != nullptr ? a.n_new[b] : 0);
+  if (threadIdx.x == 0) a.st.n_free_out[0] = error != 0 ? (int)free_pages : top - w.total_need;
+}
+
+// Sums of the chunks: the first `head_chunks` workgroups of heads, the others of sequences, PER * 1024 each.
+template <int PER>
+__global__ void __launch_bounds__(kPlanThreads) page_sums_kernel(const PageTablesArgs a, const int head_chunks) {
+  __shared__ unsigned int s_part[PER * kPlanWaves];
+  __shared__ unsigned long long s_total[2];
+  __shared__ int s_error;
+  const bool of_heads = (int)blockIdx.x < head_chunks;
+  const int chunk = of_heads ? blockIdx.x : blockIdx.x - head_chunks, items = of_heads ? a.batch * a.heads : a.batch;
+  const PlanLayout l = plan_layout(a.batch, a.batch * a.heads);
+  char* ws = static_cast<char*>(a.ws);
+  if (threadIdx.x == 0) s_error = 0;
+  if (threadIdx.x < 2) s_total[threadIdx.x] = 0ull;
+  int error = 0;
+  unsigned int x[PER], y[PER];
+  unsigned long long all_x = 0ull, all_y = 0ull;
+  int* first = reinterpret_cast<int*>(ws + (of_heads ? l.off_old : l.off_pos));
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int i = (chunk * PER + u) * kPlanThreads + (int)threadIdx.x;
+    x[u] = y[u] = 0u;
+    if (i < items) {
+      if (of_heads) {
+        const HeadStep h = head_step(a, i);
+        error |= h.error;
+        x[u] = (unsigned int)h.need;
+        y[u] = (unsigned int)h.back;
+        first[i] = h.old;
+      } else {
+        int pos;
+        x[u] = (unsigned int)seq_step(a, i, pos, error);
+        first[i] = pos;
+      }
+    }
+    all_x += x[u];
+    all_y += y[u];
+  }
+  __syncthreads();
+  const bool backs = of_heads && a.release != nullptr;               // uniform
+  all_x = wave_total(all_x);
+  if (backs) all_y = wave_total(all_y);
+  if ((threadIdx.x & 63) == 0) {
+    atomicAdd(&s_total[0], all_x);
+    if (backs) atomicAdd(&s_total[1], all_y);
+  }
+  if (error != 0) atomicOr(&s_error, error);
+  plan_scan<PER>(x, s_part);
+  if (backs) plan_scan<PER>(y, s_part);
+  int* out = reinterpret_cast<int*>(ws + (of_heads ? l.off_need : l.off_tok));
+  int* out_back = reinterpret_cast<int*>(ws + l.off_back);
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int i = (chunk * PER + u) * kPlanThreads + (int)threadIdx.x;
+    if (i < items) {
+      out[i] = (int)x[u];
+      if (backs) out_back[i] = (int)y[u];
+    }
+  }
+  if (threadIdx.x == 0)
+    reinterpret_cast<ChunkTotals*>(ws)[(of_heads ? 0 : kMaxChunks) + chunk] = ChunkTotals{s_total[0], s_total[1], s_error, a.st.n_free[0]};
+}
+
+// What a workgroup of 256 threads of the second launch needs of the totals: sums of the chunks before, and the verdict.
+struct FillPlan {
+  int base_need[kMaxChunks], base_back[kMaxChunks], base_tok[kMaxChunks];
+  unsigned long long part[3][4], total[3];
+  int error;
+};
+__device__ __forceinline__ unsigned long long lane_sum64(unsigned long long x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const unsigned int lo = __shfl_up((unsigned int)x, d), hi = __shfl_up((unsigned int)(x >> 32), d);
+    if (lane >= d) x += ((unsigned long long)hi << 32) | lo;
+  }
+  return x;
+}
+__device__ __forceinline__ PlanSums add_up(const PageTablesArgs& a, int chunk, FillPlan& f, int& error, int& top, int& n_free) {
+  const char* ws = static_cast<const char*>(a.ws);
+  const int heads = a.batch * a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int head_chunks = ((heads - 1) >> chunk) + 1, seq_chunks = ((a.batch - 1) >> chunk) + 1;
+  const PlanLayout l = plan_layout(a.batch, heads);
+  const ChunkTotals* totals = reinterpret_cast<const ChunkTotals*>(ws);
+  ChunkTotals h = {0ull, 0ull, 0, 0}, s = h;
+  if ((int)threadIdx.x < head_chunks) h = totals[threadIdx.x];
+  if ((int)threadIdx.x < seq_chunks) s = totals[kMaxChunks + threadIdx.x];
+  if (threadIdx.x == 0) f.error = 0;
+  unsigned long long x[3] = {h.need, h.back, s.need}, incl[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    incl[i] = lane_sum64(x[i]);
+    if (lane == 63) f.part[i][wave] = incl[i];
+  }
+  __syncthreads();
+  if ((h.error | s.error) != 0) atomicOr(&f.error, h.error | s.error);
+  unsigned long long before[3] = {0ull, 0ull, 0ull}, total[3] = {0ull, 0ull, 0ull};
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      if (v < wave) before[i] += f.part[i][v];
+      total[i] += f.part[i][v];
+    }
+  f.base_need[threadIdx.x] = (int)(before[0] + incl[0] - x[0]);
+  f.base_back[threadIdx.x] = (int)(before[1] + incl[1] - x[1]);
+  f.base_tok[threadIdx.x] = (int)(before[2] + incl[2] - x[2]);
+  __syncthreads();
+  n_free = totals[0].n_free;
+  error = verdict(a, f.error, n_free, total[0], total[1], total[2]);
+  top = (int)(n_free + (long long)total[1]);
+  return {reinterpret_cast<const int*>(ws + l.off_old),  reinterpret_cast<const int*>(ws + l.off_need),
+          reinterpret_cast<const int*>(ws + l.off_back), reinterpret_cast<const int*>(ws + l.off_tok),
+          reinterpret_cast<const int*>(ws + l.off_pos),  f.base_need, f.base_back, f.base_tok, chunk, heads, a.batch,
+          (int)total[0], (int)total[1], (int)total[2]};
+}
+
+__global__ void __launch_bounds__(256) page_return_kernel(const PageTablesArgs a, const int chunk) {
+  static_assert(kMaxChunks == 256, "a thread for every chunk");
+  __shared__ FillPlan f;
+  int error, top, n_free;
+  const PlanSums w = add_up(a, chunk, f, error, top, n_free);
+  if (error != 0) return;
+  give_back(a, w, n_free, blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4);
+}
+
+// The first `head_wgs` workgroups take the heads (a wavefront each), the others the tokens.
+constexpr int kSlotItems = 16;
+constexpr long long kOnePlaces = 16384;
+__global__ void __launch_bounds__(256) page_fill_kernel(const PageTablesArgs a, const int chunk, const int head_wgs) {
+  __shared__ FillPlan f;
+  int error, top, n_free;
+  const PlanSums w = add_up(a, chunk, f, error, top, n_free);
+  if ((int)blockIdx.x >= head_wgs) {
+    const unsigned int e = (blockIdx.x - head_wgs) * (256u * kSlotItems) + threadIdx.x;
+    fill_slots(a, w, top, error != 0 ? 0 : w.total_tok, e, 256u, kSlotItems);
+    return;
+  }
+  const int heads = a.batch * a.heads;
+  if (error == 0) {
+    fill_heads<true>(a, w, top, blockIdx.x * 4 + (threadIdx.x >> 6), head_wgs * 4);
+  } else {
+    for (int hb = blockIdx.x * 256 + (int)threadIdx.x; hb < heads; hb += head_wgs * 256) a.st.head_rows_out[hb] = a.st.head_rows[hb];
+  }
+  for (int b = blockIdx.x * 256 + (int)threadIdx.x; b < a.batch; b += head_wgs * 256)
+    a.st.seq_pos_out[b] = error != 0 ? a.st.seq_pos[b] : w.pos[b] + (a.n_new != nullptr ? a.n_new[b] : 0);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    a.st.n_free_out[0] = error != 0 ? n_free : top - w.total_need;
+    if (error != 0 && a.st.error != nullptr) atomicOr(a.st.error, error);
   }
 }
 
@@ -247,27 +451,37 @@ __global__ void __launch_bounds__(256) page_fill_kernel(const PageTablesArgs a, 
 size_t page_tables_bytes(int32_t batch, int32_t n_kv_heads) { return plan_layout(batch, batch * n_kv_heads).bytes; }
 
 int32_t launch_page_tables(const PageTablesArgs& a, hipStream_t s) {
+  const long long heads = (long long)a.batch * a.heads, places = a.max_tokens * a.heads;
+  // Written by the one workgroup alone: every slot, a count per head and, where heads take or give back any number of pages, up
+  // to the whole table.
+  const long long pages = a.head_counts != nullptr || a.release != nullptr ? heads * a.max_blocks : 0;
+  const bool one = heads <= kOneHeads && places + pages <= kOnePlaces;
+  if (one) {
+    ProfScope ps(KID_PAGE_PLAN, s);
+    hipLaunchKernelGGL(page_step_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+    return launch_status();
+  }
+  const int chunk = heads <= (long long)kMaxChunks * kPlanThreads ? 10 : 12;   // 1024 or 4096 heads a chunk
+  const int head_chunks = (int)((heads - 1) >> chunk) + 1, seq_chunks = ((a.batch - 1) >> chunk) + 1;
   {
     ProfScope ps(KID_PAGE_PLAN, s);
-    hipLaunchKernelGGL(page_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+    const dim3 grid((unsigned)(head_chunks + seq_chunks)), block(kPlanThreads);
+    if (chunk == 10) hipLaunchKernelGGL(page_sums_kernel<1>, grid, block, 0, s, a, head_chunks);
+    else hipLaunchKernelGGL(page_sums_kernel<4>, grid, block, 0, s, a, head_chunks);
   }
   int32_t st = launch_status();
   if (st != LAVA_OK) return st;
-  const long long heads = (long long)a.batch * a.heads;
-  long long head_wgs = (heads + 3) / 4, wgs = 0;
-  if (head_wgs > 2048) head_wgs = 2048;
+  long long head_wgs = (heads + 15) / 16;                          // four heads a wavefront
+  if (head_wgs > 1024) head_wgs = 1024;
   if (a.release != nullptr) {
     ProfScope ps(KID_PAGE_FILL, s);
-    hipLaunchKernelGGL(page_return_kernel, dim3((unsigned)head_wgs), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(page_return_kernel, dim3((unsigned)head_wgs), dim3(256), 0, s, a, chunk);
     st = launch_status();
     if (st != LAVA_OK) return st;
   }
-  if (a.max_tokens > 0) {
-    wgs = (a.max_tokens * a.heads + 255) / 256;
-    if (wgs > 4096) wgs = 4096;
-  }
+  const long long slot_wgs = (places + 256 * kSlotItems - 1) / (256 * kSlotItems);
   ProfScope ps(KID_PAGE_FILL, s);
-  hipLaunchKernelGGL(page_fill_kernel, dim3((unsigned)(head_wgs + wgs)), dim3(256), 0, s, a, (int)head_wgs);
+  hipLaunchKernelGGL(page_fill_kernel, dim3((unsigned)(head_wgs + slot_wgs)), dim3(256), 0, s, a, chunk, (int)head_wgs);
   return launch_status();
 }
 

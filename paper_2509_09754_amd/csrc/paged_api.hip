@@ -82,7 +82,7 @@ int32_t lava_page_tables(const lava_page_pool* pool, int32_t batch, int32_t n_kv
   a.head_counts = head_counts;
   a.release = release;
   a.n_pages = pool->n_pages;
-  a.max_tokens = max_tokens;
+  a.max_tokens = slots != nullptr || positions != nullptr ? max_tokens : 0;
   a.slots = reinterpret_cast<long long*>(slots);
   a.positions = positions;
   a.batch = batch;

@@ -822,13 +822,21 @@ def lava_rotary_turns(rot: RotaryDesc, device=None) -> torch.Tensor:
     return out if device is None else out.to(device)
 
 
-def _rows_of_heads(t: torch.Tensor, name: str, dtype=None) -> torch.Tensor:
+def _rows_of_heads(t: torch.Tensor, name: str, dtype) -> torch.Tensor:
     """[tokens, heads, d_h] whose heads are contiguous rows (any strides between them)."""
-    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1:
-        raise ValueError(f"{name} must be a device tensor [tokens, heads, d_h] with contiguous heads")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} must have dtype {dtype}")
+    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1 or t.dtype != dtype:
+        raise ValueError(f"{name} must be a device tensor [tokens, heads, d_h] of {dtype} with contiguous heads")
     return t
+
+
+def _token_stride(t: torch.Tensor, name: str, dtype, shape) -> int:
+    """The stride of the tokens of t, of that shape, whose heads lie one after another."""
+    if t.shape != shape or not t.is_cuda or t.dtype != dtype:
+        raise ValueError(f"{name} must be a device tensor {list(shape)} of {dtype}")
+    stride = t.stride()
+    if stride[2] != 1 or (stride[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"{name} must have its heads one after another")
+    return stride[0]
 
 
 def _check_turns(rot: RotaryDesc, turns: torch.Tensor, positions: torch.Tensor, tokens: int) -> None:
@@ -861,27 +869,24 @@ def lava_rotary_append(desc: LayerDesc, rot: RotaryDesc, turns: torch.Tensor, po
                        q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
     """New tokens into the paged cache; q [tokens, H, d_h] (or None), k, v [tokens, H_kv, d_h], parts of one projection's
     output allowed.  Returns q_out, the rotated queries [tokens, H, d_h]."""
-    dt, d = desc.torch_dtype, desc.head_dim
+    dt, d, hq, hkv = desc.torch_dtype, desc.head_dim, desc.n_q_heads, desc.n_kv_heads
     tokens = k.shape[0]
-    for name, t, heads in (("q", q, desc.n_q_heads), ("k", k, desc.n_kv_heads), ("v", v, desc.n_kv_heads)):
-        if t is None:
-            continue
-        _rows_of_heads(t, name, dt)
-        if tuple(t.shape) != (tokens, heads, d) or (heads > 1 and t.stride(1) != d):
-            raise ValueError(f"{name} must be [tokens, {heads}, {d}], its heads one after another")
+    k_stride, v_stride = _token_stride(k, "k", dt, (tokens, hkv, d)), _token_stride(v, "v", dt, (tokens, hkv, d))
+    q_stride = 0
+    if q is not None:
+        q_stride = _token_stride(q, "q", dt, (tokens, hq, d))
+        if q_out is None:
+            q_out = torch.empty(tokens, hq, d, dtype=dt, device=q.device)
+        elif q_out.numel() != tokens * hq * d:
+            raise ValueError("q_out must be [tokens, H, d_h]")
+        elif q_out is not q:
+            _dev(q_out, "q_out", dt)
     _check_turns(rot, turns, positions, tokens)
     pool._check(desc)
-    if _dev(slots, "slots", torch.int64).numel() != tokens * desc.n_kv_heads:
+    if _dev(slots, "slots", torch.int64).numel() != tokens * hkv:
         raise ValueError("slots must be [tokens, H_kv]")
-    if q is not None:
-        if q_out is None:
-            q_out = torch.empty(tokens, desc.n_q_heads, d, dtype=dt, device=q.device)
-        if q_out.data_ptr() != q.data_ptr():
-            _dev(q_out, "q_out", dt)
-        if q_out.numel() != tokens * desc.n_q_heads * d:
-            raise ValueError("q_out must be [tokens, H, d_h]")
     st = lib.lava_rotary_append(ctypes.byref(desc), ctypes.byref(rot), _ptr(turns), tokens, _ptr(positions), _ptr(q),
-                                q.stride(0) if q is not None else 0, _ptr(k), k.stride(0), _ptr(v), v.stride(0),
+                                q_stride, _ptr(k), k_stride, _ptr(v), v_stride,
                                 _ptr(q_out) if q is not None else None, pool._ref, _ptr(slots), _stream(stream))
     _check(st, "lava_rotary_append")
     return q_out
