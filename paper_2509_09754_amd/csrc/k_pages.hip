@@ -138,14 +138,23 @@ __device__ __forceinline__ void give_back(const PageTablesArgs& a, const PlanSum
   }
 }
 
-// Tables and counts of the heads: a thread per head, or a wavefront where heads may take many pages at once.
-template <bool WAVE>
+// Tables and counts of the heads, LANES threads a head: one where heads take a page now and then, more where they may take many.
+template <int LANES>
 __device__ __forceinline__ void fill_heads(const PageTablesArgs& a, const PlanSums& w, int top, int first, int step) {
-  const int lane = WAVE ? threadIdx.x & 63 : 0, lanes = WAVE ? 64 : 1, heads = a.batch * a.heads, mask = (1 << a.page_shift) - 1;
+  constexpr int kBatch = LANES > 1 ? 4 : 1;                            // look-ups a thread has in flight
+  const int lane = (int)threadIdx.x % LANES, heads = a.batch * a.heads, mask = (1 << a.page_shift) - 1;
   for (int hb = first; hb < heads; hb += step) {
     const int old = w.old[hb], start = w.need_at(hb), need = w.need_at(hb + 1) - start;
     int* table = a.st.block_table + (long long)hb * a.max_blocks + ((old + mask) >> a.page_shift);
-    for (int j = lane; j < need; j += lanes) table[j] = a.st.free_pages[top - 1 - start - j];
+    const int* fresh = a.st.free_pages + (top - 1 - start);
+    for (int j0 = lane; j0 < need; j0 += LANES * kBatch) {
+      int page[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) page[i] = j0 + LANES * i < need ? fresh[-(j0 + LANES * i)] : 0;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (j0 + LANES * i < need) table[j0 + LANES * i] = page[i];
+    }
     if (lane == 0) {
       const int add = a.head_counts != nullptr ? a.head_counts[hb] : a.n_new != nullptr ? a.n_new[hb / a.heads] : 0;
       a.st.head_rows_out[hb] = old + add;
@@ -200,6 +209,48 @@ __device__ __forceinline__ void fill_slots(const PageTablesArgs& a, const PlanSu
                                    : a.st.free_pages[top - 1 - start - (block - owned)];
     a.slots[e] = ((long long)page << a.page_shift) + (r & mask);
   }
+}
+
+// The same for the 256 * ITEMS places from place e0 on, by a workgroup of 256 threads.  Where all of them are tokens of one sequence, as
+// most of a prompt's are, a thread stays with its head and its look-ups are independent of each other.
+template <int ITEMS>
+__device__ __forceinline__ void fill_slots_wide(const PageTablesArgs& a, const PlanSums& w, int top, int tokens, unsigned int e0) {
+  const unsigned int all = (unsigned int)(a.max_tokens * a.heads), heads = (unsigned int)a.heads;
+  if (256u % heads == 0u && a.slots != nullptr && e0 + 256u * ITEMS <= all) {
+    const int t_first = (int)(e0 / heads), t_last = (int)((e0 + 256u * ITEMS - 1u) / heads);
+    if (t_last < tokens) {
+      int lo = 0, hi = a.batch - 1;                                  // uniform: the last sequence that starts at or before t_first
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__builtin_amdgcn_readfirstlane(w.tok_at(mid)) <= t_first) lo = mid; else hi = mid - 1;
+      }
+      const int begin = w.tok_at(lo);
+      if (t_last < w.tok_at(lo + 1)) {
+        const unsigned int e = e0 + threadIdx.x, t = e / heads, g = e - t * heads;
+        const int mask = (1 << a.page_shift) - 1, hb = lo * a.heads + (int)g, step = (int)(256u / heads);
+        const int old = w.old[hb], owned = (old + mask) >> a.page_shift, i0 = (int)t - begin;
+        const int* table = a.st.block_table + (long long)hb * a.max_blocks;
+        const int* fresh = a.st.free_pages + (top - 1 - w.need_at(hb) + owned);   // the page of new block j is fresh[-j]
+        int page[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          const int block = (old + i0 + i * step) >> a.page_shift;
+          page[i] = *(block < owned ? table + block : fresh - block);
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          const int r = old + i0 + i * step;
+          a.slots[e + 256u * i] = ((long long)page[i] << a.page_shift) + (r & mask);
+        }
+        if (a.positions != nullptr && g == 0u) {
+          const int pos = w.pos[lo] + i0;
+          for (int i = 0; i < ITEMS; ++i) a.positions[t + (unsigned int)(i * step)] = pos + i * step;
+        }
+        return;
+      }
+    }
+  }
+  fill_slots(a, w, top, tokens, e0 + threadIdx.x, 256u, ITEMS);
 }
 
 // What sequence b does: its tokens (0 where it cannot be), its first position.
@@ -287,7 +338,7 @@ __global__ void __launch_bounds__(kPlanThreads) page_step_kernel(const PageTable
     fill_slots(a, w, top, error != 0 ? 0 : w.total_tok, threadIdx.x, kPlanThreads, (int)((places + kPlanThreads - 1) / kPlanThreads));
   }
   if (error == 0) {
-    fill_heads<false>(a, w, top, threadIdx.x, kPlanThreads);
+    fill_heads<1>(a, w, top, threadIdx.x, kPlanThreads);
   } else {
     for (int hb = threadIdx.x; hb < heads; hb += kPlanThreads) a.st.head_rows_out[hb] = a.st.head_rows[hb];
   }
@@ -358,10 +409,12 @@ __global__ void __launch_bounds__(kPlanThreads) page_sums_kernel(const PageTable
 }
 
 // What a workgroup of 256 threads of the second launch needs of the totals: sums of the chunks before, and the verdict.
+constexpr int kFewSequences = 1024;   // as many as one chunk holds: their tokens' sums are looked up in LDS
 struct FillPlan {
   int base_need[kMaxChunks], base_back[kMaxChunks], base_tok[kMaxChunks];
-  unsigned long long part[3][4], total[3];
+  unsigned long long part[3][4];
   int error;
+  int tok[kFewSequences];
 };
 __device__ __forceinline__ unsigned long long lane_sum64(unsigned long long x) {
   const int lane = threadIdx.x & 63;
@@ -372,12 +425,29 @@ __device__ __forceinline__ unsigned long long lane_sum64(unsigned long long x) {
   }
   return x;
 }
-__device__ __forceinline__ PlanSums add_up(const PageTablesArgs& a, int chunk, FillPlan& f, int& error, int& top, int& n_free) {
+__device__ __forceinline__ PlanSums add_up(const PageTablesArgs& a, int chunk, FillPlan& f, bool with_tokens, int& error, int& top, int& n_free) {
   const char* ws = static_cast<const char*>(a.ws);
   const int heads = a.batch * a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int head_chunks = ((heads - 1) >> chunk) + 1, seq_chunks = ((a.batch - 1) >> chunk) + 1;
   const PlanLayout l = plan_layout(a.batch, heads);
   const ChunkTotals* totals = reinterpret_cast<const ChunkTotals*>(ws);
+  const int* tok = reinterpret_cast<const int*>(ws + l.off_tok);
+  if (with_tokens && a.batch <= kFewSequences) {                       // uniform
+    for (int b = threadIdx.x; b < a.batch; b += 256) f.tok[b] = tok[b];
+    tok = f.tok;
+  }
+  if (head_chunks == 1 && seq_chunks == 1) {                           // nothing to add up
+    const ChunkTotals h = totals[0], s = totals[kMaxChunks];
+    if (threadIdx.x == 0) f.base_need[0] = f.base_back[0] = f.base_tok[0] = 0;
+    __syncthreads();
+    n_free = h.n_free;
+    error = verdict(a, h.error | s.error, n_free, h.need, h.back, s.need);
+    top = (int)(n_free + (long long)h.back);
+    return {reinterpret_cast<const int*>(ws + l.off_old),  reinterpret_cast<const int*>(ws + l.off_need),
+            reinterpret_cast<const int*>(ws + l.off_back), tok,
+            reinterpret_cast<const int*>(ws + l.off_pos),  f.base_need, f.base_back, f.base_tok, chunk, heads, a.batch,
+            (int)h.need, (int)h.back, (int)s.need};
+  }
   ChunkTotals h = {0ull, 0ull, 0, 0}, s = h;
   if ((int)threadIdx.x < head_chunks) h = totals[threadIdx.x];
   if ((int)threadIdx.x < seq_chunks) s = totals[kMaxChunks + threadIdx.x];
@@ -406,7 +476,7 @@ __device__ __forceinline__ PlanSums add_up(const PageTablesArgs& a, int chunk, F
   error = verdict(a, f.error, n_free, total[0], total[1], total[2]);
   top = (int)(n_free + (long long)total[1]);
   return {reinterpret_cast<const int*>(ws + l.off_old),  reinterpret_cast<const int*>(ws + l.off_need),
-          reinterpret_cast<const int*>(ws + l.off_back), reinterpret_cast<const int*>(ws + l.off_tok),
+          reinterpret_cast<const int*>(ws + l.off_back), tok,
           reinterpret_cast<const int*>(ws + l.off_pos),  f.base_need, f.base_back, f.base_tok, chunk, heads, a.batch,
           (int)total[0], (int)total[1], (int)total[2]};
 }
@@ -415,26 +485,26 @@ __global__ void __launch_bounds__(256) page_return_kernel(const PageTablesArgs a
   static_assert(kMaxChunks == 256, "a thread for every chunk");
   __shared__ FillPlan f;
   int error, top, n_free;
-  const PlanSums w = add_up(a, chunk, f, error, top, n_free);
+  const PlanSums w = add_up(a, chunk, f, false, error, top, n_free);
   if (error != 0) return;
   give_back(a, w, n_free, blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4);
 }
 
-// The first `head_wgs` workgroups take the heads (a wavefront each), the others the tokens.
-constexpr int kSlotItems = 16;
+// The first `head_wgs` workgroups take the heads (one each, or one for each wavefront), the others the tokens.
+constexpr int kSlotItems = 8;   // 16 prompts, 559 thousand tokens: 4 19.9 us, 8 18.7, 16 20.6
 constexpr long long kOnePlaces = 16384;
 __global__ void __launch_bounds__(256) page_fill_kernel(const PageTablesArgs a, const int chunk, const int head_wgs) {
   __shared__ FillPlan f;
   int error, top, n_free;
-  const PlanSums w = add_up(a, chunk, f, error, top, n_free);
+  const PlanSums w = add_up(a, chunk, f, (int)blockIdx.x >= head_wgs, error, top, n_free);
   if ((int)blockIdx.x >= head_wgs) {
-    const unsigned int e = (blockIdx.x - head_wgs) * (256u * kSlotItems) + threadIdx.x;
-    fill_slots(a, w, top, error != 0 ? 0 : w.total_tok, e, 256u, kSlotItems);
+    fill_slots_wide<kSlotItems>(a, w, top, error != 0 ? 0 : w.total_tok, (blockIdx.x - head_wgs) * (256u * kSlotItems));
     return;
   }
   const int heads = a.batch * a.heads;
   if (error == 0) {
-    fill_heads<true>(a, w, top, blockIdx.x * 4 + (threadIdx.x >> 6), head_wgs * 4);
+    if (heads <= head_wgs) fill_heads<256>(a, w, top, blockIdx.x, head_wgs);
+    else fill_heads<64>(a, w, top, blockIdx.x * 4 + (threadIdx.x >> 6), head_wgs * 4);
   } else {
     for (int hb = blockIdx.x * 256 + (int)threadIdx.x; hb < heads; hb += head_wgs * 256) a.st.head_rows_out[hb] = a.st.head_rows[hb];
   }
@@ -471,8 +541,8 @@ int32_t launch_page_tables(const PageTablesArgs& a, hipStream_t s) {
   }
   int32_t st = launch_status();
   if (st != LAVA_OK) return st;
-  long long head_wgs = (heads + 15) / 16;                          // four heads a wavefront
-  if (head_wgs > 1024) head_wgs = 1024;
+  // a workgroup a head; more than 1024 heads share as many, a wavefront a head
+  const long long head_wgs = heads < 1024 ? heads : 1024;
   if (a.release != nullptr) {
     ProfScope ps(KID_PAGE_FILL, s);
     hipLaunchKernelGGL(page_return_kernel, dim3((unsigned)head_wgs), dim3(256), 0, s, a, chunk);
