@@ -8,8 +8,10 @@
 //
 // Inside a share's part of one head the wavefronts take tiles in turn.  K goes through a wavefront's own LDS ring with
 // direct-to-LDS loads, two tiles ahead, V straight into registers, one tile ahead (a lane owns the same columns of every row):
-//   logits   K_tile x Q^T on the matrix cores (the G heads are G columns of the 32-wide operand; exact products, fp32 sums)
-//   softmax  online, in the exp2 domain, per head, kept in the column's lanes
+//   logits   Q x K_tile^T on the matrix cores (the G heads are the first rows of the 32-row operand, the tile's rows the columns: a
+//            lane then has one row's logits for four heads, and everything up to the probabilities is four values a lane;
+//            the other way round it was sixteen, three quarters of them of no head); exact products, fp32 sums
+//   softmax  online, in the exp2 domain; a head's maximum is agreed on across the lanes, its sum kept per lane until the end
 //   output   acc[head][columns of this lane] += p[row][head] * V[row][columns], p broadcast through LDS in fp32; V is never
 //            rounded
 // Pages: the numbers of a wavefront's next 64 tiles are held by its lanes, one each (two for pages of half a tile), and become
@@ -61,22 +63,23 @@ __device__ __forceinline__ unsigned int ceil_by(unsigned int x, unsigned int y, 
 constexpr unsigned int kHeadCost = 6u;
 
 // With a window the rows that count lie together, and a run of tiles would have all of them or none.  The tiles of a head then take
-// their places column by column of a matrix of kSpread rows (place x is tile (x % kSpread) * columns + x / kSpread, or none),
-// so that every share has its part of the window, and (kSpread is odd) every wavefront of it.
+// their places column by column of a matrix of kSpread rows, whose rows are taken kStep apart (place x is tile
+// (kStep x % kSpread) * columns + x / kSpread, or none), so that every share has its part of the window, and (kSpread is odd)
+// every wavefront of it.
+constexpr int kStep = 7;
 constexpr int kSpread = 17;
 __device__ __forceinline__ int spread_columns(int tiles, bool spread) { return spread && tiles >= 4 * kSpread ? (tiles + kSpread - 1) / kSpread : 0; }
 __device__ __forceinline__ int places_of(int tiles, bool spread) {
   const int columns = spread_columns(tiles, spread);
   return columns > 0 ? columns * kSpread : tiles;
 }
-// With a window a place of the line is not one tile but `per` of them: about as many as hold one that counts if the head's rows are spread
+// With a window a place of the line is not one tile but 2, 4 or 8 of them: about as many as hold one that counts if the head's rows are spread
 // over the sequence's positions (and no more than finding out costs).  An estimate: it moves cuts, not results.
-constexpr int kMostPer = 8;
-__device__ __forceinline__ int tiles_per_place(int q_pos, int window) {
-  const int n = window > 0 && q_pos >= 0 ? (int)(((unsigned int)q_pos + 1u) / (unsigned int)window) : 1;
-  return n < 1 ? 1 : n > kMostPer ? kMostPer : n;
+__device__ __forceinline__ int log_per_place(int q_pos, int window) {
+  const long long seen = (long long)q_pos + 1;
+  return seen >= 8ll * window ? 3 : seen >= 4ll * window ? 2 : seen >= 2ll * window ? 1 : 0;
 }
-__device__ __forceinline__ int tile_at(int place, int columns) { return columns > 0 ? (place % kSpread) * columns + place / kSpread : place; }
+__device__ __forceinline__ int tile_at(int place, int columns) { return columns > 0 ? (place % kSpread * kStep % kSpread) * columns + place / kSpread : place; }
 
 // Tiles of a head with that many rows; -1: it cannot have them.
 __device__ __forceinline__ int head_tiles(const PagedDecodeArgs& a, int rows) {
@@ -105,6 +108,23 @@ __device__ __forceinline__ void write_row(const PagedDecodeArgs& p, int b, int g
   p.out[row * D + e + 1] = none ? 0.0f : sum.y / L;
   if (p.lse != nullptr && e == 0) p.lse[row] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
+
+// The maximum, and the sum, over the 32 lanes of this lane's half of the wavefront, in each of them.
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float x) {
+  return __uint_as_float((unsigned int)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));
+}
+template <typename F>
+__device__ __forceinline__ float over_half(float x, F op) {
+  x = op(x, dpp_move<0xb1>(x));                                // lane ^ 1
+  x = op(x, dpp_move<0x4e>(x));                                // lane ^ 2
+  x = op(x, dpp_move<0x141>(x));                               // mirrored in eight: the other four
+  x = op(x, dpp_move<0x140>(x));                               // mirrored in sixteen: the other eight
+  const auto h = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return op(__uint_as_float(h[0]), __uint_as_float(h[1]));
+}
+__device__ __forceinline__ float max_of_half(float x) { return over_half(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float sum_of_half(float x) { return over_half(x, [](float a, float b) { return a + b; }); }
 
 // The parts of one head, in order, eight loads of each kind in flight.
 constexpr int kPartLoads = 8;
@@ -145,8 +165,12 @@ __device__ __forceinline__ void merge_parts(const PagedArgs& a, int b, int g, in
   }
 }
 
+// Wavefronts a SIMD is to hold: as many as the ring leaves room for.
+template <int DT, int D>
+constexpr int kWavesPerSimd = Tile<DT, D>::kRowBytes == 128 ? 3 : Tile<DT, D>::kRowBytes == 256 ? 2 : 1;
+
 template <int DT, int D, int GP, bool OPT>
-__global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) {
+__global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_decode_kernel(PagedArgs a) {
   using S = DecShape<DT, D>;
   using T = Tile<DT, D>;
   constexpr int kStages = S::kStages;
@@ -166,6 +190,7 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
 
   // ---------------- this workgroup's share: sums over all heads, 64 at a time
   const bool spread = OPT && p.window > 0;
+  const double inv_heads = 1.0 / (double)p.H_kv;              // h / H_kv: half a head off the border, so the product is exact enough
   constexpr int kHeld = 8;                                    // counts a lane holds at once: 512 heads in one trip to memory
   int held[kHeld];
   auto load_counts = [&](int h0) {
@@ -177,7 +202,10 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
 #pragma unroll
     for (int c = 0; c < kHeld; ++c) {
       held[c] = places_of(head_tiles(p, held[c]), spread);
-      if (spread && held[c] > 0) held[c] = (int)ceil_of((unsigned int)held[c], (unsigned int)tiles_per_place(p.q_pos[(h0 + 64 * c + lane) / p.H_kv], p.window));
+      if (spread && held[c] > 0) {
+        const int b = (int)(((double)(h0 + 64 * c + lane) + 0.5) * inv_heads), log_per = log_per_place(p.q_pos[b], p.window);
+        held[c] = (held[c] + (1 << log_per) - 1) >> log_per;
+      }
     }
   };
   unsigned int mine = 0u, full = 0u;
@@ -258,8 +286,8 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
   frags.init_at(lane, lds_addr(ring));
   const unsigned int p_addr = lds_addr(&s_p[wave][0][0]);
   const int col = lane & 31, half = lane >> 5;
-  const unsigned int p_col = p_addr + (unsigned int)(col * 4);                  // row 0 of s_p, this head's column
-  const unsigned int p_mine = p_col + (unsigned int)(4 * half * kPs * 4);       // first row this lane's results cover
+  const unsigned int p_mine = p_addr + (unsigned int)((col * kPs + (GP > 4 ? 4 * half : 0)) * 4);   // this row, this lane's four heads
+  const unsigned int p_alpha = p_addr + (unsigned int)((kTileKeys * kPs + (GP > 4 ? 4 * half : 0)) * 4);
   const unsigned int v_lane = (unsigned int)lane * S::kBpl;   // a row is a uniform address plus this
   const float inv_cap = p.cap > 0.0f ? 1.0f / p.cap : 0.0f;
   const unsigned int window = p.window > 0 ? (unsigned int)p.window : 0x80000000u;
@@ -278,9 +306,9 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
 
   // parts that wait to be published: of the first and the last head of the share
   int pend_head[2] = {-1, -1}, pend_w0[2] = {0, 0}, pend_parts[2] = {0, 0};
-  // of a head: its rows, the columns of its tiles' order, the tiles in that order, how many make a place, its places
+  // of a head: its rows, the columns of its tiles' order, the tiles in that order, log2 of how many make a place, its places
   int rows = p.head_rows[hb], columns = spread_columns(head_tiles(p, rows), spread), order = places_of(head_tiles(p, rows), spread);
-  int per = spread ? tiles_per_place(p.q_pos[hb / p.H_kv], p.window) : 1, tiles = OPT ? (order + per - 1) / per : order;
+  int log_per = spread ? log_per_place(p.q_pos[hb / p.H_kv], p.window) : 0, tiles = (order + (1 << log_per) - 1) >> log_per;
   int page_a, page_b;
   bool pages_ready = false;
   // In the line a head's tiles follow its weight: tile j is place head_start + weight + j.
@@ -301,12 +329,12 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
     const bool last = by_heads || at + (unsigned int)tiles + weight >= t1 || at + (unsigned int)tiles >= line_end;
     const int q_pos = OPT && p.pos != nullptr ? p.q_pos[b] : 0;
     // wavefronts take turns through the whole share, so that each has as many tiles as the others
-    const int pa = OPT ? ta * per : ta, pb = OPT ? (tb == tiles ? order : tb * per) : tb;   // in the order of the head's tiles
+    const int pa = ta << log_per, pb = tb == tiles ? order : tb << log_per;   // in the order of the head's tiles
     const int first = pa + (int)(((unsigned int)wave - done) & (kDecWaves - 1));
     const int cnt = first < pb ? (pb - first + kDecWaves - 1) / kDecWaves : 0;   // this wavefront's tiles
     if (!pages_ready) load_pages(hb, rows, columns, first, cnt < kBlock ? cnt : kBlock, page_a, page_b);
 
-    // the group's query rows as the 32-column operand: column t < G is head g * G + t
+    // the group's query rows as the 32-row operand: row t < G is head g * G + t
     u32x4 qf[T::kSteps];
 #pragma unroll
     for (int j = 0; j < T::kSteps; ++j) {
@@ -314,16 +342,21 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
       if (col < p.G) x = reinterpret_cast<const u32x4*>(p.q)[((long long)b * p.H + (long long)g * p.G + col) * T::kCpr + 2 * j + half];
       qf[j] = x;
     }
-    float slope = 0.0f;
-    if (OPT && p.slopes != nullptr && col < p.G) slope = p.slopes[g * p.G + col] * kLog2e;
-    float m_run = -INFINITY, l_run = 0.0f;                    // of head `col` (lanes col < G)
+    // of heads 4 * half + v of the group; the sums are those of this lane's rows
+    float slope[4], m_run[4], l_run[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      slope[v] = OPT && p.slopes != nullptr && 4 * half + v < p.G ? p.slopes[g * p.G + 4 * half + v] * kLog2e : 0.0f;
+      m_run[v] = -INFINITY;
+      l_run[v] = 0.0f;
+    }
     float acc[GP][kDpl];
 #pragma unroll
     for (int i = 0; i < GP; ++i)
 #pragma unroll
       for (int e = 0; e < kDpl; ++e) acc[i][e] = 0.0f;
 
-    int next_head = hb, next_rows = 0, next_columns = 0, next_order = 0, next_per = 1, next_tiles = 0, next_a = 0, next_b = 0;
+    int next_head = hb, next_rows = 0, next_columns = 0, next_order = 0, next_log_per = 0, next_tiles = 0, next_a = 0, next_b = 0;
     for (int i0 = 0; i0 == 0 || i0 < cnt; i0 += kBlock) {
       const int tile0 = first + kDecWaves * i0;
       const int here = cnt - i0 < kBlock ? cnt - i0 : kBlock;
@@ -332,7 +365,8 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
       {
         const bool bad = page_a < 0 || page_a >= p.n_pages || page_b < 0 || page_b >= p.n_pages;
         if (__ballot(bad) != 0ull) {                          // the head's result is NaN: any page will do
-          l_run = NAN;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) l_run[v] = NAN;
           if (bad) page_a = page_b = 0;
         }
         if (OPT) {
@@ -411,11 +445,11 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
         next_columns = spread_columns(next_tiles, spread);
         next_tiles = next_order = places_of(next_tiles, spread);
         if (spread) {
-          next_per = tiles_per_place(p.q_pos[next_head / p.H_kv], p.window);
-          next_tiles = (next_order + next_per - 1) / next_per;
+          next_log_per = log_per_place(p.q_pos[next_head / p.H_kv], p.window);
+          next_tiles = (next_order + (1 << next_log_per) - 1) >> next_log_per;
         }
         const unsigned int n_at = at + (unsigned int)tiles + weight;
-        const int n_tb = t1 - n_at < (unsigned int)next_tiles ? (int)(t1 - n_at) * next_per : next_order;
+        const int n_tb = t1 - n_at < (unsigned int)next_tiles ? (int)(t1 - n_at) << next_log_per : next_order;
         const int n_first = (int)(((unsigned int)wave - done - (unsigned int)(pb - pa)) & (kDecWaves - 1));
         const int n_cnt = n_first < n_tb ? (n_tb - n_first + kDecWaves - 1) / kDecWaves : 0;
         load_pages(next_head, next_rows, next_columns, n_first, n_cnt < kBlock ? n_cnt : kBlock, next_a, next_b);
@@ -432,52 +466,48 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
           frags.template read_at<PAR * T::kTileBytes>(kf);     // in registers on return: the stage is free
           if (j2 >= 0) issue_k(j2, PAR);
           asm volatile("" ::: "memory");
-          f32x16 x = {0}, x2 = {0};                            // two chains halve the latency of dependent products
+          f32x16 sum = {0}, sum2 = {0};                        // two chains halve the latency of dependent products
 #pragma unroll
           for (int j = 0; j < T::kSteps; j += 2) {
-            x = mfma_chunk<DT>(kf[j], qf[j], x);
-            x2 = mfma_chunk<DT>(kf[j + 1], qf[j + 1], x2);
+            sum = mfma_chunk<DT>(qf[j], kf[j], sum);
+            sum2 = mfma_chunk<DT>(qf[j + 1], kf[j + 1], sum2);
           }
-          x += x2;                                             // x[v]: row 8*(v/4) + 4*half + v%4, head col
+          float x[4];                                          // row `col` of the tile, heads 4 * half + v
+#pragma unroll
+          for (int v = 0; v < 4; ++v) x[v] = sum[v] + sum2[v];
           if (OPT && p.cap > 0.0f) {                           // uniform
 #pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] = capped(x[v] * p.scale, p.cap, inv_cap) * kLog2e;
+            for (int v = 0; v < 4; ++v) x[v] = capped(x[v] * p.scale, p.cap, inv_cap) * kLog2e;
           } else {
 #pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] *= a.c2;
+            for (int v = 0; v < 4; ++v) x[v] *= a.c2;
           }
           if (OPT) {
             if (p.slopes != nullptr) {                         // uniform
-              u32x4 y[4];
-              lds_read128x4_strided<32>(lds_addr(&s_back[wave][0]) + (unsigned int)(((j0 >> 2) * kTileKeys + 4 * half) * 4), y[0], y[1], y[2], y[3]);
+              const float back = lds_read32(lds_addr(&s_back[wave][0]) + (unsigned int)(((j0 >> 2) * kTileKeys + col) * 4));
 #pragma unroll
-              for (int v = 0; v < 16; ++v) x[v] -= slope * __uint_as_float(y[v / 4][v % 4]);
+              for (int v = 0; v < 4; ++v) x[v] -= slope[v] * back;
             }
           }
           if (mask != ~0u) {                                   // uniform; whatever the other rows hold
-            const unsigned int my = mask >> (4 * half);
+            const bool on = (mask >> col) & 1u;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] = my & (1u << (8 * (v / 4) + v % 4)) ? x[v] : -INFINITY;
+            for (int v = 0; v < 4; ++v) x[v] = on ? x[v] : -INFINITY;
           }
-          float mt = x[0];
+          float e[4], alpha[4];
 #pragma unroll
-          for (int v = 1; v < 16; ++v) mt = fmaxf(mt, x[v]);
-          mt = fmaxf(mt, __shfl_xor(mt, 32));
-          const float m_new = fmaxf(m_run, mt);
-          const float base = m_new == -INFINITY ? 0.0f : m_new;   // logits that are all -inf
-          const float alpha = fast_exp2(m_run - base);
-          float ls = 0.0f;
-          if (col < GP) {
-            static_for<16>([&](auto vc) {
-              constexpr int v = decltype(vc)::value;
-              const float e = fast_exp2(x[v] - base);
-              ls += e;
-              lds_write32_at<(8 * (v / 4) + (v % 4)) * kPs * 4>(p_mine, e);
-            });
-            if (half == 0) lds_write32_at<kTileKeys * kPs * 4>(p_col, alpha);
+          for (int v = 0; v < 4; ++v) {
+            const float m_new = fmaxf(m_run[v], max_of_half(x[v]));
+            const float base = m_new == -INFINITY ? 0.0f : m_new;   // logits that are all -inf
+            alpha[v] = fast_exp2(m_run[v] - base);
+            e[v] = fast_exp2(x[v] - base);
+            l_run[v] = l_run[v] * alpha[v] + e[v];
+            m_run[v] = m_new;
           }
-          l_run = l_run * alpha + ls;
-          m_run = m_new;
+          if (GP > 4 || half == 0) {
+            lds_write128(p_mine, e);
+            if (col == 0) lds_write128(p_alpha, alpha);
+          }
         }
         lds_reads_done();                                      // LDS operations of a wavefront execute in order
         {
@@ -536,10 +566,13 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
     }
 
     // ---------------- merge the wavefronts
-    l_run += __shfl_xor(l_run, 32);
-    if (lane < GP) {
-      s_m[wave][lane] = m_run;
-      s_l[wave][lane] = l_run;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      l_run[v] = sum_of_half(l_run[v]);
+      if (col == 0 && 4 * half + v < GP) {
+        s_m[wave][4 * half + v] = m_run[v];
+        s_l[wave][4 * half + v] = l_run[v];
+      }
     }
     __syncthreads();                                          // every wavefront is done with its ring
     float (*s_acc)[GP][D] = reinterpret_cast<float (*)[GP][D]>(&s_tile[0][0][0]);
@@ -590,7 +623,7 @@ __global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(PagedArgs a) 
     tiles = next_tiles;
     columns = next_columns;
     order = next_order;
-    per = next_per;
+    log_per = next_log_per;
     page_a = next_a;
     page_b = next_b;
     pages_ready = true;

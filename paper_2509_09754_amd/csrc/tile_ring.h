@@ -307,6 +307,18 @@ __device__ __forceinline__ void lds_write32(unsigned int a, float x) {
   asm volatile("ds_write_b32 %0, %1" : : "v"(a), "v"(x) : "memory");
 }
 
+__device__ __forceinline__ float lds_read32(unsigned int a) {
+  float x;
+  asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x) : "v"(a) : "memory");
+  return x;
+}
+
+// four values at a 16-byte aligned address
+__device__ __forceinline__ void lds_write128(unsigned int a, const float (&x)[4]) {
+  const u32x4 y = {__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+  asm volatile("ds_write_b128 %0, %1" : : "v"(a), "v"(y) : "memory");
+}
+
 // *a = max(*a, x) for values that are not negative, which order as integers
 __device__ __forceinline__ void lds_max32(unsigned int a, float x) {
   asm volatile("ds_max_u32 %0, %1" : : "v"(a), "v"(x) : "memory");
