@@ -62,6 +62,9 @@ __device__ __forceinline__ unsigned int ceil_by(unsigned int x, unsigned int y, 
 // What a workgroup that changes heads loses, in tiles.
 constexpr unsigned int kHeadCost = 6u;
 
+// Tiles of a head that a wavefront handles alone where there are heads enough.
+constexpr int kShortHead = 16;
+
 // With a window the rows that count lie together, and a run of tiles would have all of them or none.  The tiles of a head then take
 // their places column by column of a matrix of kSpread rows, whose rows are taken kStep apart (place x is tile
 // (kStep x % kSpread) * columns + x / kSpread, or none), so that every share has its part of the window, and (kSpread is odd)
@@ -124,45 +127,65 @@ __device__ __forceinline__ float over_half(float x, F op) {
   return op(__uint_as_float(h[0]), __uint_as_float(h[1]));
 }
 __device__ __forceinline__ float max_of_half(float x) { return over_half(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float max_of_wave(float x) {
+  x = max_of_half(x);
+  const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(lane_value(__float_as_uint(fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]))), 0));
+}
 __device__ __forceinline__ float sum_of_half(float x) { return over_half(x, [](float a, float b) { return a + b; }); }
 
-// The parts of one head, in order, eight loads of each kind in flight.
-constexpr int kPartLoads = 8;
+// The parts of one head, in order; a thread has one pair of columns, or two, and 16 loads of each kind in flight.
 template <int D, int GP>
 __device__ __forceinline__ void merge_parts(const PagedArgs& a, int b, int g, int w0, int parts) {
-  constexpr int kPairs = GP * D / 2;
-  for (int i = threadIdx.x; i < kPairs; i += kDecThreads) {
-    const int t = 2 * i / D, e = 2 * i % D;
-    float M = -INFINITY, L = 0.0f;
-    float2 sum = make_float2(0.0f, 0.0f);
-    for (int c0 = 0; c0 < parts; c0 += kPartLoads) {
-      const int nu = parts - c0 < kPartLoads ? parts - c0 : kPartLoads;
-      float2 ml[kPartLoads], pv[kPartLoads];
+  constexpr int kPairs = GP * D / 2, kOut = (kPairs + kDecThreads - 1) / kDecThreads, kLoads = 16;
+  static_assert(kPairs % kDecThreads == 0 || kPairs < kDecThreads, "threads share the pairs evenly");
+  const int i = threadIdx.x;
+  if (i >= kPairs) return;
+  const int t = 2 * i / D, e = 2 * i % D;                      // pair o: row t + o * kRows
+  constexpr int kRows = 2 * kDecThreads / D;
+  float M[kOut], L[kOut];
+  float2 sum[kOut];
 #pragma unroll
-      for (int u = 0; u < kPartLoads; ++u) {
-        const int slot = part_slot(w0, c0 + (u < nu ? u : 0));
-        ml[u] = ld_dev_f2(&a.part_ml[slot * GP + t]);
-        pv[u] = ld_dev_f2(reinterpret_cast<const float2*>(a.part_acc + (long long)slot * (GP * D) + 2 * i));
-      }
-      float m_new = M;
+  for (int o = 0; o < kOut; ++o) { M[o] = -INFINITY; L[o] = 0.0f; sum[o] = make_float2(0.0f, 0.0f); }
+  for (int c0 = 0; c0 < parts; c0 += kLoads) {
+    float2 ml[kOut][kLoads], pv[kOut][kLoads];
 #pragma unroll
-      for (int u = 0; u < kPartLoads; ++u) m_new = fmaxf(m_new, ml[u].x);   // those beyond nu repeat the first
-      const float base = m_new == -INFINITY ? 0.0f : m_new;    // -inf: nothing seen so far
-      const float keep = fast_exp2(M - base);
-      M = m_new;
-      L *= keep;
-      sum.x *= keep;
-      sum.y *= keep;
+    for (int u = 0; u < kLoads; ++u) {
+      const bool there = c0 + u < parts;                       // uniform
+      const int slot = part_slot(w0, c0 + u);
 #pragma unroll
-      for (int u = 0; u < kPartLoads; ++u) {
-        const float wgt = u < nu ? fast_exp2(ml[u].x - base) : 0.0f;
-        L += u < nu ? wgt * ml[u].y : 0.0f;
-        sum.x += u < nu ? wgt * pv[u].x : 0.0f;
-        sum.y += u < nu ? wgt * pv[u].y : 0.0f;
+      for (int o = 0; o < kOut; ++o) {
+        ml[o][u] = make_float2(-INFINITY, 0.0f);
+        pv[o][u] = make_float2(0.0f, 0.0f);
+        if (!there) continue;
+        ml[o][u] = ld_dev_f2(&a.part_ml[slot * GP + t + o * kRows]);
+        pv[o][u] = ld_dev_f2(reinterpret_cast<const float2*>(a.part_acc + (long long)slot * (GP * D) + 2 * (i + o * kDecThreads)));
       }
     }
-    if (t < a.p.G) write_row<D>(a.p, b, g, t, e, M, L, sum);
+#pragma unroll
+    for (int o = 0; o < kOut; ++o) {
+      float m_new = M[o];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) m_new = fmaxf(m_new, ml[o][u].x);
+      const float base = m_new == -INFINITY ? 0.0f : m_new;    // -inf: nothing seen so far
+      const float keep = fast_exp2(M[o] - base);
+      M[o] = m_new;
+      L[o] *= keep;
+      sum[o].x *= keep;
+      sum[o].y *= keep;
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        if (c0 + u >= parts) continue;                         // uniform
+        const float wgt = fast_exp2(ml[o][u].x - base);
+        L[o] += wgt * ml[o][u].y;
+        sum[o].x += wgt * pv[o][u].x;
+        sum[o].y += wgt * pv[o][u].y;
+      }
+    }
   }
+#pragma unroll
+  for (int o = 0; o < kOut; ++o)
+    if (t + o * kRows < a.p.G) write_row<D>(a.p, b, g, t + o * kRows, e, M[o], L[o], sum[o]);
 }
 
 // Wavefronts a SIMD is to hold: as many as the ring leaves room for.
@@ -181,7 +204,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
   __shared__ float s_m[kDecWaves][GP], s_l[kDecWaves][GP];
   constexpr int kBlock = OPT ? 16 : 64;                     // tiles whose pages a wavefront holds
   __shared__ __attribute__((aligned(16))) float s_back[OPT ? kDecWaves : 1][OPT ? 16 * kTileKeys : 4];   // distances to the rows
-  __shared__ int s_flag[2];
+  __shared__ int s_flag[2], s_pend[2][3];                    // parts that wait to be published: head, first workgroup, number of parts
 
   const PagedDecodeArgs& p = a.p;
   const int lane = threadIdx.x & 63, wave = wave_index();
@@ -208,7 +231,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
       }
     }
   };
-  unsigned int mine = 0u, full = 0u;
+  unsigned int mine = 0u, full = 0u, most = 0u;
   bool empty = false;
   for (int h0 = 0; h0 < n_heads; h0 += 64 * kHeld) {
     load_counts(h0);
@@ -216,6 +239,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
     for (int c = 0; c < kHeld; ++c) {
       mine += held[c] > 0 ? (unsigned int)held[c] : 0u;
       full += held[c] > 0 ? 1u : 0u;
+      most = held[c] > (int)most ? (unsigned int)held[c] : most;
       empty |= h0 + 64 * c + lane < n_heads && held[c] <= 0;
     }
   }
@@ -232,13 +256,21 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
     }
   }
   if (total == 0u) return;
-  // Two ways to cut.  By heads: units of at most `share` tiles of one head, a workgroup each, if there are enough workgroups for
+  // Short heads, and more of them than wavefronts: a wavefront has heads of its own, and nothing is shared or merged.
+  const float longest = max_of_wave((float)most);
+  const bool by_waves = longest <= (float)kShortHead && n_full >= kDecWaves * gridDim.x;
+  // Two other ways to cut.  By heads: units of at most `share` tiles of one head, a workgroup each, if there are enough workgroups for
   // all units.  Else through the line, where a head weighs kHeadCost tiles more than it has: what it costs to change heads.
-  const unsigned int wgs = gridDim.x, even = ceil_of(total, wgs), line = ceil_of(total + kHeadCost * n_full, wgs);
+  // Parts of a long head are merged one after another, a tenth of a microsecond each, where a tile more in a share is half of
+  // one: no fewer tiles in a share than the root of a quarter of the longest head's.
+  const unsigned int wgs = gridDim.x, least = (unsigned int)sqrtf(0.25f * longest);
+  unsigned int even = ceil_of(total, wgs), line = ceil_of(total + kHeadCost * n_full, wgs);
+  if (even < least) even = least;
+  if (line < least) line = least;
   unsigned int share = 0u;
   bool by_heads = false;
 #pragma unroll 1
-  for (int attempt = 0; attempt < 2 && !by_heads; ++attempt) {   // with shares as even as can be, then with those of the line
+  for (int attempt = 0; attempt < 2 && !by_heads && !by_waves; ++attempt) {   // with shares as even as can be, then with those of the line
     share = ((attempt == 0 ? even : line) + 3u) & ~3u;        // a tile for every wavefront
     const double inv = 1.0 / (double)share;
     unsigned int units = 0u;
@@ -258,7 +290,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
   {
     const double inv = 1.0 / (double)share;
     unsigned int at = 0u;
-    for (int h0 = 0; h0 < n_heads && hb < 0; h0 += 64 * kHeld) {
+    for (int h0 = 0; h0 < n_heads && hb < 0 && !by_waves; h0 += 64 * kHeld) {
       if (n_heads > 64 * kHeld) load_counts(h0);
 #pragma unroll
       for (int c = 0; c < kHeld; ++c) {
@@ -276,7 +308,15 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
       }
     }
   }
-  if (hb < 0) return;                                         // more workgroups than units
+  // The next head with rows from h on, `step` apart; n_heads: none.
+  auto next_with_rows = [&](int h, int step) -> int {
+    while (h < n_heads && head_tiles(p, p.head_rows[h]) <= 0) h += step;
+    return h < n_heads ? h : n_heads;
+  };
+  const int head_step = by_waves ? kDecWaves * (int)gridDim.x : 1, stride = by_waves ? 0 : 2;   // stride: log2 of this wavefront's, in tiles
+  static_assert(kDecWaves == 4, "log2");
+  if (by_waves) hb = next_with_rows(kDecWaves * (int)blockIdx.x + wave, head_step);
+  if (hb < 0 || hb >= n_heads) return;                        // more workgroups than units, or wavefronts than heads
 
   using VRaw = typename RawBits<S::kBpl>::type;
   TileDma<DT, D> dma;
@@ -292,10 +332,10 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
   const float inv_cap = p.cap > 0.0f ? 1.0f / p.cap : 0.0f;
   const unsigned int window = p.window > 0 ? (unsigned int)p.window : 0x80000000u;
 
-  // Pages of tile0, tile0 + kDecWaves, ... of head h, kBlock of them, as far as there are `here`: a lane each, or four (OPT)
+  // Pages of tile0, tile0 + 2^stride, ... of head h, kBlock of them, as far as there are `here`: a lane each, or four (OPT)
   auto load_pages = [&](int h, int rows_h, int columns, int tile0, int here, int& page_a, int& page_b) {
     const int i = OPT ? lane >> 2 : lane;
-    const int row0 = tile_at(tile0 + kDecWaves * i, columns) * kTileKeys;
+    const int row0 = tile_at(tile0 + (i << stride), columns) * kTileKeys;
     const int* table = p.block_table + (long long)h * p.max_blocks;
     page_a = page_b = 0;
     if (i < here && (!OPT || row0 < rows_h)) {
@@ -304,11 +344,20 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
     }
   };
 
-  // parts that wait to be published: of the first and the last head of the share
-  int pend_head[2] = {-1, -1}, pend_w0[2] = {0, 0}, pend_parts[2] = {0, 0};
-  // of a head: its rows, the columns of its tiles' order, the tiles in that order, log2 of how many make a place, its places
-  int rows = p.head_rows[hb], columns = spread_columns(head_tiles(p, rows), spread), order = places_of(head_tiles(p, rows), spread);
-  int log_per = spread ? log_per_place(p.q_pos[hb / p.H_kv], p.window) : 0, tiles = (order + (1 << log_per) - 1) >> log_per;
+  if (threadIdx.x < 2) s_pend[threadIdx.x][2] = 0;             // of the first and of the last head of the share
+  struct HeadOrder {
+    int rows, columns, order, log_per, tiles;                 // columns of its tiles' order, tiles in that order, log2 of how many make a place, places
+  };
+  auto head_order = [&](int h) -> HeadOrder {
+    HeadOrder o;
+    o.rows = p.head_rows[h];
+    const int n = head_tiles(p, o.rows);
+    o.columns = spread_columns(n, spread);
+    o.order = places_of(n, spread);
+    o.log_per = spread ? log_per_place(p.q_pos[h / p.H_kv], p.window) : 0;
+    o.tiles = (o.order + (1 << o.log_per) - 1) >> o.log_per;
+    return o;
+  };
   int page_a, page_b;
   bool pages_ready = false;
   // In the line a head's tiles follow its weight: tile j is place head_start + weight + j.
@@ -316,9 +365,14 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
   unsigned int done = 0u;                                     // tiles of the share so far
   for (;;) {
     const int b = hb / p.H_kv, g = hb - b * p.H_kv;
+    const HeadOrder of = head_order(hb);
+    const int rows = of.rows, columns = of.columns, order = of.order, log_per = of.log_per, tiles = of.tiles;
     const unsigned int at = head_start + weight;              // place of the head's first tile
     int ta, tb;                                               // its places that are this share's
-    if (by_heads) {
+    if (by_waves) {
+      ta = 0;
+      tb = tiles;
+    } else if (by_heads) {
       ta = (int)((t0 - head_start) * share);
       tb = tiles - ta < (int)share ? tiles : ta + (int)share;
     } else {
@@ -326,12 +380,12 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
       tb = t1 <= at ? 0 : t1 - at < (unsigned int)tiles ? (int)(t1 - at) : tiles;
     }
     if (ta >= tb) return;                                     // the share ends inside the first head's weight
-    const bool last = by_heads || at + (unsigned int)tiles + weight >= t1 || at + (unsigned int)tiles >= line_end;
+    bool last = by_heads || (!by_waves && (at + (unsigned int)tiles + weight >= t1 || at + (unsigned int)tiles >= line_end));
     const int q_pos = OPT && p.pos != nullptr ? p.q_pos[b] : 0;
     // wavefronts take turns through the whole share, so that each has as many tiles as the others
     const int pa = ta << log_per, pb = tb == tiles ? order : tb << log_per;   // in the order of the head's tiles
-    const int first = pa + (int)(((unsigned int)wave - done) & (kDecWaves - 1));
-    const int cnt = first < pb ? (pb - first + kDecWaves - 1) / kDecWaves : 0;   // this wavefront's tiles
+    const int first = by_waves ? 0 : pa + (int)(((unsigned int)wave - done) & (kDecWaves - 1));
+    const int cnt = first < pb ? (pb - first + (1 << stride) - 1) >> stride : 0;   // this wavefront's tiles
     if (!pages_ready) load_pages(hb, rows, columns, first, cnt < kBlock ? cnt : kBlock, page_a, page_b);
 
     // the group's query rows as the 32-row operand: row t < G is head g * G + t
@@ -356,9 +410,9 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
 #pragma unroll
       for (int e = 0; e < kDpl; ++e) acc[i][e] = 0.0f;
 
-    int next_head = hb, next_rows = 0, next_columns = 0, next_order = 0, next_log_per = 0, next_tiles = 0, next_a = 0, next_b = 0;
+    int next_head = hb, next_a = 0, next_b = 0;
     for (int i0 = 0; i0 == 0 || i0 < cnt; i0 += kBlock) {
-      const int tile0 = first + kDecWaves * i0;
+      const int tile0 = first + (i0 << stride);
       const int here = cnt - i0 < kBlock ? cnt - i0 : kBlock;
       if (i0 > 0) load_pages(hb, rows, columns, tile0, here, page_a, page_b);
       unsigned int seen = 0xffffffffu;                        // rows of the lane's tile that count (OPT)
@@ -371,7 +425,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
         }
         if (OPT) {
           const int i = lane >> 2, part = lane & 3;           // rows 8 part .. 8 part + 7 of tile i
-          const int row0 = tile_at(tile0 + kDecWaves * i, columns) * kTileKeys;
+          const int row0 = tile_at(tile0 + (i << stride), columns) * kTileKeys;
           seen = 0u;
           if (i < here && row0 < rows) {
             int4 x = make_int4(q_pos, q_pos, q_pos, q_pos), x2 = x;
@@ -399,7 +453,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
         }
       }
       unsigned long long todo = OPT ? __ballot(seen != 0u) & 0x1111111111111111ull : here == 64 ? ~0ull : (1ull << here) - 1ull;
-      auto row_of = [&](int j) -> int { return tile_at(tile0 + kDecWaves * (OPT ? j >> 2 : j), OPT ? columns : 0) * kTileKeys; };   // first row of lane j's tile
+      auto row_of = [&](int j) -> int { return tile_at(tile0 + ((OPT ? j >> 2 : j) << stride), OPT ? columns : 0) * kTileKeys; };   // first row of lane j's tile
       // place in the pool of the first rows of the tile's two halves
       auto half_a = [&](int j) -> long long {
         return ((long long)(int)lane_value((unsigned int)page_a, j) << shift) + (row_of(j) & page_mask);
@@ -437,22 +491,16 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
       VRaw v0[kTileKeys], v1[kTileKeys];
       if (j0 >= 0) load_v(v0, j0);
       if (i0 == 0 && !last) {                                  // the next head of the share, while this one streams
-        do {
-          ++next_head;
-          next_rows = p.head_rows[next_head];
-          next_tiles = head_tiles(p, next_rows);
-        } while (next_tiles <= 0);                             // ends: the share goes on
-        next_columns = spread_columns(next_tiles, spread);
-        next_tiles = next_order = places_of(next_tiles, spread);
-        if (spread) {
-          next_log_per = log_per_place(p.q_pos[next_head / p.H_kv], p.window);
-          next_tiles = (next_order + (1 << next_log_per) - 1) >> next_log_per;
-        }
+        next_head = next_with_rows(hb + head_step, head_step);
+        last = next_head >= n_heads;                           // by wavefronts; in the line there is one
+      }
+      if (i0 == 0 && !last) {
+        const HeadOrder next = head_order(next_head);
         const unsigned int n_at = at + (unsigned int)tiles + weight;
-        const int n_tb = t1 - n_at < (unsigned int)next_tiles ? (int)(t1 - n_at) << next_log_per : next_order;
-        const int n_first = (int)(((unsigned int)wave - done - (unsigned int)(pb - pa)) & (kDecWaves - 1));
-        const int n_cnt = n_first < n_tb ? (n_tb - n_first + kDecWaves - 1) / kDecWaves : 0;
-        load_pages(next_head, next_rows, next_columns, n_first, n_cnt < kBlock ? n_cnt : kBlock, next_a, next_b);
+        const int n_tb = !by_waves && t1 - n_at < (unsigned int)next.tiles ? (int)(t1 - n_at) << next.log_per : next.order;
+        const int n_first = by_waves ? 0 : (int)(((unsigned int)wave - done - (unsigned int)(pb - pa)) & (kDecWaves - 1));
+        const int n_cnt = n_first < n_tb ? (n_tb - n_first + (1 << stride) - 1) >> stride : 0;
+        load_pages(next_head, next.rows, next.columns, n_first, n_cnt < kBlock ? n_cnt : kBlock, next_a, next_b);
       }
 
       auto step = [&](auto par, VRaw (&v_cur)[kTileKeys], VRaw (&v_next)[kTileKeys]) {
@@ -565,6 +613,27 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
       wait_vmcnt<0>();
     }
 
+    if (by_waves) {
+      // ---------------- the head is this wavefront's alone
+#pragma unroll
+      for (int v = 0; v < 4; ++v) l_run[v] = sum_of_half(l_run[v]);
+#pragma unroll
+      for (int i = 0; i < GP; ++i) {
+        if (i >= p.G) continue;                               // uniform
+        const float M = __uint_as_float(lane_value(__float_as_uint(m_run[i & 3]), i < 4 ? 0 : 32));
+        const float L = __uint_as_float(lane_value(__float_as_uint(l_run[i & 3]), i < 4 ? 0 : 32));
+        const long long row = (long long)b * p.H + (long long)g * p.G + i;
+#pragma unroll
+        for (int e = 0; e < kDpl; ++e) p.out[row * D + lane * kDpl + e] = L == 0.0f ? 0.0f : acc[i][e] / L;
+        if (p.lse != nullptr && lane == 0) p.lse[row] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+      }
+      if (last) return;
+      hb = next_head;
+      page_a = next_a;
+      page_b = next_b;
+      pages_ready = true;
+      continue;
+    }
     // ---------------- merge the wavefronts
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
@@ -611,48 +680,49 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
     if (!whole) {
       const int w0 = (int)(by_heads ? head_start : at / share);
       const int parts = by_heads ? (int)ceil_of((unsigned int)tiles, share) : (int)((at + (unsigned int)tiles - 1u) / share) - w0 + 1;
-      if (ta > 0) { pend_head[0] = hb; pend_w0[0] = w0; pend_parts[0] = parts; }
-      else { pend_head[1] = hb; pend_w0[1] = w0; pend_parts[1] = parts; }
+      if (threadIdx.x == 0) {
+        int* pend = s_pend[ta > 0 ? 0 : 1];
+        pend[0] = hb;
+        pend[1] = w0;
+        pend[2] = parts;
+      }
     }
     if (last) break;
     __syncthreads();                                          // the ring and s_m are free again
     head_start = at + (unsigned int)tiles;
     done += (unsigned int)(pb - pa);
     hb = next_head;
-    rows = next_rows;
-    tiles = next_tiles;
-    columns = next_columns;
-    order = next_order;
-    log_per = next_log_per;
     page_a = next_a;
     page_b = next_b;
     pages_ready = true;
   }
 
   // ---------------- publish the parts; merge every head all of whose parts are published
-  if (pend_parts[0] == 0 && pend_parts[1] == 0) return;       // uniform
   drain_vmem();
   __syncthreads();                                            // every thread's share of the parts is visible to the device
+  if (s_pend[0][2] == 0 && s_pend[1][2] == 0) return;         // uniform
   if (wave == 0) {
-    if (lane < 2 && (lane == 0 ? pend_parts[0] : pend_parts[1]) > 0) {
+    if (lane < 2 && s_pend[lane][2] > 0) {
       st_dev(&a.flags[2 * blockIdx.x + lane], a.tag);
       drain_vmem();
     }
-#pragma unroll
     for (int i = 0; i < 2; ++i) {
-      bool all = pend_parts[i] > 0;
-      for (int u = lane; u < pend_parts[i]; u += 64) all &= ld_dev(&a.flags[part_slot(pend_w0[i], u)]) == a.tag;
+      const int w0 = s_pend[i][1], parts = s_pend[i][2];
+      bool all = parts > 0;
+      for (int u = lane; u < parts; u += 64) all &= ld_dev(&a.flags[part_slot(w0, u)]) == a.tag;
       const bool every = __ballot(!all) == 0ull;
       if (lane == 0) s_flag[i] = every ? 1 : 0;
     }
   }
   __syncthreads();
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < 2; ++i) {
     if (s_flag[i] == 0) continue;
-    for (int u = threadIdx.x; u < pend_parts[i]; u += kDecThreads) st_dev(&a.flags[part_slot(pend_w0[i], u)], 0ull);
-    const int b = pend_head[i] / p.H_kv;
-    merge_parts<D, GP>(a, b, pend_head[i] - b * p.H_kv, pend_w0[i], pend_parts[i]);
+    const int h = (int)lane_value((unsigned int)s_pend[i][0], 0), w0 = (int)lane_value((unsigned int)s_pend[i][1], 0),
+              parts = (int)lane_value((unsigned int)s_pend[i][2], 0);
+    for (int u = threadIdx.x; u < parts; u += kDecThreads) st_dev(&a.flags[part_slot(w0, u)], 0ull);
+    const int b = h / p.H_kv;
+    merge_parts<D, GP>(a, b, h - b * p.H_kv, w0, parts);
   }
 }
 

@@ -701,3 +701,26 @@ def test_serving_loop(lava, dtype, page):
     decode(2, step)
     pages = owned(host(st.block_table), host(st.head_rows), page) + [int(p) for p in host(st.free_pages)[: int(st.n_free[0])]]
     assert sorted(pages) == list(range(n_pages))
+
+
+@pytest.mark.parametrize("H,Hkv,d,dtype,page", [(32, 8, 128, "bf16", 16), (8, 8, 64, "bf16", 32), (40, 8, 128, "f32", 16)])
+@pytest.mark.parametrize("kw", [{}, dict(softcap=20.0, window=60, bias=True)])
+def test_decode_many_short_heads(lava, H, Hkv, d, dtype, page, kw):
+    """More short heads than the device holds wavefronts, some of them empty, a few of many tiles."""
+    say(f"paged decode: short heads H{H}/{Hkv} d{d} {dtype} {kw}")
+    rng = np.random.default_rng(H)
+    rows = rng.integers(0, 70, (430, Hkv))
+    rows[rng.random(rows.shape) < 0.03] = 0
+    rows[rng.random(rows.shape) < 0.01] = 500
+    c = Decode(lava, H, Hkv, d, dtype, page, rows, H + 3)
+    first = c.check(**kw)
+    assert np.array_equal(c.run(**kw)[0], first)
+
+
+def test_decode_split_over_every_workgroup(lava):
+    """One head alone: as many parts as its length allows, merged in order."""
+    for H, rows, page in ((8, 70000, 128), (1, 33000, 16), (3, 5, 16)):
+        say(f"paged decode: one head of {rows} rows, {H} query heads")
+        c = Decode(lava, H, 1, 128, "bf16", page, [[rows]], H)
+        first = c.check()
+        assert np.array_equal(c.run()[0], first)
