@@ -745,6 +745,7 @@ def lava_page_tables(state: PageState, n_new: Optional[torch.Tensor] = None, hea
                        ("head_counts", head_counts, state.batch * state.n_kv_heads)):
         if t is not None and _dev(t, name, torch.int32).numel() != n:
             raise ValueError(f"{name} must hold {n} values")
+    _here(state.block_table)
     max_tokens = 0
     if slots is not None:
         max_tokens = _dev(slots, "slots", torch.int64).numel() // state.n_kv_heads
@@ -798,6 +799,7 @@ def paged_compact_problem(desc: LayerDesc, src_rows, k_src, v_src, head_offsets,
 def lava_compact_paged(desc: LayerDesc, problems, pool: PagePool, stream=None) -> None:
     """problems: sequence of PagedCompactProblem, or a ready (PagedCompactProblem * n) array."""
     pool._check(desc)
+    _here(pool.k)
     table = problems if isinstance(problems, ctypes.Array) else (PagedCompactProblem * len(problems))(*problems)
     st = lib.lava_compact_paged(ctypes.byref(desc), len(problems), ctypes.cast(table, ctypes.c_void_p), pool._ref, _stream(stream))
     _check(st, "lava_compact_paged")
@@ -820,6 +822,12 @@ def lava_rotary_turns(rot: RotaryDesc, device=None) -> torch.Tensor:
     out = torch.empty(max(rot.rotary_dim // 2, 1), dtype=torch.int64)
     _check(lib.lava_rotary_turns(ctypes.byref(rot), out.data_ptr()), "lava_rotary_turns")
     return out if device is None else out.to(device)
+
+
+def _here(t: torch.Tensor) -> None:
+    """The library works on the current device, on whose stream the call is enqueued."""
+    if _device_index is not None and t.is_cuda and t.get_device() != _device_index():
+        raise ValueError("the tensors are on another device than the current one")
 
 
 def _rows_of_heads(t: torch.Tensor, name: str, dtype) -> torch.Tensor:
@@ -852,6 +860,7 @@ def lava_rotary(rot: RotaryDesc, turns: torch.Tensor, positions: torch.Tensor, x
     dt = torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float32
     _rows_of_heads(x, "x", dt)
     tokens, heads, d = x.shape
+    _here(x)
     _check_turns(rot, turns, positions, tokens)
     if out is None:
         out = torch.empty(x.shape, dtype=dt, device=x.device)
@@ -871,6 +880,7 @@ def lava_rotary_append(desc: LayerDesc, rot: RotaryDesc, turns: torch.Tensor, po
     output allowed.  Returns q_out, the rotated queries [tokens, H, d_h]."""
     dt, d, hq, hkv = desc.torch_dtype, desc.head_dim, desc.n_q_heads, desc.n_kv_heads
     tokens = k.shape[0]
+    _here(k)
     k_stride, v_stride = _token_stride(k, "k", dt, (tokens, hkv, d)), _token_stride(v, "v", dt, (tokens, hkv, d))
     q_stride = 0
     if q is not None:
@@ -913,6 +923,7 @@ def lava_paged_decode(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_ta
     """One new token per sequence, q [batch, H, d_h], attends to the pages of its heads; block_table
     [batch, H_kv, pool.max_blocks], head_rows [batch, H_kv], q_pos [batch] int32.  Returns (out, lse)."""
     _dev(q, "q", desc.torch_dtype), _dev(block_table, "block_table", torch.int32), _dev(head_rows, "head_rows", torch.int32)
+    _here(q)
     batch = q.numel() // (desc.n_q_heads * desc.head_dim)
     heads = batch * desc.n_kv_heads
     if q.numel() != batch * desc.n_q_heads * desc.head_dim:

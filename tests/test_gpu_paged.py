@@ -724,3 +724,165 @@ def test_decode_split_over_every_workgroup(lava):
         c = Decode(lava, H, 1, 128, "bf16", page, [[rows]], H)
         first = c.check()
         assert np.array_equal(c.run()[0], first)
+
+
+# ------------------------------------------------------------------------------------------- the ends of the ranges
+def test_tables_of_many_heads(lava):
+    """More heads than one chunk of sums per thread covers, one of them the last to change."""
+    say("tables: 320 thousand heads")
+    rng = np.random.default_rng(31)
+    batch, heads, page, mb = 40000, 8, 16, 2
+    n_pages = batch * heads + 100
+    rows = rng.integers(0, 17, (batch, heads)).astype(np.int32)
+    nb = -(-rows // page)
+    order = rng.permutation(n_pages).astype(np.int32)
+    table = np.full((batch, heads, mb), -7, np.int32)
+    table[..., 0][nb > 0] = order[: int(nb.sum())]
+    free = np.full(n_pages, -9, np.int32)
+    n_free = n_pages - int(nb.sum())
+    free[:n_free] = order[n_pages - n_free:]
+    pos = rng.integers(0, 50, batch).astype(np.int32)
+    new = (rng.random(batch) < 0.02).astype(np.int32)
+    new[-1] = 3
+    release = (rng.random(batch) < 0.3).astype(np.int32)
+    tokens = int(new.sum()) + 1
+    t = Tables(lava, page, table, rows, pos, free, n_free)
+    check_step(t.step(new, None, release, tokens), P.page_tables(page, n_pages, table, rows, pos, free, n_free, new, None, release, tokens))
+
+
+@pytest.mark.parametrize("batch,heads,per", [(6, 4, 3), (3, 8, 9000)])
+def test_tables_one_map_alone(lava, batch, heads, per):
+    """Slots without positions, positions without slots."""
+    say(f"tables: one map alone, {per} tokens")
+    rng = np.random.default_rng(32)
+    page, mb = 64, 200
+    n_pages = batch * heads * mb
+    table, rows, pos, free, n_free = random_state(rng, batch, heads, mb, page, n_pages, 0.1)
+    new = np.full(batch, per)
+    tokens = int(new.sum()) + 2
+    want = P.page_tables(page, n_pages, table, rows, pos, free, n_free, new, None, None, tokens)
+    for which in ("slots", "positions"):
+        t = Tables(lava, page, table, rows, pos, free, n_free)
+        out = torch.full((tokens, heads), 7, dtype=torch.int64, device=DEV) if which == "slots" else torch.full((tokens,), 7, dtype=torch.int32, device=DEV)
+        lava.lava_page_tables(t.state, dev(new.astype(np.int32)), **{which: out})
+        torch.cuda.synchronize()
+        assert np.array_equal(host(out), want[5 if which == "slots" else 6])
+        assert np.array_equal(host(t.view("rows_out")), want[1]) and int(t.view("n_free_out")[0]) == want[4]
+
+
+def test_pool_beyond_four_gib(lava):
+    """Pages whose bytes lie beyond 2^32 of the pool's start: appended to, gathered into, attended to."""
+    say("a pool of 2 x 6.5 GB")
+    H, Hkv, d, page = 8, 2, 128, 256
+    n_pages = 100_000
+    desc = lava.LayerDesc.make(H, Hkv, d, 1, "bf16")
+    k, v = (torch.empty(n_pages, page, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    pos = torch.empty(n_pages, page, dtype=torch.int32, device=DEV)
+    pool = lava.PagePool(k, v, pos, max_blocks=3)
+    table = torch.tensor([[[99_999, 70_001, 5], [99_998, 80_000, 3]]], dtype=torch.int32, device=DEV)
+    rng = np.random.default_rng(41)
+    n, kept = 700, 520                                               # per head: two pages and eight rows
+    src = [stored(rng, (Hkv, n, d), "bf16") for _ in range(2)]
+    idx = np.concatenate([np.sort(rng.permutation(n)[:kept]) for _ in range(Hkv)]).astype(np.int32)
+    offs = dev(np.arange(Hkv + 1, dtype=np.int64) * kept)
+    sd = [lava.to_device(x, "bf16") for x in src]
+    lava.lava_compact_paged(desc, [lava.paged_compact_problem(desc, n, sd[0], sd[1], offs, dev(idx), kept * Hkv, table[0])], pool)
+    slots = torch.tensor([[5 * page + 8, 3 * page + 8], [99_999 * page + 7, 99_998 * page + 9]], device=DEV)
+    x = stored(rng, (2, H + 2 * Hkv, d), "bf16")
+    xd = lava.to_device(x, "bf16")
+    rot = lava.RotaryDesc.make(d)
+    lava.lava_rotary_append(desc, rot, lava.lava_rotary_turns(rot, DEV), torch.zeros(2, dtype=torch.int32, device=DEV), xd[:, :H],
+                            xd[:, H: H + Hkv], xd[:, H + Hkv:], pool, slots)             # position 0: unturned
+    torch.cuda.synchronize()
+    rows = [[synth.load_f64(s[g][idx[g * kept: (g + 1) * kept]], "bf16") for g in range(Hkv)] for s in src]
+    x64 = synth.load_f64(x, "bf16")
+    for g in range(Hkv):
+        for which, part in ((0, H + g), (1, H + Hkv + g)):
+            r = rows[which][g]
+            r[7 if g == 0 else 9] = x64[1, part]
+            rows[which][g] = np.concatenate([r, x64[:1, part]])
+    q = stored(rng, (1, H, d), "bf16")
+    out, _ = lava.lava_paged_decode(desc, lava.to_device(q, "bf16"), pool, table, torch.full((1, Hkv), kept + 1, dtype=torch.int32, device=DEV))
+    kp, vp = (np.zeros((Hkv, 768, d)) for _ in range(2))
+    for g in range(Hkv):
+        kp[g, : kept + 1], vp[g, : kept + 1] = rows[0][g], rows[1][g]
+    want, _, tol, _ = P.paged_decode(synth.load_f64(q, "bf16"), kp, vp, np.arange(Hkv).reshape(1, Hkv, 1), np.full((1, Hkv), kept + 1), 1 / math.sqrt(d))
+    torch.cuda.synchronize()
+    assert (np.abs(host(out.double()) - want) <= tol).all()
+
+
+def test_first_call_of_a_kernel_inside_a_capture(lava):
+    """A kernel whose first launch of the process is recorded: its grid is found without disturbing the capture."""
+    say("paged decode: first use inside a capture")
+    c = Decode(lava, 2, 2, 128, "f32", 16, [[70, 5]], 51)
+    options = lava.DecodeOptions.make(softcap=7.0)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        lava.lava_paged_decode(c.desc, c.dev["q"], c.pool, c.dev["table"], c.dev["rows"], options, out=c.out, lse=c.lse, workspace=c.ws[: c.need])
+    for _ in range(3):
+        c.out.fill_(777.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = host(c.out.double())
+    assert np.array_equal(got, c.check(softcap=7.0))
+
+
+def test_two_calls_at_once(lava):
+    """Two streams, each with its own workspace, over one pool."""
+    say("paged decode: two streams")
+    cs = [Decode(lava, 8, 2, 128, "bf16", 32, [[3000, 200], [40, 900]], 60 + i) for i in range(2)]
+    want = [c.check() for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    for _ in range(5):
+        for c in cs:
+            c.out.fill_(777.0)
+        torch.cuda.synchronize()
+        for c, s in zip(cs, streams):
+            lava.lava_paged_decode(c.desc, c.dev["q"], c.pool, c.dev["table"], c.dev["rows"], out=c.out, lse=c.lse, workspace=c.ws[: c.need], stream=s)
+        torch.cuda.synchronize()
+        for c, w in zip(cs, want):
+            assert np.array_equal(host(c.out.double()), w)
+
+
+def test_tensors_on_another_device(lava, monkeypatch):
+    """The binding launches on the current device only."""
+    c = Decode(lava, 2, 2, 64, "bf16", 16, [[5, 5]], 70)
+    monkeypatch.setattr(lava, "_device_index", lambda: 1)
+    with pytest.raises(ValueError):
+        lava.lava_paged_decode(c.desc, c.dev["q"], c.pool, c.dev["table"], c.dev["rows"])
+    with pytest.raises(ValueError):
+        lava.lava_rotary(lava.RotaryDesc.make(64), torch.zeros(32, dtype=torch.int64, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV),
+                         torch.zeros(1, 2, 64, device=DEV))
+    with pytest.raises(ValueError):
+        lava.lava_page_tables(lava.PageState.empty(1, 1, 1, 1, 16))
+
+
+def test_binding_refuses_shapes(lava):
+    z = lambda *s, dt=torch.float32: torch.zeros(*s, dtype=dt, device=DEV)
+    i32 = torch.int32
+    desc = lava.LayerDesc.make(4, 2, 64, 1, "f32")
+    pool = lava.PagePool(z(4, 16, 64), z(4, 16, 64), max_blocks=2)
+    bad = [lambda: lava.PagePool(z(4, 16, 64), z(4, 16, 32)), lambda: lava.PagePool(z(4, 16, 64), z(4, 16, 64), z(4, 15, dt=i32)),
+           lambda: lava.lava_paged_decode(desc, z(1, 4, 64), pool, z(1, 2, 3, dt=i32), z(1, 2, dt=i32)),
+           lambda: lava.lava_paged_decode(desc, z(1, 4, 64), pool, z(1, 2, 2, dt=i32), z(1, 3, dt=i32)),
+           lambda: lava.lava_paged_decode(desc, z(1, 4, 64), pool, z(1, 2, 2, dt=i32), z(1, 2, dt=i32), q_pos=z(2, dt=i32)),
+           lambda: lava.lava_paged_decode(desc, z(1, 4, 64), pool, z(1, 2, 2, dt=i32), z(1, 2, dt=i32), lava.DecodeOptions.make(slopes=z(3))),
+           lambda: lava.lava_paged_decode(desc, z(1, 4, 64), pool, z(1, 2, 2, dt=i32), z(1, 2, dt=i32), out=z(1, 4, 32)),
+           lambda: lava.lava_paged_decode(lava.LayerDesc.make(4, 2, 64, 1, "bf16"), z(1, 4, 64).bfloat16(), pool, z(1, 2, 2, dt=i32), z(1, 2, dt=i32)),
+           lambda: lava.lava_rotary(lava.RotaryDesc.make(64), z(32, dt=torch.int64), z(3, dt=i32), z(2, 2, 64)),
+           lambda: lava.lava_rotary(lava.RotaryDesc.make(64), z(31, dt=torch.int64), z(2, dt=i32), z(2, 2, 64)),
+           lambda: lava.lava_rotary(lava.RotaryDesc.make(64), z(32, dt=torch.int64), z(2, dt=i32), z(2, 2, 64), out=z(2, 3, 64)),
+           lambda: lava.lava_rotary(lava.RotaryDesc.make(64), z(32, dt=torch.int64), z(2, dt=i32), z(2, 2, 128)[..., ::2]),
+           lambda: lava.lava_rotary(lava.RotaryDesc.make(64), z(32, dt=torch.int64), z(2, dt=i32), z(2, 2, 64).half()),
+           lambda: lava.lava_rotary_append(desc, lava.RotaryDesc.make(64), z(32, dt=torch.int64), z(1, dt=i32), z(1, 4, 64), z(1, 3, 64), z(1, 2, 64), pool, z(1, 2, dt=torch.int64)),
+           lambda: lava.lava_rotary_append(desc, lava.RotaryDesc.make(64), z(32, dt=torch.int64), z(1, dt=i32), z(1, 4, 64), z(1, 2, 64), z(1, 2, 64), pool, z(1, 3, dt=torch.int64)),
+           lambda: lava.lava_page_tables(lava.PageState.empty(2, 2, 1, 4, 16), z(3, dt=i32)),
+           lambda: lava.lava_page_tables(lava.PageState.empty(2, 2, 1, 4, 16), z(2, dt=i32), slots=z(3, dt=torch.int64)),
+           lambda: lava.lava_page_tables(lava.PageState.empty(2, 2, 1, 4, 16), z(2, dt=i32), slots=z(2, 2, dt=torch.int64), positions=z(3, dt=i32)),
+           lambda: lava.paged_compact_problem(desc, 10, z(2, 10, 64), z(2, 10, 64), z(3, dt=torch.int64), z(4, dt=i32), 5, z(2, 2, dt=i32)),
+           lambda: lava.paged_compact_problem(desc, 11, z(2, 10, 64), z(2, 10, 64), z(3, dt=torch.int64), z(4, dt=i32), 4, z(2, 2, dt=i32))]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            say("not refused:", i)
