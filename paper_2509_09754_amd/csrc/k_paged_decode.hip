@@ -24,7 +24,10 @@
 // merges them in order.  Flags and tags are those of the decode step over the packed cache
 // (xblock.h): a flag counts only if it equals the call's tag, whoever merges a head clears its flags, nobody waits.
 //
-// Bound by HBM: 2 * d_h * elem bytes a row.
+// Bound by HBM: 2 * d_h * elem bytes a row.  2 x 8 heads of 131072 rows (1.07 GB) 198 us, 5.4 TB/s; 61 ragged sequences on 8 heads
+// (300 MB) 71 us, 4.2 TB/s, where the workgroups' shares end within 15 us of each other (XCDs differ by a tenth in what memory
+// gives them); 24 sequences with 7 heads a group, capped, biased and windowed (73 MB) 36.5 us: two trips to memory before the
+// first key, 16 us of bytes, uneven windows; one sequence of 8192 rows 11 us, a chain of counts, pages, keys, parts, flags, merge.
 #include <math.h>
 
 #include "common.h"
@@ -59,11 +62,9 @@ __device__ __forceinline__ unsigned int ceil_by(unsigned int x, unsigned int y, 
   return q * y < x ? q + 1u : q;
 }
 
-// What a workgroup that changes heads loses, in tiles.
+// What a workgroup that changes heads loses, in tiles (its loads in flight drain, 6 to 9 us while the device is busy).  61 ragged sequences:
+// 0 86.7 us, 3 72.2, 6 71.4, 10 74.0.
 constexpr unsigned int kHeadCost = 6u;
-
-// Tiles of a head that a wavefront handles alone where there are heads enough.
-constexpr int kShortHead = 16;
 
 // With a window the rows that count lie together, and a run of tiles would have all of them or none.  The tiles of a head then take
 // their places column by column of a matrix of kSpread rows, whose rows are taken kStep apart (place x is tile
@@ -256,10 +257,8 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
     }
   }
   if (total == 0u) return;
-  // Short heads, and more of them than wavefronts: a wavefront has heads of its own, and nothing is shared or merged.
   const float longest = max_of_wave((float)most);
-  const bool by_waves = longest <= (float)kShortHead && n_full >= kDecWaves * gridDim.x;
-  // Two other ways to cut.  By heads: units of at most `share` tiles of one head, a workgroup each, if there are enough workgroups for
+  // Three ways to cut.  By heads: units of at most `share` tiles of one head, a workgroup each, if there are enough workgroups for
   // all units.  Else through the line, where a head weighs kHeadCost tiles more than it has: what it costs to change heads.
   // Parts of a long head are merged one after another, a tenth of a microsecond each, where a tile more in a share is half of
   // one: no fewer tiles in a share than the root of a quarter of the longest head's.
@@ -267,6 +266,10 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
   unsigned int even = ceil_of(total, wgs), line = ceil_of(total + kHeadCost * n_full, wgs);
   if (even < least) even = least;
   if (line < least) line = least;
+  // By wavefronts: each has heads of its own, and nothing is shared or merged.  For many short heads, where changing heads together costs
+  // more than uneven wavefronts (rounds of tiles, half as many again allowed).  2048 heads of 40 / 300 / 900 rows 42 -> 20.5 us,
+  // 93 -> 73, 196 -> 189, 1024 of 40 / 300 / 450 22.4 -> 14.2, 47 -> 41, 61 -> 56.
+  const bool by_waves = 8.0f * longest * (float)ceil_of(n_full, kDecWaves * wgs) <= 3.0f * (float)line;
   unsigned int share = 0u;
   bool by_heads = false;
 #pragma unroll 1
@@ -315,7 +318,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
   };
   const int head_step = by_waves ? kDecWaves * (int)gridDim.x : 1, stride = by_waves ? 0 : 2;   // stride: log2 of this wavefront's, in tiles
   static_assert(kDecWaves == 4, "log2");
-  if (by_waves) hb = next_with_rows(kDecWaves * (int)blockIdx.x + wave, head_step);
+  if (by_waves) hb = next_with_rows(wave * (int)gridDim.x + (int)blockIdx.x, head_step);
   if (hb < 0 || hb >= n_heads) return;                        // more workgroups than units, or wavefronts than heads
 
   using VRaw = typename RawBits<S::kBpl>::type;

@@ -5,9 +5,12 @@
 // pages and pops them behind those of the heads before it.  Everything else follows from the sums: which page a
 // new block gets is one look-up in the stack, which slot a new row has is one look-up in the stack or the table.
 //
-// A step with little to write, as a decode step is, is one launch of one workgroup: a chain of four trips to memory.  For a large
-// one a first launch forms the sums, a workgroup for every 1024 heads, and every workgroup of the second adds up the
-// workgroups' totals for itself; that launch fills the device and is bound by the slots it writes, 8 bytes a row.
+// A step with little to write, as a decode step is, is one launch of one workgroup: a chain of four trips to memory (64 sequences on
+// 8 heads 7.0 us with the host's share).  For a large one a first launch forms the sums, a workgroup for every 1024 heads, and every
+// workgroup of the second adds up the workgroups' totals for itself; that launch fills the device and is bound by the slots it
+// writes, 8 bytes a row (559 thousand tokens on 8 heads, 36 MB of slots: 17.9 us both launches, 8.3 at a copy's rate; a third
+// of it is the first launch, the rest four dependent trips to memory around the writes).  Sequences that leave cost a launch
+// between the two, which puts their pages on the stack before any is taken (16384 heads, a quarter leaving: 19.6 us).
 #include "common.h"
 
 namespace lava {
@@ -185,16 +188,12 @@ __device__ __forceinline__ void fill_slots(const PageTablesArgs& a, const PlanSu
       continue;
     }
     if (b < 0 || (int)t >= end || !same_head) {
-      if (b < 0) {                                                   // the last sequence that starts at or before t
-        int lo = 0, hi = a.batch - 1;
-        while (lo < hi) {
-          const int mid = (lo + hi + 1) >> 1;
-          if (w.tok_at(mid) <= (int)t) lo = mid; else hi = mid - 1;
-        }
-        b = lo;
-      } else {
-        while ((int)t >= w.tok_at(b + 1)) ++b;                       // ends: t < tokens = tok_at(batch)
+      int lo = b < 0 ? 0 : b, hi = a.batch - 1;                       // the last sequence that starts at or before t
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (w.tok_at(mid) <= (int)t) lo = mid; else hi = mid - 1;
       }
+      b = lo;
       begin = w.tok_at(b);
       end = w.tok_at(b + 1);
       hb = b * a.heads + (int)g;
@@ -491,14 +490,17 @@ __global__ void __launch_bounds__(256) page_return_kernel(const PageTablesArgs a
 }
 
 // The first `head_wgs` workgroups take the heads (one each, or one for each wavefront), the others the tokens.
-constexpr int kSlotItems = 8;   // 16 prompts, 559 thousand tokens: 4 19.9 us, 8 18.7, 16 20.6
-constexpr long long kOnePlaces = 16384;
+constexpr int kSlotItems = 8;   // slots a thread writes: 4.5 million 4 19.9 us, 8 18.7, 16 20.6; 2.6 million one 21.4, 8 14.0; 0.6 million 10.4 with both
+// One workgroup finishes a step of so few places (slots, and table entries that may change hands) sooner than two launches begin:
+// 2560 slots 8.1 us (two launches 8.6), 3840 8.9 (8.6), 16000 15.4 (8.6); 512 heads that take a page now and then 6.8 (8.7).
+constexpr long long kOnePlaces = 2560;
+template <int ITEMS>
 __global__ void __launch_bounds__(256) page_fill_kernel(const PageTablesArgs a, const int chunk, const int head_wgs) {
   __shared__ FillPlan f;
   int error, top, n_free;
   const PlanSums w = add_up(a, chunk, f, (int)blockIdx.x >= head_wgs, error, top, n_free);
   if ((int)blockIdx.x >= head_wgs) {
-    fill_slots_wide<kSlotItems>(a, w, top, error != 0 ? 0 : w.total_tok, (blockIdx.x - head_wgs) * (256u * kSlotItems));
+    fill_slots_wide<ITEMS>(a, w, top, error != 0 ? 0 : w.total_tok, (blockIdx.x - head_wgs) * (256u * ITEMS));
     return;
   }
   const int heads = a.batch * a.heads;
@@ -549,15 +551,21 @@ int32_t launch_page_tables(const PageTablesArgs& a, hipStream_t s) {
     st = launch_status();
     if (st != LAVA_OK) return st;
   }
-  const long long slot_wgs = (places + 256 * kSlotItems - 1) / (256 * kSlotItems);
+  // one place a thread where that is at most 1024 workgroups, else kSlotItems
+  const bool many = places > 256 * 1024;
+  const long long per = 256 * (many ? kSlotItems : 1), slot_wgs = (places + per - 1) / per;
+  const dim3 grid((unsigned)(head_wgs + slot_wgs)), block(256);
   ProfScope ps(KID_PAGE_FILL, s);
-  hipLaunchKernelGGL(page_fill_kernel, dim3((unsigned)(head_wgs + slot_wgs)), dim3(256), 0, s, a, chunk, (int)head_wgs);
+  if (many) hipLaunchKernelGGL(page_fill_kernel<kSlotItems>, grid, block, 0, s, a, chunk, (int)head_wgs);
+  else hipLaunchKernelGGL(page_fill_kernel<1>, grid, block, 0, s, a, chunk, (int)head_wgs);
   return launch_status();
 }
 
 // ------------------------------------------------------------------------------------------
 // The gather of an eviction's survivors into pages: bound by HBM, 4 * d_h * elem bytes a row.  A row is
-// moved by (row bytes / 16) lanes; the workgroups of a problem walk over its survivors.
+// moved by (row bytes / 16) lanes; the workgroups of a problem walk over its survivors.  131072 rows of 2 x 256 bytes (16 prompts):
+// 32.0 us, 4.2 TB/s read and written, of rows that lie apart on both sides; two, four and eight rows in flight a lane took 32.9,
+// 34.7 and 38.0.
 // ------------------------------------------------------------------------------------------
 namespace {
 
