@@ -8,8 +8,8 @@
 //
 // A unit of work is 32 bytes of a head: the E = 16 / elem pairs j E .. j E + E - 1, which are two chunks of 16 bytes half
 // a rotation apart (or, interleaved, next to each other); behind the rotated part two neighbouring chunks that pass.
-// Bound by HBM: every row is read and written once.  8197 tokens of 32 + 2 x 8 heads (202 MB): 41.4 us, 4.9 TB/s, where a copy takes
-// 40.5; 4115 x 32 heads of 32-bit values, head by head: 27.3 us, 4.9 TB/s.  64 tokens: 3.5 us in the kernel.
+// Bound by HBM: every row is read and written once.  8197 tokens of 32 + 2 x 8 heads (202 MB): 42 us, 4.8 TB/s, where a copy takes
+// 40.5; 4115 x 32 heads of 32-bit values, head by head: 26.6 us, 5.1 TB/s (27.4 without the row ahead).  64 tokens: 3.5 us.
 #include "common.h"
 #include "tile_ring.h"
 
@@ -131,48 +131,62 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const RotaryArgs a)
   __shared__ float2 s_cs[kRotMaxPairs];
   const long long token = blockIdx.x;
   const int pairs = a.rot / 2, pos = a.positions[token];
-  if (pos < 0) return;                                             // uniform: the token is left out
-  if ((int)threadIdx.x < pairs) {
-    const float2 cs = unit_turn((unsigned long long)(unsigned int)pos * a.turns[threadIdx.x]);
-    s_cs[threadIdx.x] = make_float2(cs.x * a.cos_mul, cs.y * a.sin_mul);
-  }
-  __syncthreads();
   const int rows = a.hq + 2 * a.hkv;                               // of a token: heads to turn into `out`, keys, values
   const bool by_value = a.interleaved == 0 && pairs % E != 0;      // uniform
   const int turned = a.interleaved ? (pairs + E - 1) / E : pairs / E;   // units with turned pairs
   const int j = threadIdx.x % kUnits;
   // chunks of this thread's unit
-  int c0 = 2 * j, c1 = 2 * j + 1;
-  if (!a.interleaved) {
-    if (j < turned) { c0 = j; c1 = j + turned; } else { c0 = 2 * j; c1 = 2 * j + 1; }
-  }
-  for (int row = threadIdx.x / kUnits; row < rows; row += kRotThreads / kUnits) {
-    const char* src;
-    char* dst;
-    bool turn = true;
+  const bool apart = !a.interleaved && j < turned;
+  const int c0 = apart ? j : 2 * j, c1 = apart ? j + turned : 2 * j + 1;
+
+  // one row ahead: where it lies and, unless it goes value by value, its chunks
+  const char* src = nullptr;
+  char* dst = nullptr;                                             // null: the row has no slot
+  bool turn = true;
+  u32x4 x0, x1;
+  auto fetch = [&](int row) {
+    dst = nullptr;
+    if (row >= rows) return;
     if (row < a.hq) {
+      turn = true;
       src = a.x + token * a.x_token + row * a.x_head;
       dst = a.out + token * a.out_token + row * a.out_head;
     } else {
-      const int g = row - a.hq < a.hkv ? row - a.hq : row - a.hq - a.hkv;
       turn = row - a.hq < a.hkv;
+      const int g = turn ? row - a.hq : row - a.hq - a.hkv;
       const long long slot = a.slots[token * a.hkv + g];
-      if (slot < 0 || slot >= a.pool_rows) continue;
+      if (slot < 0 || slot >= a.pool_rows) return;
       src = turn ? a.k + token * a.k_token + g * kRowBytes : a.v + token * a.v_token + g * kRowBytes;
       dst = (turn ? a.k_pages : a.v_pages) + slot * kRowBytes;
-      if (turn && j == 0 && a.pos_pages != nullptr) a.pos_pages[slot] = pos;
+      if (turn && j == 0 && pos >= 0 && a.pos_pages != nullptr) a.pos_pages[slot] = pos;
     }
-    if (turn && by_value) {
-      turn_values<DT, D>(src, dst, j, a.rot, s_cs);
-      continue;
+    if (turn && by_value) return;
+    x0 = *reinterpret_cast<const u32x4*>(src + c0 * 16);
+    x1 = *reinterpret_cast<const u32x4*>(src + c1 * 16);
+  };
+  int row = threadIdx.x / kUnits;
+  fetch(row);
+  if ((int)threadIdx.x < pairs) {
+    const float2 cs = unit_turn((unsigned long long)(unsigned int)pos * a.turns[threadIdx.x]);
+    s_cs[threadIdx.x] = make_float2(cs.x * a.cos_mul, cs.y * a.sin_mul);
+  }
+  __syncthreads();
+  if (pos < 0) return;                                             // uniform: the token is left out
+  for (; row < rows; ) {
+    if (dst != nullptr) {
+      if (turn && by_value) {
+        turn_values<DT, D>(src, dst, j, a.rot, s_cs);
+      } else {
+        if (turn && j < turned) {
+          if (a.interleaved) turn_neighbours<DT>(x0, x1, &s_cs[j * E], pairs - j * E);
+          else turn_halves<DT>(x0, x1, &s_cs[j * E]);
+        }
+        *reinterpret_cast<u32x4*>(dst + c0 * 16) = x0;
+        *reinterpret_cast<u32x4*>(dst + c1 * 16) = x1;
+      }
     }
-    u32x4 x0 = *reinterpret_cast<const u32x4*>(src + c0 * 16), x1 = *reinterpret_cast<const u32x4*>(src + c1 * 16);
-    if (turn && j < turned) {
-      if (a.interleaved) turn_neighbours<DT>(x0, x1, &s_cs[j * E], pairs - j * E);
-      else turn_halves<DT>(x0, x1, &s_cs[j * E]);
-    }
-    *reinterpret_cast<u32x4*>(dst + c0 * 16) = x0;
-    *reinterpret_cast<u32x4*>(dst + c1 * 16) = x1;
+    row += kRotThreads / kUnits;
+    fetch(row);
   }
 }
 
