@@ -1,5 +1,5 @@
-// What the decode steps over the packed cache and over pages share: the shape of a workgroup and its tile ring, lane moves, and the
-// tag by which a call knows its own flags.
+// What the decode steps over the packed cache and over pages share: the shape of a workgroup and its tile ring, lane moves (which
+// the block tables' sums use too), and the tag by which a call knows its own flags.
 #pragma once
 
 #include <unistd.h>

@@ -12,6 +12,7 @@
 // of it is the first launch, the rest four dependent trips to memory around the writes).  Sequences that leave cost a launch
 // between the two, which puts their pages on the stack before any is taken (16384 heads, a quarter leaving: 19.6 us).
 #include "common.h"
+#include "decode_parts.h"
 
 namespace lava {
 
@@ -47,23 +48,10 @@ __host__ __device__ inline PlanLayout plan_layout(int batch, int heads) {
   return l;
 }
 
-// Inclusive sum over the lanes of a wavefront.
-__device__ __forceinline__ unsigned int lane_sum(unsigned int x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const unsigned int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
-}
+// Sum over the lanes of values below 2^48, in two halves of 24 bits and more.
 __device__ __forceinline__ unsigned long long wave_total(unsigned long long x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    const unsigned int lo = __shfl_xor((unsigned int)x, d), hi = __shfl_xor((unsigned int)(x >> 32), d);
-    x += ((unsigned long long)hi << 32) | lo;
-  }
-  return x;
+  const unsigned int lo = lane_value(wave_incl((unsigned int)x & 0xffffffu), 63), hi = lane_value(wave_incl((unsigned int)(x >> 24)), 63);
+  return ((unsigned long long)hi << 24) + lo;
 }
 
 // Exclusive sums of a workgroup's values x[u] of items u * kPlanThreads + thread, in the order of the items.  32 bits: where they
@@ -74,7 +62,7 @@ __device__ __forceinline__ void plan_scan(unsigned int (&x)[PER], unsigned int* 
   unsigned int incl[PER];
 #pragma unroll
   for (int u = 0; u < PER; ++u) {
-    incl[u] = lane_sum(x[u]);
+    incl[u] = wave_incl(x[u]);
     if (lane == 63) s_part[u * kPlanWaves + wave] = incl[u];
   }
   __syncthreads();
@@ -82,9 +70,9 @@ __device__ __forceinline__ void plan_scan(unsigned int (&x)[PER], unsigned int* 
     unsigned int carry = 0u;
     for (int i0 = 0; i0 < PER * kPlanWaves; i0 += 64) {
       const int i = i0 + lane;
-      const unsigned int v = i < PER * kPlanWaves ? s_part[i] : 0u, s = lane_sum(v);
+      const unsigned int v = i < PER * kPlanWaves ? s_part[i] : 0u, s = wave_incl(v);
       if (i < PER * kPlanWaves) s_part[i] = carry + s - v;
-      carry += __shfl(s, 63);
+      carry += lane_value(s, 63);
     }
   }
   __syncthreads();
