@@ -527,6 +527,8 @@ int32_t lava_decode_attention(const lava_layer_desc* desc, int32_t batch, const 
  *   lava_paged_decode    one new token per sequence attends to the pages
  * Nothing is read back by any of them.  A slot is page * page_rows + row in the page; a negative one
  * is no row.  Page numbers and slots are checked on the device against the pool before they are followed.
+ * A workspace may hold anything and serves one call at a time; calls that share a state or a pool's pages are
+ * ordered by the caller (one stream, or events).
  */
 typedef struct lava_page_pool {
   int64_t n_pages;      /* 1 .. 2^31 - 1                                                      */

@@ -20,7 +20,8 @@
 //    Published buffers in this library: the statistic partials (ent_part), the statistics partials
 //    of the persistent sweep and its unit / completion words; of the selection the histograms, the
 //    segments of keys, the exchange words (one per workgroup), the state words (the outcome among them)
-//    and, if prepared, head_counts; of a decode step the units' partials (part_ml, part_acc) and flags.
+//    and, if prepared, head_counts; of a decode step the units' partials (part_ml, part_acc) and flags, of one over
+//    pages the parts' (the same names).
 //  * The selection's segments and exchange words: every wavefront drains its stores to the workgroup's
 //    segment, a workgroup barrier follows, then one lane stores the word with the segment's length and
 //    the epoch; whoever has seen the epoch finds the keys.  Segment and word are written again in a
@@ -35,14 +36,15 @@
 //    barrier), one lane stores the flag, DRAINS AGAIN and only then reads the flags of the head.  Of any
 //    two workgroups the one whose flag became visible later therefore reads both, so at least one workgroup of a head
 //    finds all its flags.  The workspace may hold anything: a flag counts only if it equals the call's
-//    tag, which no other call uses, and is cleared by whoever merges the head.
+//    tag, which no other call uses, and is cleared by whoever merges the head.  The step over pages does the same with the
+//    parts of its share's first and last head: both flags are stored, drained, and then both heads' flags read.
 //  * Counters, tickets and the outcome (the decode step has none of them) must be zero before the launch that uses them: they are cleared by an
 //    EARLIER kernel of the same call on the same stream (the value-norm / statistics launch, the
 //    selection's init kernel, a cascade step's plan kernel) or by the same kernel before a grid-wide wait that every workgroup passes;
 //    never by a memset node (a caller may capture the calls in a graph).
 //  * Stress tests: tests/test_gpu_parity.py runs launches of over a thousand workgroups thirty times and
 //    requires the bits of the first run every time, and prepared selections whose waits are limited to
-//    a few polls; tests/test_gpu_decode_units.py replays decode steps over workspaces of any contents.
+//    a few polls; tests/test_gpu_decode_units.py and tests/test_gpu_paged.py replay decode steps over workspaces of any contents.
 #pragma once
 
 #include <hip/hip_runtime.h>
