@@ -649,7 +649,7 @@ int32_t lava_rotary_turns(const lava_rotary_desc* rot, uint64_t* turns);
  *              overlap is not.  Strides are multiples of 16 bytes
  *   transpose  non-zero: the transposed rotation, which is the gradient's way through it (the inverse, for
  *              magnitude 1)
- * dtype LAVA_F32 or LAVA_BF16, head_dim 64 or 128; 32-bit arithmetic, rounded once.
+ * dtype LAVA_F32 or LAVA_BF16, head_dim 64 or 128, n_heads <= 1024, n_tokens < 2^31; 32-bit arithmetic, rounded once.
  */
 int32_t lava_rotary(const lava_rotary_desc* rot, const uint64_t* turns, int32_t dtype, int32_t head_dim,
                     int64_t n_tokens, int32_t n_heads, const int32_t* positions, const void* x,
@@ -667,6 +667,7 @@ int32_t lava_rotary(const lava_rotary_desc* rot, const uint64_t* turns, int32_t 
  *   slots          device int64 [n_tokens][H_kv] as written by lava_page_tables; a row whose slot is negative
  *                  or not in the pool is not written.  No two rows may have the same slot
  *   positions      device int32 [n_tokens]; a token with a negative one is left out altogether
+ * n_tokens * H_kv < 2^31.
  */
 int32_t lava_rotary_append(const lava_layer_desc* desc, const lava_rotary_desc* rot, const uint64_t* turns,
                            int64_t n_tokens, const int32_t* positions, const void* q, int64_t q_token_stride,
@@ -688,7 +689,8 @@ size_t lava_paged_decode_workspace_bytes(const lava_layer_desc* desc);
  *   out[h] = Softmax(z[h]) V_g,  g = h / G, over the head_rows[b][g] rows that head g of sequence b holds.
  *
  *   q            device [batch][H][d_h], dtype of the descriptor
- *   pool         k, v; pos is read if the options have a window or slopes (INVALID_ARG if it is NULL then)
+ *   pool         k, v; pos is read if the options have a window or slopes (INVALID_ARG if it is NULL or not
+ *                16-byte aligned then)
  *   block_table  device int32 [batch][H_kv][max_blocks]; only the entries of rows that are held are read
  *   head_rows    device int32 [batch][H_kv]
  *   options      or NULL

@@ -193,8 +193,25 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const RotaryArgs a)
 template <int DT, int D>
 int32_t launch_rotary_type(const RotaryArgs& a, hipStream_t s) {
   ProfScope ps(KID_ROTARY, s);
-  hipLaunchKernelGGL((rotary_kernel<DT, D>), dim3((unsigned)a.n_tokens), dim3(kRotThreads), 0, s, a);
-  return launch_status();
+  constexpr long long kTokens = 1ll << 23;                           // a launch's threads are counted in 32 bits
+  for (long long t0 = 0; t0 < a.n_tokens; t0 += kTokens) {
+    RotaryArgs b = a;
+    b.n_tokens = a.n_tokens - t0 < kTokens ? a.n_tokens - t0 : kTokens;
+    b.positions += t0;
+    if (a.x != nullptr) {
+      b.x += t0 * a.x_token;
+      b.out += t0 * a.out_token;
+    }
+    if (a.slots != nullptr) {
+      b.k += t0 * a.k_token;
+      b.v += t0 * a.v_token;
+      b.slots += t0 * a.hkv;
+    }
+    hipLaunchKernelGGL((rotary_kernel<DT, D>), dim3((unsigned)b.n_tokens), dim3(kRotThreads), 0, s, b);
+    const int32_t st = launch_status();
+    if (st != LAVA_OK) return st;
+  }
+  return LAVA_OK;
 }
 
 }  // namespace

@@ -247,7 +247,7 @@ int32_t lava_paged_decode(const lava_layer_desc* desc, int32_t batch, const void
   if (options != nullptr) o = *options;
   if (!(o.softcap >= 0.0f) || o.softcap > 1e30f || o.window < 0) return LAVA_ERR_INVALID_ARG;
   const bool needs_pos = o.window > 0 || o.slopes != nullptr;
-  if (needs_pos && (q_pos == nullptr || pool->pos == nullptr)) return LAVA_ERR_INVALID_ARG;
+  if (needs_pos && (q_pos == nullptr || pool->pos == nullptr || !aligned16(pool->pos))) return LAVA_ERR_INVALID_ARG;
   if (batch > 65535 || (int64_t)batch * d.n_kv_heads > 65536) return LAVA_ERR_SHAPE;
   // the tiles of all heads are counted in 32 bits
   if ((int64_t)batch * d.n_kv_heads > (((int64_t)1 << 35) - 1) / ((int64_t)pool->max_blocks * pool->page_rows)) return LAVA_ERR_SHAPE;

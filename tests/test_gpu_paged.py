@@ -886,3 +886,75 @@ def test_binding_refuses_shapes(lava):
         with pytest.raises(ValueError):
             call()
             say("not refused:", i)
+
+
+def test_decode_without_rows_and_without_lse(lava):
+    """Nothing held at all; a softmax scale of the caller's; no log-sum-exp asked for."""
+    say("paged decode: empty batch, scale, no lse")
+    import ctypes
+    c = Decode(lava, 4, 2, 64, "bf16", 16, [[0, 0], [0, 0]], 80)
+    out = c.check()
+    assert (out == 0).all()
+    c = Decode(lava, 4, 2, 128, "f32", 16, [[50, 3], [0, 900]], 81, scale=0.031)
+    first = c.check()
+    c.out.fill_(777.0)
+    assert lava.lib.lava_paged_decode(ctypes.byref(c.desc), 2, c.dev["q"].data_ptr(), ctypes.byref(c.pool.c), c.dev["table"].data_ptr(),
+                                      c.dev["rows"].data_ptr(), None, None, c.out.data_ptr(), None, c.ws.data_ptr(), c.need, None) == lava.LAVA_OK
+    torch.cuda.synchronize()
+    assert np.array_equal(host(c.out.double()), first)
+
+
+@pytest.mark.parametrize("window", [0, 40])
+def test_bad_tables_among_many_short_heads(lava, window):
+    """Heads that wavefronts handle alone: impossible row counts and pages that are none give NaN for those heads only."""
+    say(f"paged decode: bad tables among short heads, window {window}")
+    rng = np.random.default_rng(82)
+    rows = rng.integers(1, 60, (400, 8))
+    c = Decode(lava, 8, 8, 64, "bf16", 16, rows, 82)
+    c.rows[7, 3], c.rows[399, 7] = -4, c.table.shape[2] * 16 + 1
+    c.table[100, 0, 0], c.table[0, 0, 0], c.table[200, 5, (c.rows[200, 5] - 1) // 16] = -1, c.k.shape[0], 1 << 30
+    c.dev["rows"].copy_(dev(c.rows)), c.dev["table"].copy_(dev(c.table))
+    out = c.check(window=window)
+    bad = np.zeros((400, 8), bool)
+    for at in ((7, 3), (399, 7), (100, 0), (0, 0), (200, 5)):
+        bad[at] = True
+    assert np.array_equal(np.isnan(out).all(-1), bad)
+
+
+def test_rotary_of_more_tokens_than_a_launch_counts(lava):
+    """Eight million tokens and five."""
+    say("rotary: 2^23 + 5 tokens")
+    tokens, d = (1 << 23) + 5, 64
+    desc = lava.RotaryDesc.make(d)
+    turns = lava.lava_rotary_turns(desc, DEV)
+    x = torch.randn(tokens, 1, d, device=DEV).bfloat16()
+    pos = torch.randint(0, 1 << 20, (tokens,), dtype=torch.int32, device=DEV)
+    out = lava.lava_rotary(desc, turns, pos, x)
+    at = torch.cat([torch.arange(3), torch.arange((1 << 23) - 3, tokens)]).to(DEV)
+    few = lava.lava_rotary(desc, turns, pos[at].contiguous(), x[at].contiguous())
+    torch.cuda.synchronize()
+    assert torch.equal(out[at], few)
+    assert not bool((out == 0).all(-1).any())
+
+
+def test_buffers_off_their_lines(lava):
+    """The same step through tables whose buffers start four bytes off a line: nothing assumes more than its type's alignment."""
+    say("tables and decode: buffers off their lines")
+    off = lambda t: torch.cat([torch.zeros(1, dtype=t.dtype, device=DEV), t.reshape(-1)])[1:].view(t.shape)
+    rng = np.random.default_rng(83)
+    page, batch, heads, mb, n_pages = 16, 6, 3, 7, 200
+    table, rows, pos, free, n_free = random_state(rng, batch, heads, mb, page, n_pages, 0.4)
+    st = lava.PageState(*(off(dev(a)) for a in (table, rows, pos, free, np.array([n_free], np.int32))), page)
+    new = np.minimum(rng.integers(0, 4, batch), mb * page - rows.max(1)).astype(np.int32)
+    tokens = int(new.sum()) + 1
+    slots, positions = off(torch.zeros(tokens, heads, dtype=torch.int64, device=DEV)), off(torch.zeros(tokens, dtype=torch.int32, device=DEV))
+    lava.lava_page_tables(st, off(dev(new)), slots=slots, positions=positions)
+    torch.cuda.synchronize()
+    want = P.page_tables(page, n_pages, table, rows, pos, free, n_free, new, max_tokens=tokens)
+    assert np.array_equal(host(st.block_table), want[0]) and np.array_equal(host(slots), want[5]) and np.array_equal(host(positions), want[6])
+    c = Decode(lava, 6, 2, 64, "f32", 16, [[90, 30], [5, 700]], 84)
+    first = c.check(window=50, bias=True)
+    for name in ("table", "rows", "slopes", "q_pos"):
+        c.dev[name] = off(c.dev[name])
+    c.out, c.lse = off(c.out), off(c.lse)
+    assert np.array_equal(c.run(window=50, bias=True)[0], first)

@@ -114,6 +114,7 @@ def decode(d=None, batch=2, q=FAKE, p=None, table=FAKE, rows=FAKE, o=None, q_pos
     (dict(p=pool(max_blocks=0)), ARG), (dict(o=lava.DecodeOptions(-1.0, 0, None)), ARG), (dict(o=lava.DecodeOptions(0.0, -1, None)), ARG),
     (dict(o=lava.DecodeOptions(math.nan, 0, None)), ARG), (dict(o=lava.DecodeOptions(0.0, 5, None)), ARG),
     (dict(o=lava.DecodeOptions(0.0, 0, FAKE)), ARG), (dict(o=lava.DecodeOptions(0.0, 5, None), q_pos=FAKE, p=pool(pos=None)), ARG),
+    (dict(o=lava.DecodeOptions(0.0, 5, None), q_pos=FAKE, p=pool(pos=ODD)), ARG), (dict(p=pool(max_blocks=1 << 25), batch=130), SHAPE),
     (dict(batch=65536), SHAPE), (dict(batch=8193), SHAPE), (dict(ws=None), SPACE), (dict(ws=FAKE + 128), SPACE), (dict(ws_bytes=255), SPACE)])
 def test_decode_refuses(kw, want):
     assert decode(**kw) == want
