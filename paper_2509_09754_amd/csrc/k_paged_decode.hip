@@ -1,10 +1,11 @@
 // Decode-step attention over the pages of the paged cache: out[h] = Softmax(z[h]) V_g over the rows that head g holds, z =
 // scale <q, k>, optionally capped (cap tanh(z / cap)), biased by distance and restricted to a window of positions.
 //
-// The work is one line of 32-row tiles, head after head through the whole batch.  It is cut into equal shares, one per workgroup
-// and as many workgroups as the device holds at a time, whatever the lengths: a ragged batch, a long sequence alone and a
-// padded one all end together, and the host needs to know no length.  A share is a run of tiles that may end in one head
-// and go on in the next; every wavefront finds its workgroup's by itself, with one pass over the row counts (sums over its lanes).
+// The work is one line of 32-row tiles, head after head through the whole batch, cut on the device for as many workgroups as it holds at
+// a time, whatever the lengths: a ragged batch, a long sequence alone and a padded one end together, and the host needs to
+// know no length.  Every wavefront finds its workgroup's share by itself, with one pass over the row counts (sums over its
+// lanes), in one of three cuts: units of one head where that is even; equal runs of the line, which may end in one head and go on
+// in the next; whole heads by single wavefronts, for many short ones.
 //
 // Inside a share's part of one head the wavefronts take tiles in turn.  K goes through a wavefront's own LDS ring with
 // direct-to-LDS loads, two tiles ahead, V straight into registers, one tile ahead (a lane owns the same columns of every row):
@@ -69,7 +70,8 @@ constexpr unsigned int kHeadCost = 6u;
 // With a window the rows that count lie together, and a run of tiles would have all of them or none.  The tiles of a head then take
 // their places column by column of a matrix of kSpread rows, whose rows are taken kStep apart (place x is tile
 // (kStep x % kSpread) * columns + x / kSpread, or none), so that every share has its part of the window, and (kSpread is odd)
-// every wavefront of it.
+// every wavefront of it.  24 windowed sequences: runs of tiles 51 us, 16 rows 47.7, several tiles a place (below) 42.4, 17 rows 39.8,
+// rows 7 apart 38.3.
 constexpr int kStep = 7;
 constexpr int kSpread = 17;
 __device__ __forceinline__ int spread_columns(int tiles, bool spread) { return spread && tiles >= 4 * kSpread ? (tiles + kSpread - 1) / kSpread : 0; }
