@@ -8,6 +8,7 @@
 
 #include "../../include/lava.h"
 #include "select_layout.h"
+#include "tile_order.h"
 
 namespace lava {
 
@@ -71,7 +72,6 @@ __device__ __forceinline__ unsigned int sel_digit0(unsigned int key) {
 }
 
 // ---------------------------------------------------------------- sweep (K, V) kernels
-constexpr int kTileKeys = 32;        // keys per MFMA tile
 constexpr int kMaxChunkHeads = 4;    // query heads a wavefront keeps in registers
 
 struct SweepPlan {

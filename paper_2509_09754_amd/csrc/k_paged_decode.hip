@@ -67,26 +67,6 @@ __device__ __forceinline__ unsigned int ceil_by(unsigned int x, unsigned int y, 
 // 0 86.7 us, 3 72.2, 6 71.4, 10 74.0.
 constexpr unsigned int kHeadCost = 6u;
 
-// With a window the rows that count lie together, and a run of tiles would have all of them or none.  The tiles of a head then take
-// their places column by column of a matrix of kSpread rows, whose rows are taken kStep apart (place x is tile
-// (kStep x % kSpread) * columns + x / kSpread, or none), so that every share has its part of the window, and (kSpread is odd)
-// every wavefront of it.  24 windowed sequences: runs of tiles 51 us, 16 rows 47.7, several tiles a place (below) 42.4, 17 rows 39.8,
-// rows 7 apart 38.3.
-constexpr int kStep = 7;
-constexpr int kSpread = 17;
-__device__ __forceinline__ int spread_columns(int tiles, bool spread) { return spread && tiles >= 4 * kSpread ? (tiles + kSpread - 1) / kSpread : 0; }
-__device__ __forceinline__ int places_of(int tiles, bool spread) {
-  const int columns = spread_columns(tiles, spread);
-  return columns > 0 ? columns * kSpread : tiles;
-}
-// With a window a place of the line is not one tile but 2, 4 or 8 of them: about as many as hold one that counts if the head's rows are spread
-// over the sequence's positions (and no more than finding out costs).  An estimate: it moves cuts, not results.
-__device__ __forceinline__ int log_per_place(int q_pos, int window) {
-  const long long seen = (long long)q_pos + 1;
-  return seen >= 8ll * window ? 3 : seen >= 4ll * window ? 2 : seen >= 2ll * window ? 1 : 0;
-}
-__device__ __forceinline__ int tile_at(int place, int columns) { return columns > 0 ? (place % kSpread * kStep % kSpread) * columns + place / kSpread : place; }
-
 // Tiles of a head with that many rows; -1: it cannot have them.
 __device__ __forceinline__ int head_tiles(const PagedDecodeArgs& a, int rows) {
   if (rows < 0 || rows > a.max_blocks << a.page_shift) return -1;
@@ -340,12 +320,12 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
   // Pages of tile0, tile0 + 2^stride, ... of head h, kBlock of them, as far as there are `here`: a lane each, or four (OPT)
   auto load_pages = [&](int h, int rows_h, int columns, int tile0, int here, int& page_a, int& page_b) {
     const int i = OPT ? lane >> 2 : lane;
-    const int row0 = tile_at(tile0 + (i << stride), columns) * kTileKeys;
+    const unsigned int row0 = row_at(tile0 + (i << stride), columns);
     const int* table = p.block_table + (long long)h * p.max_blocks;
     page_a = page_b = 0;
-    if (i < here && (!OPT || row0 < rows_h)) {
+    if (i < here && (!OPT || row0 < (unsigned int)rows_h)) {
       page_a = table[row0 >> shift];
-      page_b = shift == 4 && row0 + 16 < rows_h ? table[(row0 >> 4) + 1] : page_a;
+      page_b = shift == 4 && row0 + 16u < (unsigned int)rows_h ? table[(row0 >> 4) + 1u] : page_a;
     }
   };
 
@@ -430,13 +410,13 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
         }
         if (OPT) {
           const int i = lane >> 2, part = lane & 3;           // rows 8 part .. 8 part + 7 of tile i
-          const int row0 = tile_at(tile0 + (i << stride), columns) * kTileKeys;
+          const unsigned int row0 = row_at(tile0 + (i << stride), columns);
           seen = 0u;
-          if (i < here && row0 < rows) {
+          if (i < here && row0 < (unsigned int)rows) {
             int4 x = make_int4(q_pos, q_pos, q_pos, q_pos), x2 = x;
             if (p.pos != nullptr) {                            // uniform
               const long long place = shift == 4 ? ((long long)(part < 2 ? page_a : page_b) << 4) + 8 * (part & 1)
-                                                 : ((long long)page_a << shift) + (row0 & page_mask) + 8 * part;
+                                                 : ((long long)page_a << shift) + ((int)row0 & page_mask) + 8 * part;
               x = *reinterpret_cast<const int4*>(p.pos + place);
               x2 = *reinterpret_cast<const int4*>(p.pos + place + 4);
             }
@@ -446,7 +426,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
             for (int e = 0; e < 8; ++e) {
               const unsigned int d = (unsigned int)q_pos - (unsigned int)y[e];   // a later row: 2^31 and more
               back[e] = (float)d;
-              if (d < window && row0 + 8 * part + e < rows) seen |= 1u << e;
+              if (d < window && (int)row0 + 8 * part + e < rows) seen |= 1u << e;
             }
             float* dst = &s_back[wave][lane * 8];
 #pragma unroll
@@ -458,7 +438,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
         }
       }
       unsigned long long todo = OPT ? __ballot(seen != 0u) & 0x1111111111111111ull : here == 64 ? ~0ull : (1ull << here) - 1ull;
-      auto row_of = [&](int j) -> int { return tile_at(tile0 + ((OPT ? j >> 2 : j) << stride), OPT ? columns : 0) * kTileKeys; };   // first row of lane j's tile
+      auto row_of = [&](int j) -> int { return (int)row_at(tile0 + ((OPT ? j >> 2 : j) << stride), OPT ? columns : 0); };   // first row of lane j's tile, which the head has
       // place in the pool of the first rows of the tile's two halves
       auto half_a = [&](int j) -> long long {
         return ((long long)(int)lane_value((unsigned int)page_a, j) << shift) + (row_of(j) & page_mask);
