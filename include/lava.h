@@ -603,6 +603,8 @@ typedef struct lava_paged_compact_problem {
   int64_t capacity;             /* entries of kept_idx; survivors beyond it are not written        */
   const int32_t* block_table;   /* device [H_kv][max_blocks]: the sequence's rows of the table      */
   const int32_t* first_rows;    /* device [H_kv] or NULL: rows every head held before (NULL: none)  */
+  int32_t table_blocks;         /* entries a head has in block_table: the pool's max_blocks, any other
+                                   number is refused (LAVA_ERR_SHAPE); 0 leaves it unchecked        */
 } lava_paged_compact_problem;
 
 /*

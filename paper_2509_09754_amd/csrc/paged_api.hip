@@ -104,8 +104,10 @@ int32_t lava_compact_paged(const lava_layer_desc* desc, int32_t n_problems,
   for (int i = 0; i < n_problems; ++i) {
     const lava_paged_compact_problem& p = problems[i];
     if (p.k_src == nullptr || p.v_src == nullptr || p.head_offsets == nullptr || p.kept_idx == nullptr ||
-        p.block_table == nullptr || p.src_rows < 1 || p.capacity < 0 || !aligned16(p.k_src) || !aligned16(p.v_src))
+        p.block_table == nullptr || p.src_rows < 1 || p.capacity < 0 || !aligned16(p.k_src) || !aligned16(p.v_src) ||
+        p.table_blocks < 0)
       return LAVA_ERR_INVALID_ARG;
+    if (p.table_blocks != 0 && p.table_blocks != pool->max_blocks) return LAVA_ERR_SHAPE;
     if (p.capacity > (p.src_offsets ? p.src_rows : (int64_t)desc->n_kv_heads * p.src_rows)) return LAVA_ERR_BUDGET;
   }
   discard_stale_error();

@@ -772,14 +772,14 @@ class PagedCompactProblem(ctypes.Structure):
         ("src_rows", ctypes.c_int64), ("src_offsets", ctypes.c_void_p), ("k_src", ctypes.c_void_p),
         ("v_src", ctypes.c_void_p), ("pos_src", ctypes.c_void_p), ("head_offsets", ctypes.c_void_p),
         ("kept_idx", ctypes.c_void_p), ("capacity", ctypes.c_int64), ("block_table", ctypes.c_void_p),
-        ("first_rows", ctypes.c_void_p),
+        ("first_rows", ctypes.c_void_p), ("table_blocks", ctypes.c_int32),
     ]
 
 
 def paged_compact_problem(desc: LayerDesc, src_rows, k_src, v_src, head_offsets, kept_idx, capacity, block_table,
                           first_rows=None, src_offsets=None, pos_src=None) -> PagedCompactProblem:
     """One row of the table of lava_compact_paged (dense source when src_offsets is None); block_table: the sequence's
-    [H_kv, max_blocks].  The caller keeps the tensors."""
+    [H_kv, max_blocks], as many blocks as the pool's.  The caller keeps the tensors."""
     for name, t in (("k_src", k_src), ("v_src", v_src)):
         _dev(t, name, desc.torch_dtype)
     _dev(head_offsets, "head_offsets", torch.int64), _dev(kept_idx, "kept_idx", torch.int32)
@@ -789,11 +789,18 @@ def paged_compact_problem(desc: LayerDesc, src_rows, k_src, v_src, head_offsets,
             _dev(t, name, dt)
     if head_offsets.numel() != desc.n_kv_heads + 1 or kept_idx.numel() < int(capacity):
         raise ValueError("head_offsets must hold H_kv + 1 values and kept_idx `capacity` ones")
-    rows = int(src_rows) * (1 if src_offsets is not None else desc.n_kv_heads)
+    hkv = desc.n_kv_heads
+    rows = int(src_rows) * (1 if src_offsets is not None else hkv)
     if k_src.numel() != rows * desc.head_dim or v_src.numel() != rows * desc.head_dim:
         raise ValueError("k_src / v_src hold a different number of rows than src_rows")
+    for name, t, n in (("src_offsets", src_offsets, hkv + 1), ("pos_src", pos_src, rows), ("first_rows", first_rows, hkv)):
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name} must hold {n} values")
+    blocks = block_table.numel() // hkv
+    if blocks < 1 or block_table.numel() != blocks * hkv:
+        raise ValueError("block_table must be [H_kv, max_blocks]")
     return PagedCompactProblem(int(src_rows), _addr(src_offsets), _addr(k_src), _addr(v_src), _addr(pos_src),
-                               _addr(head_offsets), _addr(kept_idx), int(capacity), _addr(block_table), _addr(first_rows))
+                               _addr(head_offsets), _addr(kept_idx), int(capacity), _addr(block_table), _addr(first_rows), blocks)
 
 
 def lava_compact_paged(desc: LayerDesc, problems, pool: PagePool, stream=None) -> None:

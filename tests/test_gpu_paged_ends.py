@@ -54,3 +54,30 @@ def test_window_over_the_longest_head(lava, page, rows):
                                                   1 / math.sqrt(d), window=window, pos_pages=pos, q_pos=[q_pos])
     assert (np.abs(out.cpu().double().numpy() - want) <= tol).all()
     assert (np.abs(lse.cpu().double().numpy() - want_lse) <= tol_lse).all()
+
+
+def test_gather_refuses_tables_and_lists_of_other_sizes(lava):
+    """A pool made for appending knows no table width; a problem whose table, row counts, offsets or positions have another length than
+    the heads and the source is refused before anything is read."""
+    say("compact into pages: sizes that do not belong together")
+    z = lambda *s, dt=torch.int32: torch.zeros(*s, dtype=dt, device=DEV)
+    desc = lava.LayerDesc.make(4, 2, 64, 1, "f32")
+    kp = [z(8, 16, 64, dt=torch.float32) for _ in range(2)]
+    kv = [torch.ones(2, 10, 64, device=DEV) for _ in range(2)]
+    offs, idx = torch.tensor([0, 2, 4], device=DEV), z(4)
+    make = lambda table, **kw: lava.paged_compact_problem(desc, kw.pop("n", 10), *kv, offs, idx, 4, table, **kw)
+    table = torch.arange(8, dtype=torch.int32, device=DEV).view(2, 4)
+    for pool in (lava.PagePool(*kp), lava.PagePool(*kp, max_blocks=3), lava.PagePool(*kp, max_blocks=5)):
+        for problems in ([make(table)], (lava.PagedCompactProblem * 1)(make(table)), [make(z(2, pool.max_blocks)), make(table)]):
+            with pytest.raises(lava.LavaError):
+                lava.lava_compact_paged(desc, problems, pool)
+    for call in (lambda: make(z(2, 4)[:, :0]), lambda: make(z(7)), lambda: make(table, first_rows=z(1)), lambda: make(table, first_rows=z(4)),
+                 lambda: make(table, n=20, src_offsets=z(2, dt=torch.int64)), lambda: make(table, pos_src=z(10)),
+                 lambda: make(table, n=20, src_offsets=z(3, dt=torch.int64), pos_src=z(19))):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert not bool(kp[0].any()) and not bool(kp[1].any())
+    lava.lava_compact_paged(desc, [make(table, first_rows=z(2), pos_src=z(20))], lava.PagePool(*kp, max_blocks=4))
+    torch.cuda.synchronize()
+    assert bool((kp[0].view(8, 16, 64)[[0, 4], :2] == 1).all()) and int(kp[0].sum()) == 4 * 64
