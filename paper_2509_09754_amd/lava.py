@@ -201,6 +201,20 @@ def _stream(stream):
     return _raw_stream(_device_index())
 
 
+def _empty(*shape, dtype, device, stream) -> torch.Tensor:
+    """A buffer the call makes itself, a workspace or an output.  Its memory is the stream's the call is enqueued on, so that it is given to
+    nobody else before the call has run, whenever the binding lets go of it; the stream that is current (whose caller may read
+    an output) is noted as a user of it as well."""
+    if stream is None:
+        return torch.empty(*shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):            # anything that has a handle
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(*shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _lengths(seq_lens):
     """(C array of int64, number of sequences, their sum)."""
     if type(seq_lens) in (list, tuple) and all(type(n) is int and 0 <= n < 1 << 40 for n in seq_lens):
@@ -270,14 +284,14 @@ def lava_window_scores(desc: LayerDesc, seq_lens: Sequence[int], q_win: torch.Te
         if lse.numel() != batch * desc.n_q_heads * desc.window:
             raise ValueError("lse must be [batch, H, w]")
     if scores is None:
-        scores = torch.empty(total * desc.n_kv_heads, dtype=torch.float32, device=k.device)
+        scores = _empty(total * desc.n_kv_heads, dtype=torch.float32, device=k.device, stream=stream)
     if vbar is None:
-        vbar = torch.empty(batch, desc.n_kv_heads, dtype=torch.float32, device=k.device)
+        vbar = _empty(batch, desc.n_kv_heads, dtype=torch.float32, device=k.device, stream=stream)
     if layer_stat is None:
-        layer_stat = torch.empty(batch, dtype=torch.float32, device=k.device)
+        layer_stat = _empty(batch, dtype=torch.float32, device=k.device, stream=stream)
     if workspace is None:
         nbytes = lava_window_scores_workspace_bytes(desc, batch, total)
-        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=k.device)
+        workspace = _empty(max(nbytes, 256), dtype=torch.uint8, device=k.device, stream=stream)
     if budget_plan is not None:
         st = lib.lava_window_scores_planned(ctypes.byref(desc), batch, lens, _ptr(q_win),
                                             _ptr(k), _ptr(v), _ptr(lse), _ptr(scores), _ptr(vbar), _ptr(layer_stat),
@@ -323,7 +337,7 @@ def lava_layer_budgets(e, total, lo, hi, budgets=None, stream=None):
                             ("hi", hi, torch.int64)):
             _dev(t, name, dt)
         if budgets is None:
-            budgets = torch.empty(batch, L, dtype=torch.int64, device=e.device)
+            budgets = _empty(batch, L, dtype=torch.int64, device=e.device, stream=stream)
         st = lib.lava_layer_budgets(batch, L, _ptr(e), _ptr(total), _ptr(lo), _ptr(hi), _ptr(budgets), 1,
                                     _stream(stream))
         _check(st, "lava_layer_budgets")
@@ -358,15 +372,15 @@ def lava_select_topk(n_heads: int, scores: torch.Tensor, budget: int, seg_offset
     if budget_dev is not None:
         _dev(budget_dev, "budget_dev", torch.int64)
     if head_counts is None:
-        head_counts = torch.empty(n_heads, dtype=torch.int32, device=scores.device)
+        head_counts = _empty(n_heads, dtype=torch.int32, device=scores.device, stream=stream)
     if head_offsets is None:
-        head_offsets = torch.empty(n_heads + 1, dtype=torch.int64, device=scores.device)
+        head_offsets = _empty(n_heads + 1, dtype=torch.int64, device=scores.device, stream=stream)
     if kept_idx is None:
-        kept_idx = torch.empty(max(int(budget), 1), dtype=torch.int32, device=scores.device)
+        kept_idx = _empty(max(int(budget), 1), dtype=torch.int32, device=scores.device, stream=stream)
     if kept_scores is None and want_scores:
-        kept_scores = torch.empty(max(int(budget), 1), dtype=torch.float32, device=scores.device)
+        kept_scores = _empty(max(int(budget), 1), dtype=torch.float32, device=scores.device, stream=stream)
     if workspace is None:
-        workspace = torch.empty(max(lava_select_workspace_bytes(total), 256), dtype=torch.uint8, device=scores.device)
+        workspace = _empty(max(lava_select_workspace_bytes(total), 256), dtype=torch.uint8, device=scores.device, stream=stream)
     if primed:
         if seg_offsets is not None:
             raise ValueError("a prepared workspace serves equal segments only")
@@ -481,7 +495,7 @@ def lava_select_topk_batch(n_heads: int, problems, max_total_entries=None, works
     widest = max((p.total_entries for p in problems), default=0) if max_total_entries is None else int(max_total_entries)
     if workspace is None:
         need = lava_select_batch_workspace_bytes(len(problems), widest)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        workspace = _empty(max(need, 256), dtype=torch.uint8, device=device, stream=stream)
     st = lib.lava_select_topk_batch(int(n_heads), len(problems), ctypes.cast(table, ctypes.c_void_p), widest,
                                     _ptr(workspace), workspace.numel(), _stream(stream))
     _check(st, "lava_select_topk_batch")
@@ -506,9 +520,9 @@ def lava_compact_kv(desc: LayerDesc, n: int, k: torch.Tensor, v: torch.Tensor, h
     _dev(k, "k", desc.torch_dtype), _dev(v, "v", desc.torch_dtype)
     _dev(head_offsets, "head_offsets", torch.int64), _dev(kept_idx, "kept_idx", torch.int32)
     if k_out is None:
-        k_out = torch.empty(max(int(capacity), 1), desc.head_dim, dtype=desc.torch_dtype, device=k.device)
+        k_out = _empty(max(int(capacity), 1), desc.head_dim, dtype=desc.torch_dtype, device=k.device, stream=stream)
     if v_out is None:
-        v_out = torch.empty(max(int(capacity), 1), desc.head_dim, dtype=desc.torch_dtype, device=k.device)
+        v_out = _empty(max(int(capacity), 1), desc.head_dim, dtype=desc.torch_dtype, device=k.device, stream=stream)
     st = lib.lava_compact_kv(ctypes.byref(desc), int(n), _ptr(k), _ptr(v), _ptr(head_offsets), _ptr(kept_idx),
                              int(capacity), _ptr(k_out), _ptr(v_out), _stream(stream))
     _check(st, "lava_compact_kv")
@@ -526,11 +540,11 @@ def lava_compact_packed(desc: LayerDesc, src_offsets: torch.Tensor, k_src: torch
         _dev(pos_src, "pos_src", torch.int32)
     rows = max(int(capacity), 1)
     if k_out is None:
-        k_out = torch.empty(rows, desc.head_dim, dtype=desc.torch_dtype, device=k_src.device)
+        k_out = _empty(rows, desc.head_dim, dtype=desc.torch_dtype, device=k_src.device, stream=stream)
     if v_out is None:
-        v_out = torch.empty(rows, desc.head_dim, dtype=desc.torch_dtype, device=k_src.device)
+        v_out = _empty(rows, desc.head_dim, dtype=desc.torch_dtype, device=k_src.device, stream=stream)
     if pos_out is None:
-        pos_out = torch.empty(rows, dtype=torch.int32, device=k_src.device)
+        pos_out = _empty(rows, dtype=torch.int32, device=k_src.device, stream=stream)
     st = lib.lava_compact_packed(ctypes.byref(desc), _ptr(src_offsets), k_src.shape[0], _ptr(k_src), _ptr(v_src),
                                  _ptr(pos_src), _ptr(head_offsets), _ptr(kept_idx), int(capacity), _ptr(k_out),
                                  _ptr(v_out), _ptr(pos_out), _stream(stream))
@@ -620,7 +634,7 @@ def lava_cascade_step(desc: LayerDesc, layer: int, n: int, k_new: torch.Tensor, 
     _dev(scores_new, "scores_new", torch.float32)
     if workspace is None:
         need = lava_cascade_workspace_bytes(desc, n, state.n_layers, total_budget)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=k_new.device)
+        workspace = _empty(max(need, 256), dtype=torch.uint8, device=k_new.device, stream=stream)
     st = lib.lava_cascade_step(ctypes.byref(desc), int(layer), int(n), _ptr(k_new), _ptr(v_new), _ptr(scores_new),
                                _ptr(state.e), int(total_budget), ctypes.byref(state.c),
                                _ptr(state.budgets), _ptr(workspace), workspace.numel(), _stream(stream))
@@ -643,12 +657,12 @@ def lava_decode_attention(desc: LayerDesc, batch: int, q: torch.Tensor, k_hat, v
     if seq_base is not None:
         _dev(seq_base, "seq_base", torch.int64)
     if out is None:
-        out = torch.empty(batch, desc.n_q_heads, desc.head_dim, dtype=torch.float32, device=q.device)
+        out = _empty(batch, desc.n_q_heads, desc.head_dim, dtype=torch.float32, device=q.device, stream=stream)
     if lse is None:
-        lse = torch.empty(batch, desc.n_q_heads, dtype=torch.float32, device=q.device)
+        lse = _empty(batch, desc.n_q_heads, dtype=torch.float32, device=q.device, stream=stream)
     if workspace is None:
         need = lava_decode_workspace_bytes(desc, batch, rows_capacity, tail_len)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(need, 256), dtype=torch.uint8, device=q.device, stream=stream)
     st = lib.lava_decode_attention(ctypes.byref(desc), int(batch), _ptr(q), _ptr(k_hat), _ptr(v_hat),
                                    _ptr(head_offsets), _ptr(seq_base), int(rows_capacity), _ptr(k_tail),
                                    _ptr(v_tail), int(tail_len), int(tail_capacity), _ptr(out), _ptr(lse),
@@ -758,7 +772,7 @@ def lava_page_tables(state: PageState, n_new: Optional[torch.Tensor] = None, hea
         max_tokens = positions.numel()
     if workspace is None:
         need = lava_page_tables_workspace_bytes(state.batch, state.n_kv_heads)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=state.block_table.device)
+        workspace = _empty(max(need, 256), dtype=torch.uint8, device=state.block_table.device, stream=stream)
     st = lib.lava_page_tables(state._sizes_ref, state.batch, state.n_kv_heads, state._ref, _ptr(n_new), _ptr(head_counts),
                               _ptr(release), max_tokens, _ptr(slots), _ptr(positions), _ptr(workspace), workspace.numel(),
                               _stream(stream))
@@ -870,7 +884,7 @@ def lava_rotary(rot: RotaryDesc, turns: torch.Tensor, positions: torch.Tensor, x
     _here(x)
     _check_turns(rot, turns, positions, tokens)
     if out is None:
-        out = torch.empty(x.shape, dtype=dt, device=x.device)
+        out = _empty(x.shape, dtype=dt, device=x.device, stream=stream)
     if _rows_of_heads(out, "out", dt).shape != x.shape:
         raise ValueError("out must have the shape of x")
     st = lib.lava_rotary(ctypes.byref(rot), _ptr(turns), LAVA_BF16 if dt == torch.bfloat16 else LAVA_F32, d, tokens, heads,
@@ -893,7 +907,7 @@ def lava_rotary_append(desc: LayerDesc, rot: RotaryDesc, turns: torch.Tensor, po
     if q is not None:
         q_stride = _token_stride(q, "q", dt, (tokens, hq, d))
         if q_out is None:
-            q_out = torch.empty(tokens, hq, d, dtype=dt, device=q.device)
+            q_out = _empty(tokens, hq, d, dtype=dt, device=q.device, stream=stream)
         elif q_out.numel() != tokens * hq * d:
             raise ValueError("q_out must be [tokens, H, d_h]")
         elif q_out is not q:
@@ -944,14 +958,14 @@ def lava_paged_decode(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_ta
     if slopes is not None and slopes.numel() != desc.n_q_heads:
         raise ValueError("slopes must be [H]")
     if out is None:
-        out = torch.empty(batch, desc.n_q_heads, desc.head_dim, dtype=torch.float32, device=q.device)
+        out = _empty(batch, desc.n_q_heads, desc.head_dim, dtype=torch.float32, device=q.device, stream=stream)
     if lse is None:
-        lse = torch.empty(batch, desc.n_q_heads, dtype=torch.float32, device=q.device)
+        lse = _empty(batch, desc.n_q_heads, dtype=torch.float32, device=q.device, stream=stream)
     for name, t, n in (("out", out, q.numel()), ("lse", lse, batch * desc.n_q_heads)):
         if _dev(t, name, torch.float32).numel() != n:
             raise ValueError(f"{name} must hold {n} values")
     if workspace is None:
-        workspace = torch.empty(max(lava_paged_decode_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(lava_paged_decode_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device, stream=stream)
     st = lib.lava_paged_decode(ctypes.byref(desc), batch, _ptr(q), pool._ref, _ptr(block_table), _ptr(head_rows),
                                ctypes.byref(options) if options is not None else None, _ptr(q_pos), _ptr(out), _ptr(lse),
                                _ptr(workspace), workspace.numel(), _stream(stream))
@@ -990,7 +1004,7 @@ def evict_layer(desc: LayerDesc, n: int, q_win, k, v, budget: int, lse=None, str
     lava_select_topk_primed) instead of the plain pair; the results are the same."""
     ws = None
     if primed:
-        ws = torch.empty(max(lava_select_workspace_bytes(desc.n_kv_heads * n), 256), dtype=torch.uint8, device=k.device)
+        ws = _empty(max(lava_select_workspace_bytes(desc.n_kv_heads * n), 256), dtype=torch.uint8, device=k.device, stream=stream)
     scores, vbar, stat = lava_window_scores(desc, [n], q_win, k, v, lse=lse, stream=stream, select_workspace=ws)
     counts, offs, idx, kept_s = lava_select_topk(desc.n_kv_heads, scores, budget, stream=stream, workspace=ws,
                                                  primed=primed)
