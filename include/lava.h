@@ -600,7 +600,8 @@ typedef struct lava_paged_compact_problem {
   const int32_t* pos_src;       /* or NULL (the position is then the index itself)                 */
   const int64_t* head_offsets;
   const int32_t* kept_idx;
-  int64_t capacity;             /* entries of kept_idx; survivors beyond it are not written        */
+  int64_t capacity;             /* entries of kept_idx, which may be NULL if there are none; survivors
+                                   beyond it are not written                                       */
   const int32_t* block_table;   /* device [H_kv][max_blocks]: the sequence's rows of the table      */
   const int32_t* first_rows;    /* device [H_kv] or NULL: rows every head held before (NULL: none)  */
   int32_t table_blocks;         /* entries a head has in block_table: the pool's max_blocks, any other
@@ -651,7 +652,8 @@ int32_t lava_rotary_turns(const lava_rotary_desc* rot, uint64_t* turns);
  *              overlap is not.  Strides are multiples of 16 bytes
  *   transpose  non-zero: the transposed rotation, which is the gradient's way through it (the inverse, for
  *              magnitude 1)
- * dtype LAVA_F32 or LAVA_BF16, head_dim 64 or 128, n_heads <= 1024, n_tokens < 2^31; 32-bit arithmetic, rounded once.
+ * dtype LAVA_F32 or LAVA_BF16, head_dim 64 or 128, n_heads <= 1024, n_tokens < 2^31 (0: nothing is done, and the buffers
+ * may be NULL); 32-bit arithmetic, rounded once.
  */
 int32_t lava_rotary(const lava_rotary_desc* rot, const uint64_t* turns, int32_t dtype, int32_t head_dim,
                     int64_t n_tokens, int32_t n_heads, const int32_t* positions, const void* x,
@@ -669,7 +671,7 @@ int32_t lava_rotary(const lava_rotary_desc* rot, const uint64_t* turns, int32_t 
  *   slots          device int64 [n_tokens][H_kv] as written by lava_page_tables; a row whose slot is negative
  *                  or not in the pool is not written.  No two rows may have the same slot
  *   positions      device int32 [n_tokens]; a token with a negative one is left out altogether
- * n_tokens * H_kv < 2^31.
+ * n_tokens * H_kv < 2^31; without tokens nothing is done, and their buffers may be NULL.
  */
 int32_t lava_rotary_append(const lava_layer_desc* desc, const lava_rotary_desc* rot, const uint64_t* turns,
                            int64_t n_tokens, const int32_t* positions, const void* q, int64_t q_token_stride,

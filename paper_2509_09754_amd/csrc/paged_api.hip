@@ -103,7 +103,7 @@ int32_t lava_compact_paged(const lava_layer_desc* desc, int32_t n_problems,
   if (n_problems < 1 || problems == nullptr) return LAVA_ERR_INVALID_ARG;
   for (int i = 0; i < n_problems; ++i) {
     const lava_paged_compact_problem& p = problems[i];
-    if (p.k_src == nullptr || p.v_src == nullptr || p.head_offsets == nullptr || p.kept_idx == nullptr ||
+    if (p.k_src == nullptr || p.v_src == nullptr || p.head_offsets == nullptr || (p.kept_idx == nullptr && p.capacity > 0) ||
         p.block_table == nullptr || p.src_rows < 1 || p.capacity < 0 || !aligned16(p.k_src) || !aligned16(p.v_src) ||
         p.table_blocks < 0)
       return LAVA_ERR_INVALID_ARG;
@@ -146,8 +146,9 @@ int32_t lava_rotary(const lava_rotary_desc* rot, const uint64_t* turns, int32_t 
   if (head_dim != 64 && head_dim != 128) return LAVA_ERR_SHAPE;
   const int32_t st = check_rotary(rot, head_dim);
   if (st != LAVA_OK) return st;
-  if (turns == nullptr || positions == nullptr || x == nullptr || out == nullptr || n_tokens < 0 || n_heads < 1 ||
-      !aligned16(x) || !aligned16(out))
+  if (n_tokens < 0 || n_heads < 1) return LAVA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return LAVA_OK;                                 // empty buffers may have no address
+  if (turns == nullptr || positions == nullptr || x == nullptr || out == nullptr || !aligned16(x) || !aligned16(out))
     return LAVA_ERR_INVALID_ARG;
   const int64_t elem = dtype == LAVA_BF16 ? 2 : 4;
   if (!take_stride(&x_token_stride, n_tokens, elem) || !take_stride(&x_head_stride, n_heads, elem) ||
@@ -162,7 +163,6 @@ int32_t lava_rotary(const lava_rotary_desc* rot, const uint64_t* turns, int32_t 
   };
   if (!apart(out_head_stride, n_heads, out_token_stride, n_tokens) && !apart(out_token_stride, n_tokens, out_head_stride, n_heads))
     return LAVA_ERR_INVALID_ARG;
-  if (n_tokens == 0) return LAVA_OK;
   RotaryArgs a = {};
   a.turns = reinterpret_cast<const unsigned long long*>(turns);
   a.positions = positions;
@@ -190,8 +190,9 @@ int32_t lava_rotary_append(const lava_layer_desc* desc, const lava_rotary_desc* 
   if (st == LAVA_OK) st = check_rotary(rot, desc->head_dim);
   if (st == LAVA_OK) st = check_pool(pool, false);
   if (st != LAVA_OK) return st;
-  if (turns == nullptr || positions == nullptr || k == nullptr || v == nullptr || slots == nullptr || n_tokens < 0 ||
-      (q == nullptr) != (q_out == nullptr))
+  if (n_tokens < 0) return LAVA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return LAVA_OK;                                 // empty buffers may have no address
+  if (turns == nullptr || positions == nullptr || k == nullptr || v == nullptr || slots == nullptr || (q == nullptr) != (q_out == nullptr))
     return LAVA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return LAVA_ERR_INVALID_ARG;
   const int64_t elem = desc->dtype == LAVA_BF16 ? 2 : 4;
@@ -201,7 +202,6 @@ int32_t lava_rotary_append(const lava_layer_desc* desc, const lava_rotary_desc* 
     return LAVA_ERR_INVALID_ARG;
   if (q != nullptr && q == q_out && n_tokens > 1 && q_token_stride != q_row) return LAVA_ERR_INVALID_ARG;
   if (n_tokens >= ((int64_t)1 << 31) / desc->n_kv_heads) return LAVA_ERR_SHAPE;
-  if (n_tokens == 0) return LAVA_OK;
   RotaryArgs a = {};
   a.turns = reinterpret_cast<const unsigned long long*>(turns);
   a.positions = positions;

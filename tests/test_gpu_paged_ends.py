@@ -81,3 +81,26 @@ def test_gather_refuses_tables_and_lists_of_other_sizes(lava):
     lava.lava_compact_paged(desc, [make(table, first_rows=z(2), pos_src=z(20))], lava.PagePool(*kp, max_blocks=4))
     torch.cuda.synchronize()
     assert bool((kp[0].view(8, 16, 64)[[0, 4], :2] == 1).all()) and int(kp[0].sum()) == 4 * 64
+
+
+def test_steps_of_nothing(lava):
+    """No tokens, no survivors: tensors of no elements are accepted, nothing is written."""
+    say("paged cache: empty tensors")
+    desc, rot = lava.LayerDesc.make(4, 2, 64, 1, "bf16"), lava.RotaryDesc.make(64)
+    turns = lava.lava_rotary_turns(rot, DEV)
+    kp, vp = (torch.full((8, 16, 64), 3.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    none = lambda *s, dt=torch.bfloat16: torch.empty(*s, dtype=dt, device=DEV)
+    pos, slots = none(0, dt=torch.int32), none(0, 2, dt=torch.int64)
+    x = none(0, 8, 64)
+    assert lava.lava_rotary(rot, turns, pos, x).shape == (0, 8, 64)
+    q_out = lava.lava_rotary_append(desc, rot, turns, pos, x[:, :4], x[:, 4:6], x[:, 6:], lava.PagePool(kp, vp), slots)
+    assert q_out.shape == (0, 4, 64)
+    assert lava.lava_rotary_append(desc, rot, turns, pos, None, x[:, 4:6], x[:, 6:], lava.PagePool(kp, vp), slots) is None
+    st = lava.PageState.empty(2, 2, 4, 8, 16)
+    lava.lava_page_tables(st, torch.zeros(2, dtype=torch.int32, device=DEV), slots=slots, positions=pos)
+    k = torch.ones(2, 10, 64, dtype=torch.bfloat16, device=DEV)
+    table = torch.arange(8, dtype=torch.int32, device=DEV).view(2, 4)
+    offs = torch.tensor([0, 1, 2], device=DEV)                         # the capacity rules
+    lava.lava_compact_paged(desc, [lava.paged_compact_problem(desc, 10, k, k, offs, pos, 0, table)], lava.PagePool(kp, vp, max_blocks=4))
+    torch.cuda.synchronize()
+    assert bool((kp == 3.0).all()) and bool((vp == 3.0).all()) and int(st.n_free[0]) == 8 and int(st.error[0]) == 0

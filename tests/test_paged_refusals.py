@@ -21,3 +21,26 @@ def test_gather_takes_tables_of_the_pools_width_only(blocks, want):
     table = (lava.PagedCompactProblem * 2)(good, bad)
     got = lava.lib.lava_compact_paged(ctypes.byref(desc), 2, ctypes.byref(table), ctypes.byref(pool), None)
     assert got == (lava.LAVA_ERR_BUDGET if want is None else want)
+
+
+def test_no_tokens_need_no_buffers():
+    """Empty tensors have no address; a step without tokens is nothing all the same, but for what is wrong whatever the tokens."""
+    desc, rot = lava.LayerDesc.make(32, 8, 128, 32, "bf16"), lava.RotaryDesc.make(128)
+    pool = lava.PagePoolStruct(10, 32, 4, FAKE, FAKE, FAKE)
+    turn = lambda tokens, heads=8, r=rot: lava.lib.lava_rotary(ctypes.byref(r), FAKE, lava.LAVA_BF16, 128, tokens, heads, None, None, 1024, 128,
+                                                               None, 1024, 128, 0, None)
+    append = lambda tokens, p=pool: lava.lib.lava_rotary_append(ctypes.byref(desc), ctypes.byref(rot), FAKE, tokens, None, None, 4096, None, 1024,
+                                                                None, 1024, None, ctypes.byref(p), None, None)
+    assert turn(0) == lava.LAVA_OK and append(0) == lava.LAVA_OK
+    assert turn(1) == ARG and append(1) == ARG and turn(-1) == ARG and append(-1) == ARG
+    assert turn(0, heads=0) == ARG and turn(0, r=lava.RotaryDesc.make(130)) == SHAPE
+    assert append(0, lava.PagePoolStruct(10, 33, 4, FAKE, FAKE, FAKE)) == SHAPE
+
+
+def test_a_selection_of_nothing_needs_no_indices():
+    desc = lava.LayerDesc.make(32, 8, 128, 32, "bf16")
+    pool = lava.PagePoolStruct(10, 32, 4, FAKE, FAKE, FAKE)
+    call = lambda capacity: lava.lib.lava_compact_paged(
+        ctypes.byref(desc), 1, ctypes.byref(lava.PagedCompactProblem(100, None, FAKE, FAKE, None, FAKE, None, capacity, FAKE, None, 4)),
+        ctypes.byref(pool), None)
+    assert call(0) == lava.LAVA_OK and call(1) == ARG
