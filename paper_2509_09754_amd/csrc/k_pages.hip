@@ -481,6 +481,8 @@ __global__ void __launch_bounds__(256) page_return_kernel(const PageTablesArgs a
 constexpr int kSlotItems = 8;   // slots a thread writes: 4.5 million 4 19.9 us, 8 18.7, 16 20.6; 2.6 million one 21.4, 8 14.0; 0.6 million 10.4 with both
 // One workgroup finishes a step of so few places (slots, and table entries that may change hands) sooner than two launches begin:
 // 2560 slots 8.1 us (two launches 8.6), 3840 8.9 (8.6), 16000 15.4 (8.6); 512 heads that take a page now and then 6.8 (8.7).
+// Where a table may fill by any number of pages it is the table that counts, whatever happens then: without maps 8 heads that take 4096
+// pages each 479 us (two launches 7.4), 2048 heads that take 63 each 150 (7.5), 512 that take a page now and then 5.0 (7.2).
 constexpr long long kOnePlaces = 2560;
 template <int ITEMS>
 __global__ void __launch_bounds__(256) page_fill_kernel(const PageTablesArgs a, const int chunk, const int head_wgs) {
@@ -513,8 +515,9 @@ size_t page_tables_bytes(int32_t batch, int32_t n_kv_heads) { return plan_layout
 int32_t launch_page_tables(const PageTablesArgs& a, hipStream_t s) {
   const long long heads = (long long)a.batch * a.heads, places = a.max_tokens * a.heads;
   // Written by the one workgroup alone: every slot, a count per head and, where heads take or give back any number of pages, up
-  // to the whole table.
-  const long long pages = a.head_counts != nullptr || a.release != nullptr ? heads * a.max_blocks : 0;
+  // to the whole table.  Tokens with maps cannot take more than the maps have room for; without maps nothing else bounds them.
+  const bool unbounded = a.head_counts != nullptr || a.release != nullptr || (a.n_new != nullptr && a.max_tokens == 0);
+  const long long pages = unbounded ? heads * a.max_blocks : 0;
   const bool one = heads <= kOneHeads && places + pages <= kOnePlaces;
   if (one) {
     ProfScope ps(KID_PAGE_PLAN, s);
