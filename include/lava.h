@@ -575,7 +575,8 @@ size_t lava_page_tables_workspace_bytes(int32_t batch, int32_t n_kv_heads);
  *                step without rows at position 0 (the place can be given to a new sequence at once)
  *   max_tokens   entries of slots and positions; 0 (and both NULL) with head_counts
  *   slots        device int64 [max_tokens][H_kv] or NULL: slot of every new row.  Tokens are numbered
- *                through the sequences, n_new[0] of the first one first; entries behind the last are -1
+ *                through the sequences without gaps, n_new[0] of the first one first: sequence b's are
+ *                rows n_new[0] + .. + n_new[b - 1] on.  Entries behind the last are -1
  *   positions    device int32 [max_tokens] or NULL: position of every new token, -1 behind the last
  *
  * New pages are taken from the top of the stack in order of (sequence, head, block); a head's row
@@ -692,7 +693,10 @@ size_t lava_paged_decode_workspace_bytes(const lava_layer_desc* desc);
  * Attention of ONE new token per sequence over the pages of its heads:
  *   out[h] = Softmax(z[h]) V_g,  g = h / G, over the head_rows[b][g] rows that head g of sequence b holds.
  *
- *   q            device [batch][H][d_h], dtype of the descriptor
+ *   q            device [batch][H][d_h], dtype of the descriptor: a row for every sequence.  Where some
+ *                sequences see no token in a step (n_new[b] = 0), the rows that lava_rotary_append wrote
+ *                are fewer and lie closer: the caller moves row n_new[0] + .. + n_new[b] - 1 to row b
+ *                (an idle sequence may have any row; its output says nothing)
  *   pool         k, v; pos is read if the options have a window or slopes (INVALID_ARG if it is NULL or not
  *                16-byte aligned then)
  *   block_table  device int32 [batch][H_kv][max_blocks]; only the entries of rows that are held are read

@@ -942,7 +942,8 @@ def lava_paged_decode(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_ta
                       options: Optional[DecodeOptions] = None, q_pos: Optional[torch.Tensor] = None, out=None, lse=None,
                       workspace=None, stream=None):
     """One new token per sequence, q [batch, H, d_h], attends to the pages of its heads; block_table
-    [batch, H_kv, pool.max_blocks], head_rows [batch, H_kv], q_pos [batch] int32.  Returns (out, lse)."""
+    [batch, H_kv, pool.max_blocks], head_rows [batch, H_kv], q_pos [batch] int32.  Returns (out, lse).  Where n_new of the step is zero for some
+    sequences, q is q_out.index_select(0, (n_new.cumsum(0) - 1).clamp(min=0)) of lava_rotary_append's."""
     _dev(q, "q", desc.torch_dtype), _dev(block_table, "block_table", torch.int32), _dev(head_rows, "head_rows", torch.int32)
     _here(q)
     batch = q.numel() // (desc.n_q_heads * desc.head_dim)

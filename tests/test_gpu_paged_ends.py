@@ -104,3 +104,70 @@ def test_steps_of_nothing(lava):
     lava.lava_compact_paged(desc, [lava.paged_compact_problem(desc, 10, k, k, offs, pos, 0, table)], lava.PagePool(kp, vp, max_blocks=4))
     torch.cuda.synchronize()
     assert bool((kp == 3.0).all()) and bool((vp == 3.0).all()) and int(st.n_free[0]) == 8 and int(st.error[0]) == 0
+
+
+def test_idle_sequences_between_others(lava):
+    """A captured step in which any of the sequences may see no token: slots number the tokens without gaps, and the queries are moved to
+    their sequences' rows as the documentation says.  Every replay against the oracle."""
+    say("paged cache: idle sequences")
+    H, Hkv, d, page, batch, mb = 4, 2, 64, 16, 4, 3
+    desc, rot = lava.LayerDesc.make(H, Hkv, d, 1, "f32"), lava.RotaryDesc.make(d)
+    turns = lava.lava_rotary_turns(rot, DEV)
+    st = lava.PageState.empty(batch, Hkv, mb, batch * Hkv * mb, page)
+    kp, vp = (torch.zeros(batch * Hkv * mb, page, d, device=DEV) for _ in range(2))
+    pool = lava.PagePool(kp, vp, max_blocks=mb)
+    new = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    x = torch.zeros(batch, H + 2 * Hkv, d, device=DEV)
+    slots, pos = torch.zeros(batch, Hkv, dtype=torch.int64, device=DEV), torch.zeros(batch, dtype=torch.int32, device=DEV)
+    q_out, out, lse = torch.zeros(batch, H, d, device=DEV), torch.zeros(batch, H, d, device=DEV), torch.zeros(batch, H, device=DEV)
+    tws, dws = (torch.zeros(n, dtype=torch.uint8, device=DEV) for n in (lava.lava_page_tables_workspace_bytes(batch, Hkv),
+                                                                        lava.lava_paged_decode_workspace_bytes(desc)))
+
+    def step():
+        lava.lava_page_tables(st, new, slots=slots, positions=pos, workspace=tws)
+        lava.lava_rotary_append(desc, rot, turns, pos, x[:, :H], x[:, H: H + Hkv], x[:, H + Hkv:], pool, slots, q_out=q_out)
+        q = q_out.index_select(0, (new.cumsum(0) - 1).clamp(min=0))
+        lava.lava_paged_decode(desc, q, pool, st.block_table, st.head_rows, out=out, lse=lse, workspace=dws)
+
+    snapshot = [t.clone() for t in (st.block_table, st.head_rows, st.seq_pos, st.free_pages, st.n_free)]
+    step()                                                           # no tokens: warms up torch's own calls
+    torch.cuda.synchronize()
+    for t, s in zip((st.block_table, st.head_rows, st.seq_pos, st.free_pages, st.n_free), snapshot):
+        assert torch.equal(t, s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    rng = np.random.default_rng(3)
+    f = P.rotary_frequencies(d)
+    held = [[[] for _ in range(Hkv)] for _ in range(batch)]            # (key, value) of every head, as turned in 64 bits
+    seen = [0] * batch
+    patterns = [[1, 0, 1, 1], [0, 1, 0, 0], [0, 0, 0, 0], [0, 0, 0, 1], [1, 1, 1, 1], [1, 0, 0, 1], [0, 1, 1, 0]] * 3
+    for i, n in enumerate(patterns):
+        xs = rng.standard_normal((batch, H + 2 * Hkv, d)).astype(np.float32)
+        x.copy_(dev(xs)), new.copy_(dev(np.array(n, np.int32)))
+        graph.replay() if i % 4 else step()
+        torch.cuda.synchronize()
+        assert int(st.error[0]) == 0
+        row = 0
+        q64 = np.zeros((batch, H, d))
+        for b in range(batch):
+            if not n[b]:
+                continue
+            turned = P.rotary(xs[row: row + 1].astype(np.float64), [seen[b]], f)[0]
+            q64[b] = turned[:H]
+            for g in range(Hkv):
+                held[b][g].append((turned[H + g], xs[row, H + Hkv + g].astype(np.float64)))
+            seen[b] += 1
+            row += 1
+        rows = np.array([[len(h) for h in hb] for hb in held], np.int32)
+        assert np.array_equal(st.head_rows.cpu().numpy(), rows) and st.seq_pos.cpu().tolist() == seen
+        k64, v64 = (np.array([np.pad(np.array([r[j] for r in h]).reshape(len(h), d), ((0, 64 - len(h)), (0, 0))) for hb in held for h in hb])
+                    for j in range(2))
+        want, _, tol, _ = P.paged_decode(q64, k64, v64, np.arange(batch * Hkv).reshape(batch, Hkv, 1), rows, 1 / math.sqrt(d))
+        # queries and keys are within 2^-20 of the turned values here (two products of values below 6 with 2^-22 sines, rounded): a
+        # logit, of 64 products of size up to 6, over 8, within 2 * 64 * 6 * 2^-20 / 8 = 2^-13.4; twice that in a weight, times |v| < 6
+        tol = tol + 2.0 ** -12.4 * 6
+        busy = np.array(n, bool)
+        assert (np.abs(out.cpu().double().numpy() - want)[busy] <= tol[busy]).all()
+        wrong = P.paged_decode(q64[::-1], k64, v64, np.arange(batch * Hkv).reshape(batch, Hkv, 1), rows, 1 / math.sqrt(d))[0]
+        assert i < 5 or not busy.any() or (np.abs(wrong - want)[busy].max() > tol[busy].max())   # another row's query would be seen
