@@ -681,7 +681,7 @@ int32_t lava_rotary_append(const lava_layer_desc* desc, const lava_rotary_desc* 
 
 /* How lava_paged_decode changes logits, z = scale * <q, k> at first.  All zero: not at all. */
 typedef struct lava_decode_options {
-  float softcap;               /* > 0: z <- softcap * tanh(z / softcap)                                  */
+  float softcap;               /* 1e-30 .. 1e30: z <- softcap * tanh(z / softcap); others but 0 are refused */
   int32_t window;              /* > 0: only rows at positions q_pos - window + 1 .. q_pos count           */
   const float* slopes;         /* device [H] or NULL: z <- z - slopes[h] * (q_pos - position of the row)  */
 } lava_decode_options;

@@ -247,7 +247,8 @@ int32_t lava_paged_decode(const lava_layer_desc* desc, int32_t batch, const void
     return LAVA_ERR_INVALID_ARG;
   lava_decode_options o = {};
   if (options != nullptr) o = *options;
-  if (!(o.softcap >= 0.0f) || o.softcap > 1e30f || o.window < 0) return LAVA_ERR_INVALID_ARG;
+  // the kernel multiplies by the cap's reciprocal, which has to be finite: a logit of zero would give NaN
+  if (!(o.softcap >= 0.0f) || o.softcap > 1e30f || (o.softcap > 0.0f && o.softcap < 1e-30f) || o.window < 0) return LAVA_ERR_INVALID_ARG;
   const bool needs_pos = o.window > 0 || o.slopes != nullptr;
   if (needs_pos && (q_pos == nullptr || pool->pos == nullptr || !aligned16(pool->pos))) return LAVA_ERR_INVALID_ARG;
   if (batch > 65535 || (int64_t)batch * d.n_kv_heads > 65536) return LAVA_ERR_SHAPE;

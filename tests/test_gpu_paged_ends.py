@@ -171,3 +171,21 @@ def test_idle_sequences_between_others(lava):
         assert (np.abs(out.cpu().double().numpy() - want)[busy] <= tol[busy]).all()
         wrong = P.paged_decode(q64[::-1], k64, v64, np.arange(batch * Hkv).reshape(batch, Hkv, 1), rows, 1 / math.sqrt(d))[0]
         assert i < 5 or not busy.any() or (np.abs(wrong - want)[busy].max() > tol[busy].max())   # another row's query would be seen
+
+
+@pytest.mark.parametrize("cap", [1e-30, 1e-6, 1e30])
+def test_caps_at_the_ends(lava, cap):
+    """The smallest cap makes every row weigh the same, zeros among the logits included; the largest changes nothing."""
+    say(f"paged decode: cap {cap}")
+    rng = np.random.default_rng(4)
+    desc = lava.LayerDesc.make(4, 2, 64, 1, "f32")
+    k, v, q = (rng.standard_normal(s).astype(np.float32) for s in ((6, 16, 64), (6, 16, 64), (1, 4, 64)))
+    q[0, 1] = 0.0
+    table, rows = np.arange(6, dtype=np.int32).reshape(1, 2, 3), np.array([[40, 17]], np.int32)
+    pool = lava.PagePool(dev(k), dev(v), max_blocks=3)
+    out, lse = lava.lava_paged_decode(desc, dev(q), pool, dev(table), dev(rows), lava.DecodeOptions.make(softcap=cap))
+    want, want_lse, tol, tol_lse = P.paged_decode(*(x.astype(np.float64) for x in (q, k, v)), table, rows, 0.125, softcap=0.0 if cap > 1 else cap)
+    # near zero the cap's series is relative: z (1 + 2^-20); the oracle counts 2^-20 of the cap, which says nothing for a large one
+    slack = 2.0 ** -19 * 8 * 6 if cap > 1 else 0.0                     # logits below 8, values below 6
+    assert (np.abs(out.cpu().double().numpy() - want) <= tol + slack).all()
+    assert (np.abs(lse.cpu().double().numpy() - want_lse) <= tol_lse + slack).all()

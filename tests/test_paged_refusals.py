@@ -44,3 +44,13 @@ def test_a_selection_of_nothing_needs_no_indices():
         ctypes.byref(desc), 1, ctypes.byref(lava.PagedCompactProblem(100, None, FAKE, FAKE, None, FAKE, None, capacity, FAKE, None, 4)),
         ctypes.byref(pool), None)
     assert call(0) == lava.LAVA_OK and call(1) == ARG
+
+
+@pytest.mark.parametrize("cap,refused", [(1e-40, True), (1e-39, True), (9e-31, True), (2e30, True), (float("inf"), True), (1e-30, False), (1e30, False),
+                                         (0.0, False)])
+def test_caps_have_a_reciprocal(cap, refused):
+    """A cap whose reciprocal overflows would make NaN of a logit of zero.  Without a workspace nothing is launched."""
+    desc = lava.LayerDesc.make(32, 8, 128, 32, "bf16")
+    pool, options = lava.PagePoolStruct(10, 32, 4, FAKE, FAKE, FAKE), lava.DecodeOptions(cap, 0, None)
+    got = lava.lib.lava_paged_decode(ctypes.byref(desc), 1, FAKE, ctypes.byref(pool), FAKE, FAKE, ctypes.byref(options), None, FAKE, FAKE, None, 0, None)
+    assert got == (ARG if refused else lava.LAVA_ERR_WORKSPACE)
