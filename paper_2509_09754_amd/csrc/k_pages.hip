@@ -6,11 +6,11 @@
 // new block gets is one look-up in the stack, which slot a new row has is one look-up in the stack or the table.
 //
 // A step with little to write, as a decode step is, is one launch of one workgroup: a chain of four trips to memory (64 sequences on
-// 8 heads 7.0 us with the host's share).  For a large one a first launch forms the sums, a workgroup for every 1024 heads, and every
+// 8 heads 6.0 us with the host's share).  For a large one a first launch forms the sums, a workgroup for every 1024 heads, and every
 // workgroup of the second adds up the workgroups' totals for itself; that launch fills the device and is bound by the slots it
-// writes, 8 bytes a row (559 thousand tokens on 8 heads, 36 MB of slots: 17.9 us both launches, 8.3 at a copy's rate; a third
+// writes, 8 bytes a row (559 thousand tokens on 8 heads, 36 MB of slots: 17.1 us both launches, 8.3 at a copy's rate; a fifth
 // of it is the first launch, the rest four dependent trips to memory around the writes).  Sequences that leave cost a launch
-// between the two, which puts their pages on the stack before any is taken (16384 heads, a quarter leaving: 19.6 us).
+// between the two, which puts their pages on the stack before any is taken (16384 heads, a quarter leaving: 18.5 us).
 #include "common.h"
 #include "decode_parts.h"
 
@@ -199,7 +199,8 @@ __device__ __forceinline__ void fill_slots(const PageTablesArgs& a, const PlanSu
 }
 
 // The same for the 256 * ITEMS places from place e0 on, by a workgroup of 256 threads.  Where all of them are tokens of one sequence, as
-// most of a prompt's are, a thread stays with its head and its look-ups are independent of each other.
+// most of a prompt's are, a thread stays with its head and its look-ups are independent of each other; that takes a head count that
+// divides 256 (16 prompts on 8 heads 17 us both launches, on 10 and 12 heads, place by place, 31 and 32.5).
 template <int ITEMS>
 __device__ __forceinline__ void fill_slots_wide(const PageTablesArgs& a, const PlanSums& w, int top, int tokens, unsigned int e0) {
   const unsigned int all = (unsigned int)(a.max_tokens * a.heads), heads = (unsigned int)a.heads;

@@ -91,7 +91,7 @@ __device__ __forceinline__ void turn_neighbours(u32x4& a, u32x4& b, const float2
 }
 
 // Halves whose length is no multiple of a chunk: value by value, pair p by whoever has unit p / E, the values behind the
-// rotated part spread over the units.
+// rotated part spread over the units.  8197 tokens of 32 + 2 x 8 heads, 38 values of 128 turned: 130 us, where whole chunks take 40.
 template <int DT, int D>
 __device__ __forceinline__ void turn_values(const char* src, char* dst, int j, int rot, const float2* cs) {
   constexpr int E = 16 / Elem<DT>::kBytes, kUnits = D / E / 2;
