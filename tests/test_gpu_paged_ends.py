@@ -189,3 +189,52 @@ def test_caps_at_the_ends(lava, cap):
     slack = 2.0 ** -19 * 8 * 6 if cap > 1 else 0.0                     # logits below 8, values below 6
     assert (np.abs(out.cpu().double().numpy() - want) <= tol + slack).all()
     assert (np.abs(lse.cpu().double().numpy() - want_lse) <= tol_lse + slack).all()
+
+
+def test_tables_of_as_many_heads_as_there_may_be(lava):
+    """2^20 heads: every chunk of the sums is full.  One token for a few sequences, a few that leave."""
+    say("tables: 2^20 heads")
+    rng = np.random.default_rng(61)
+    batch, heads, page, mb = 16384, 64, 16, 1
+    n_pages = batch * heads
+    rows = rng.integers(0, 2, (batch, heads)).astype(np.int32) * rng.integers(1, 15, (batch, 1)).astype(np.int32)
+    order = rng.permutation(n_pages).astype(np.int32)
+    held = int((rows > 0).sum())
+    table = np.full((batch, heads, mb), -7, np.int32)
+    table[..., 0][rows > 0] = order[:held]
+    free = np.full(n_pages, -9, np.int32)
+    free[: n_pages - held] = order[held:]
+    pos = rng.integers(0, 50, batch).astype(np.int32)
+    new, release = (rng.random(batch) < 0.01).astype(np.int32), (rng.random(batch) < 0.02).astype(np.int32)
+    new[-1] = release[-1] = 1
+    tokens = int(new.sum()) + 1
+    want = P.page_tables(page, n_pages, table, rows, pos, free, n_pages - held, new, None, release, tokens)
+    assert want[7] == 0
+    st = lava.PageState(*(dev(a) for a in (table, rows, pos, free, np.array([n_pages - held], np.int32))), page)
+    slots, positions = torch.zeros(tokens, heads, dtype=torch.int64, device=DEV), torch.zeros(tokens, dtype=torch.int32, device=DEV)
+    lava.lava_page_tables(st, dev(new), release=dev(release), slots=slots, positions=positions)
+    torch.cuda.synchronize()
+    for got, a in zip((st.block_table, st.head_rows, st.seq_pos, st.free_pages, st.n_free, slots, positions), want[:4] + (want[4:5],) + want[5:7]):
+        assert np.array_equal(got.cpu().numpy(), np.asarray(a))
+
+
+def test_decode_of_as_many_heads_as_there_may_be(lava):
+    """65536 heads, most of them of a row or two, one long."""
+    from oracle.paged_counts import SCALE, Pages
+    say("paged decode: 65536 heads")
+    batch, Hkv, page, d = 8192, 8, 16, 64
+    rng = np.random.default_rng(62)
+    rows = rng.integers(0, 40, (batch, Hkv)).astype(np.int32)
+    for longest in (40, 3000):
+        rows[batch // 2, 3] = rows[-1, -1] = longest
+        blocks = -(-int(rows.max()) // page)
+        pages = Pages(longest, 300, page, d, device=DEV)
+        table = torch.randint(0, 300, (batch, Hkv, blocks), device=DEV, dtype=torch.int32)
+        desc = lava.LayerDesc.make(2 * Hkv, Hkv, d, 1, "bf16", softmax_scale=SCALE)
+        pool = lava.PagePool(pages.k.bfloat16(), pages.v.bfloat16(), max_blocks=blocks)
+        out, lse = lava.lava_paged_decode(desc, pages.queries(batch, 2 * Hkv, 2).bfloat16(), pool, table, dev(rows))
+        want, want_lse, tol, tol_lse = pages.attend(table, rows, 2)
+        torch.cuda.synchronize()
+        some = torch.isfinite(want_lse)
+        assert bool((torch.isfinite(lse) == some).all())
+        assert bool(((out.double() - want).abs() <= tol).all()) and bool(((lse.double() - want_lse).abs() <= tol_lse)[some].all())

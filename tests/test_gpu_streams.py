@@ -124,3 +124,29 @@ def test_the_current_stream_allocates_while_the_call_waits(lava, name):
     assert len(got) == len(want) and len(junk) == 48
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("name", ["lava_paged_decode", "evict_layer", "lava_decode_attention", "lava_rotary"])
+def test_a_call_on_a_joined_stream_is_captured(lava, name):
+    """A call without buffers on a side stream inside a capture: its buffers are the graph's, replays and eager work between them agree."""
+    print(name, flush=True)
+    keep, calls = make(lava)
+    want = [t.clone() for t in flat(calls[name](None))]
+    side = torch.cuda.Stream()
+    calls[name](side)                                                # the side stream has memory of its own to begin with
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = flat(calls[name](side))
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(4):
+        for t in got:
+            t.fill_(1)
+        graph.replay()
+        junk = [torch.full((1 << s,), 0xFF, dtype=torch.uint8, device=DEV) for s in range(8, 24)]
+        eager = flat(calls[name](None))
+        torch.cuda.synchronize()
+        assert len(junk) == 16
+        for a, b, c in zip(got, want, eager):
+            assert torch.equal(a, b) and torch.equal(c, b)
