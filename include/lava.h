@@ -17,7 +17,8 @@
  * selections / compactions in one launch each (the sequences of a ragged batch, the layers of a
  * stack), and lava_cascade_step is Algorithm 2 as a driver over a stack's compressed caches.
  * lava_page_tables, lava_compact_paged, lava_rotary_append and lava_paged_decode keep compressed caches
- * in pages, for sequences that come, grow and leave.
+ * in pages, for sequences that come, grow and leave; lava_beam_step, lava_page_fork, lava_page_compact and
+ * lava_shared_decode let sequences that begin alike share pages.
  *
  * Conventions common to all calls
  *   - "device" pointers are HIP device memory of the current device, "host" pointers are
@@ -716,6 +717,116 @@ int32_t lava_paged_decode(const lava_layer_desc* desc, int32_t batch, const void
                           const int32_t* block_table, const int32_t* head_rows, const lava_decode_options* options,
                           const int32_t* q_pos, float* out, float* lse, void* workspace, size_t workspace_bytes,
                           void* hip_stream);
+
+/*
+ * ------------------------------------------------------------------------------------------
+ * Sequences that begin alike: beams, samples of one prompt, a common system prompt.  Their pages are shared:
+ *   a page that is full may be in the block tables of several sequences (of one head each, and of no head twice);
+ *   a page that is not full, a head's last one, belongs to one sequence alone.
+ * New rows only ever go to pages that are not full or fresh, so lava_page_tables with new tokens or survivors,
+ * lava_compact_paged behind the rows a head holds, lava_rotary_append and lava_paged_decode know nothing of sharing.  Who holds a
+ * page is not counted anywhere: it is read from the tables, by the calls that need it.  All sequences that hold pages of
+ * a pool have to be in the state that such a call is given.  `release` of lava_page_tables gives pages back whoever else holds
+ * them: where pages are shared, sequences end by lava_page_fork with source -1.
+ */
+
+/* Bytes of device workspace lava_beam_step needs; 0 for invalid arguments. */
+size_t lava_beam_step_workspace_bytes(int32_t batch, int32_t beams, int64_t vocab, int32_t n_out);
+
+/*
+ * One step of beam search: of each group of beams the best n_out continuations.
+ *   Beam i with score s_i and logits x_i goes on with token v at  c = s_i + (x_i[v] - log sum_u exp(x_i[u])).
+ *   A beam that is done has one continuation: pad_token, at its score.
+ *   One candidate comes before another if its c is larger; if the beam's number is smaller; if, of one beam, the
+ *   logit is larger; if the token's number is smaller.  c is formed in 64 bits.
+ *
+ *   dtype        LAVA_F32 or LAVA_BF16, of the logits
+ *   logits       device, row b * beams + i at element (b * beams + i) * logit_stride, vocab values one after another;
+ *                aligned to their size only.  -inf is a token that cannot follow
+ *   scores       device float [batch][beams].  A beam whose score is not finite has no continuation (at the first step
+ *                all beams but one of a group that starts from one prompt: -inf)
+ *   done         device int32 [batch][beams] or NULL (none is): non-zero, the beam is over.  Its logits are not read
+ *   end_token    a continuation with it is done from now on; negative: there is none
+ *   pad_token    0 <= pad_token < vocab
+ *   parents      device int32 [batch][n_out]   row of the beam that goes on, b * beams + i: `source` of lava_page_fork
+ *   tokens       device int32 [batch][n_out]
+ *   scores_out   device float [batch][n_out]   c, rounded once; may be `scores` itself where n_out = beams
+ *   done_out     device int32 [batch][n_out] or NULL; may be `done` itself where n_out = beams
+ *   sources      device int32 [n_tables][batch * n_out] or NULL (n_tables 0): parents + t * batch * beams (a parent of -1 stays),
+ *                the `source` of a state that holds n_tables layers as sequences of their own
+ * Sorted, the best first.  A place without a candidate gets parent -1, token -1, score -inf, done 1.  A beam with a NaN or +inf
+ * among its logits, or with nothing but -inf, has no continuation.
+ * beams, n_out <= 64, vocab < 2^31, batch <= 65535, n_tables <= 1024, batch * beams * ceil(vocab / 8192) < 2^31,
+ * n_tables * batch * max(beams, n_out) < 2^31.  The same inputs give the same outputs bit for bit, and beams with the
+ * same logits and scores the same candidates.
+ */
+int32_t lava_beam_step(int32_t dtype, int32_t batch, int32_t beams, int64_t vocab, const void* logits, int64_t logit_stride,
+                       const float* scores, const int32_t* done, int32_t end_token, int32_t pad_token, int32_t n_out,
+                       int32_t* parents, int32_t* tokens, float* scores_out, int32_t* done_out, int32_t* sources, int32_t n_tables,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of device workspace lava_page_fork and lava_page_compact need; 0 for invalid arguments. */
+size_t lava_page_fork_workspace_bytes(int32_t batch, int32_t n_kv_heads, int32_t max_blocks, int64_t n_pages);
+
+/*
+ * Sequence b becomes what sequence source[b] was: copies, reorderings, ends of sequences in one call.
+ *
+ *   pool             sizes, and the pages whose rows are copied (positions too if the pool has them)
+ *   state            as for lava_page_tables; the new counts go to its *_out buffers, each of which may be the buffer itself
+ *   source           device int32 [batch], -1 .. batch - 1; -1: the sequence is empty from now on, at position 0
+ *   block_table_out  device int32 [batch][H_kv][max_blocks] or NULL: the new tables; NULL: state's own are changed
+ *   free_pages_out   device int32 [n_pages] or NULL: the new stack; NULL: state's own is changed
+ *
+ * Full pages are shared.  The last page of a head, if it is not full, goes on with one of the copies: sequence source[b] itself if it is
+ * its own source, else the first; every other copy gets a fresh page, into which the rows are copied.  Fresh pages are
+ * taken from the top of the stack in order of (sequence, head, block).  Then the pages that are in no table any more go
+ * back, in the order in which the old tables first named them.  Entries of a table behind a head's last page, and of a stack behind
+ * the last free page, are not written.  The state after it may be used at once; nothing is read back.
+ * A call that cannot be carried out changes nothing (separate outputs receive what there was) and sets its bits in
+ * state->error: LAVA_PAGES_EXHAUSTED, or LAVA_PAGES_INVALID for a source, a row count, n_free, a page in use or one to
+ * be taken that is out of range, or more pages given back than the stack can hold.
+ * Limits as for lava_page_tables, and batch * H_kv * max_blocks < 2^31.  The same inputs give the same outputs bit for bit.
+ */
+int32_t lava_page_fork(const lava_layer_desc* desc, const lava_page_pool* pool, int32_t batch, const lava_page_state* state,
+                       const int32_t* source, int32_t* block_table_out, int32_t* free_pages_out, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Heads keep some of the rows that they hold in pages: a cache that has grown is evicted again, tokens that were tried are taken back.
+ *
+ *   head_counts    device int32 [batch][H_kv]      rows every head keeps, as written by lava_select_topk
+ *   kept_idx       device int32 [batch][kept_capacity]  of sequence b the rows that its heads keep, ascending in each head,
+ *                  heads one after another without gaps, as written by lava_select_topk; rows that a head does not hold leave
+ *                  their places unwritten
+ *   evict          device int32 [batch] or NULL (all): 0, the sequence stays as it is and its counts and list are not read
+ * Leading pages all of whose rows stay where they are stay in the table, shared or not (of a last one that is not full: if it was
+ * the head's last before); the rows behind go to fresh pages, and pages that are in no table any more go back.  seq_pos stays as it is.  Pages are
+ * taken before any go back: the stack has to hold as many as the call fills.  Everything else as for lava_page_fork; counts that
+ * are negative, more than a head holds or together more than kept_capacity are LAVA_PAGES_INVALID.
+ */
+int32_t lava_page_compact(const lava_layer_desc* desc, const lava_page_pool* pool, int32_t batch, const lava_page_state* state,
+                          const int32_t* head_counts, const int32_t* kept_idx, int64_t kept_capacity, const int32_t* evict,
+                          int32_t* block_table_out, int32_t* free_pages_out, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
+
+/* Bytes of device workspace lava_shared_decode needs for pools with that many blocks a table; 0 for invalid arguments. */
+size_t lava_shared_decode_workspace_bytes(const lava_layer_desc* desc, int32_t batch, int32_t max_blocks);
+
+/*
+ * lava_paged_decode for groups of sequences that share pages: the pages that the tables of all sequences of a group begin with are read
+ * once, for the queries of all of them; then every sequence's own.  The result is lava_paged_decode's up to the order of
+ * summation, whatever the tables hold.
+ *
+ *   n_groups     1 .. batch
+ *   group_start  device int32 [n_groups + 1]: group i is sequences group_start[i] .. group_start[i + 1] - 1; from 0, without a
+ *                decrease, to batch.  Others are no error: nothing is shared then
+ * All other arguments, limits and results as for lava_paged_decode.  Sequences of a group without rows in a head are left out of its
+ * comparison.
+ */
+int32_t lava_shared_decode(const lava_layer_desc* desc, int32_t batch, const void* q, const lava_page_pool* pool,
+                           const int32_t* block_table, const int32_t* head_rows, int32_t n_groups, const int32_t* group_start,
+                           const lava_decode_options* options, const int32_t* q_pos, float* out, float* lse, void* workspace,
+                           size_t workspace_bytes, void* hip_stream);
 
 /*
  * Per-kernel timing for benchmarks.  When enabled, every kernel the library launches is

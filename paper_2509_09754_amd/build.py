@@ -23,7 +23,8 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(HERE, "liblava.so")
 
 SOURCES = ["lava_api.hip", "k_sweep.hip", "k_select.hip", "k_compact.hip", "k_budgets.hip", "k_decode.hip", "k_probe.hip",
-           "paged_api.hip", "k_pages.hip", "k_rotary.hip", "k_paged_decode.hip"]
+           "paged_api.hip", "k_pages.hip", "k_rotary.hip", "k_paged_decode.hip",
+           "branch_api.hip", "k_beam.hip", "k_fork.hip", "k_shared.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON_FLAGS = [

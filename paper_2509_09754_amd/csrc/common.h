@@ -30,6 +30,12 @@ enum KernelId : int {
   KID_PAGE_FILL,      // block tables, slots and positions of a step; pages given back
   KID_ROTARY,         // rotary positions, keys and values to their slots
   KID_PAGED_DECODE,   // decode attention over the pages
+  KID_BEAM,           // the best continuations of a step's beams
+  KID_PAGE_MARK,      // forks and compaction of pages: who holds which page, fresh pages
+  KID_PAGE_APPLY,     // their tables, counts, stack and copied rows
+  KID_SHARED_PLAN,    // decode over shared pages: which pages are common
+  KID_SHARED_DECODE,  // the common pages, for all queries of a group
+  KID_SHARED_MERGE,   // common and own rows put together
   KID_COUNT
 };
 
@@ -292,6 +298,41 @@ struct PagedDecodeArgs {
 };
 size_t paged_decode_bytes(const lava_layer_desc& d);
 int32_t launch_paged_decode(const lava_layer_desc& d, const PagedDecodeArgs& a, void* ws, hipStream_t s);
+
+// ---------------------------------------------------------------- sequences that share pages
+struct BeamArgs {
+  const char* logits;
+  long long vocab, stride_bytes;
+  const float* scores;
+  const int32_t* done;         // or null
+  int32_t *parents, *tokens;
+  float* scores_out;
+  int32_t* done_out;           // or null
+  int32_t* sources;            // [n_tables][batch * n_out] or null
+  int batch, beams, n_out, n_tables, end_token, pad_token;
+};
+size_t beam_step_bytes(int32_t batch, int32_t beams, int64_t vocab, int32_t n_out);
+int32_t launch_beam_step(const BeamArgs& a, int32_t dtype, void* ws, hipStream_t s);
+
+struct PageChangeArgs {
+  lava_page_state st;
+  const int32_t* source;       // [batch] or null: every sequence is its own
+  const int32_t* head_counts;  // [batch][heads] or null: heads keep all rows
+  const int32_t* kept_idx;     // [batch][kept_capacity]
+  const int32_t* evict;        // [batch] or null
+  int32_t *table_out, *free_out;   // the state's own: in place
+  char *k, *v;
+  int32_t* pos;                // or null
+  long long n_pages, kept_capacity;
+  int batch, heads, max_blocks, page_shift, row_bytes;
+};
+size_t page_change_bytes(int32_t batch, int32_t n_kv_heads, int32_t max_blocks, int64_t n_pages);
+int32_t launch_page_change(const PageChangeArgs& p, void* ws, hipStream_t s);
+
+size_t shared_decode_bytes(const lava_layer_desc& d, int32_t batch, int32_t max_blocks);
+// p as for launch_paged_decode over the whole tables
+int32_t launch_shared_decode(const lava_layer_desc& d, const PagedDecodeArgs& p, int32_t n_groups, const int32_t* group_start, void* ws,
+                             hipStream_t s);
 
 // ---------------------------------------------------------------- layer budgets
 // The host path runs the sequential allocation, the device kernel the same arithmetic spread over

@@ -33,6 +33,7 @@
 
 #include "common.h"
 #include "decode_parts.h"
+#include "paged_common.h"
 #include "tile_ring.h"
 #include "xblock.h"
 
@@ -71,18 +72,6 @@ constexpr unsigned int kHeadCost = 6u;
 __device__ __forceinline__ int head_tiles(const PagedDecodeArgs& a, int rows) {
   if (rows < 0 || rows > a.max_blocks << a.page_shift) return -1;
   return (int)(((unsigned int)rows + kTileKeys - 1u) / kTileKeys);
-}
-
-// cap * tanh(z / cap): near zero by its series (the quotient of exponentials would cancel), else from e^(-2 |z / cap|).
-__device__ __forceinline__ float capped(float z, float cap, float inv_cap) {
-  const float y = z * inv_cap, a = fabsf(y), s = y * y;
-  float series = fmaf(s, 2.1869489e-2f, -5.3968254e-2f);             // 62 / 2835, -17 / 315
-  series = fmaf(s, series, 1.3333333e-1f);
-  series = fmaf(s, series, -3.3333333e-1f);
-  series = fmaf(a * s, series, a);
-  const float t = fast_exp2(a * (-2.0f * kLog2e));
-  const float far = (1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t);
-  return cap * copysignf(a < 0.25f ? series : far, y);
 }
 
 // Two values of an output row from the maximum (log2 units), the sum and the weighted values; no row seen: zeros.

@@ -1,0 +1,772 @@
+// Decode-step attention of groups of sequences that share pages: softmax over a head's rows splits into the rows of the pages that
+// a group has in common and a sequence's own,
+//   out = (e^(m_c) a_c + e^(m_o) a_o) / (e^(m_c) l_c + e^(m_o) l_o),   m, l, a: maximum, sum and weighted values of either,
+// and the common part of all n sequences of a group with G query heads a KV head is one matrix product of n * G queries.
+//
+//   plan    a workgroup per group and head: leading blocks that the tables of all its sequences have in common; tables of what is
+//           left, for the decode step over pages; the list of items: up to 256 / G sequences of a group, one head
+//   common  the items' rows, cut into equal units of stages (64 KiB of keys and values) for as many workgroups as the device holds
+//   own     the decode step over pages, over the tables of what is left
+//   merge   the parts of the common rows and the own ones, per sequence and head
+//
+// Common rows: a workgroup of eight wavefronts.  A stage's keys and values come to LDS by direct-to-LDS loads, one stage ahead.  A wavefront
+// has 32 queries as the columns of its products and takes every n-th tile of 32 rows, n = 8 / tiles of queries:
+//   logits  K_tile x Q^T: a lane has 16 of a query's 32 logits
+//   softmax online, in the exp2 domain; the other 16 are in lane ^ 32
+//   output  V_tile^T x P^T: in the order in which the first product leaves the rows to a lane they are the operand of the second, so
+//           probabilities stay in registers.  bf16: V is read transposed from LDS, a probability is three bf16 parts (8 + 8 +
+//           8 bits), so that products are exact and sums 32 bits, as in the decode step over pages
+// Rows that are masked may hold anything there.  A product cannot leave them out, so an item whose sums are not all
+// finite is marked, and merge computes its heads' outputs again, row by row.
+#include <math.h>
+
+#include "common.h"
+#include "decode_parts.h"
+#include "paged_common.h"
+#include "tile_ring.h"
+
+namespace lava {
+
+namespace {
+
+constexpr int kShWaves = 8, kShThreads = kShWaves * 64;
+constexpr int kShRows = 32 * kShWaves;         // query rows of an item at most
+constexpr int kStageBytes = 65536;             // keys and values
+
+struct SharedItem {
+  int first_seq, n_seq, head, rows;            // rows in common
+  int lead;                                    // a sequence that holds them
+};
+struct SharedParts {
+  int row, units;                              // first row of its parts, number of parts (each n_seq * G rows)
+};
+
+struct SharedArgs {
+  PagedDecodeArgs p;                           // over the whole tables
+  int n_groups;
+  const int32_t* group_start;
+  float c2;
+  int* n_items;
+  SharedItem* items;
+  SharedParts* parts;                          // [items]
+  int* marked;                                 // [items] sums that are not finite
+  int* item_of;                                // [batch][H_kv] item that has the sequence's common rows, -1: none
+  int* rest_rows;                              // [batch][H_kv]
+  int* rest_table;                             // [batch][H_kv][max_blocks]
+  float* rest_lse;                             // [batch][H]
+  float2* part_ml;                             // [rows] maximum (log2 units) and sum
+  float* part_acc;                             // [rows][D]
+};
+
+// ---------------------------------------------------------------- plan
+constexpr int kPlanShThreads = 1024, kPlanShWaves = kPlanShThreads / 64;
+__global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const SharedArgs a) {
+  __shared__ int s_bad, s_blocks[kPlanShWaves], s_before[kPlanShWaves], s_all[kPlanShWaves], s_lead[kPlanShWaves], s_some[kPlanShWaves];
+  const PagedDecodeArgs& p = a.p;
+  const int group = blockIdx.x / p.H_kv, g = blockIdx.x - group * p.H_kv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int seqs = kShRows / p.G, P = 1 << p.page_shift;
+  if (threadIdx.x == 0) s_bad = 0;
+  __syncthreads();
+  int before = 0, all = 0;                                     // blocks of sequences of the groups before, of all
+  for (int i = threadIdx.x; i < a.n_groups; i += kPlanShThreads) {
+    const int x = a.group_start[i], y = a.group_start[i + 1];
+    if (x < 0 || y < x || y > p.batch || (i == 0 && x != 0) || (i == a.n_groups - 1 && y != p.batch)) {
+      s_bad = 1;
+    } else {
+      const int n = (y - x + seqs - 1) / seqs;
+      before += i < group ? n : 0;
+      all += n;
+    }
+  }
+  before = (int)lane_value(wave_incl((unsigned int)before), 63);
+  all = (int)lane_value(wave_incl((unsigned int)all), 63);
+  if (lane == 0) {
+    s_before[wave] = before;
+    s_all[wave] = all;
+  }
+  __syncthreads();
+  const bool bad = s_bad != 0;
+  before = all = 0;
+  for (int w = 0; w < kPlanShWaves; ++w) {
+    before += s_before[w];
+    all += s_all[w];
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.n_items[0] = bad ? 0 : all * p.H_kv;
+  // groups that are none: every sequence by itself
+  const int b0 = bad ? group : a.group_start[group], b1 = bad ? p.batch : a.group_start[group + 1], step = bad ? a.n_groups : 1;
+  int common = 0, lead = 0x7fffffff;
+  if (!bad && b1 - b0 > 1) {                                   // uniform
+    auto held = [&](int b) { return p.head_rows[(long long)b * p.H_kv + g]; };
+    auto table = [&](int b) { return p.block_table + ((long long)b * p.H_kv + g) * p.max_blocks; };
+    // the sequence to compare with, full blocks that all have
+    int least = 0x7fffffff, some = 0;
+    for (int b = b0 + threadIdx.x; b < b1; b += kPlanShThreads) {
+      const int rows = held(b);
+      if (rows == 0) continue;
+      const int blocks = rows < 0 || rows > p.max_blocks << p.page_shift ? 0 : rows >> p.page_shift;
+      least = blocks < least ? blocks : least;
+      lead = b < lead ? b : lead;
+      ++some;
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      least = min(least, __shfl_xor(least, m));
+      lead = min(lead, __shfl_xor(lead, m));
+      some += __shfl_xor(some, m);
+    }
+    if (lane == 0) {
+      s_blocks[wave] = least;
+      s_lead[wave] = lead;
+      s_some[wave] = some;
+    }
+    __syncthreads();
+    some = 0;
+    for (int w = 0; w < kPlanShWaves; ++w) {
+      least = min(least, s_blocks[w]);
+      lead = min(lead, s_lead[w]);
+      some += s_some[w];
+    }
+    if (some > 1) {
+      const int* first = table(lead);
+      common = least;
+      for (int b = b0 + wave; b < b1; b += kPlanShWaves) {     // a wavefront a sequence: the first block that differs
+        if (b == lead || held(b) == 0) continue;
+        const int* mine = table(b);
+        for (int j0 = 0; j0 < common; j0 += 256) {
+          unsigned long long off[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int j = j0 + 64 * u + lane;
+            off[u] = __ballot(j < common && mine[j] != first[j]);
+          }
+#pragma unroll
+          for (int u = 3; u >= 0; --u)
+            if (off[u] != 0ull) common = j0 + 64 * u + __builtin_ctzll(off[u]);
+        }
+      }
+    }
+    __syncthreads();                                           // s_blocks is read
+    if (lane == 0) s_blocks[wave] = common;
+    __syncthreads();
+    for (int w = 0; w < kPlanShWaves; ++w) common = min(common, s_blocks[w]);
+  }
+  const int n = b1 - b0, blocks = bad ? 0 : (n + seqs - 1) / seqs, item0 = before * p.H_kv + g * blocks;
+  for (int i = threadIdx.x; i < blocks; i += kPlanShThreads) {
+    SharedItem it;
+    it.first_seq = b0 + i * seqs;
+    it.n_seq = n - i * seqs < seqs ? n - i * seqs : seqs;
+    it.head = g;
+    it.rows = common << p.page_shift;
+    it.lead = common > 0 ? lead : b0;
+    a.items[item0 + i] = it;
+    a.marked[item0 + i] = 0;
+  }
+  for (int b = b0 + wave * step; b < b1; b += kPlanShWaves * step) {   // a wavefront a sequence: what is left
+    const long long h = (long long)b * p.H_kv + g;
+    const int rows = p.head_rows[h], skip = rows == 0 ? 0 : common;
+    if (lane == 0) {
+      a.rest_rows[h] = rows - (skip << p.page_shift);
+      a.item_of[h] = skip > 0 ? item0 + (b - b0) / seqs : -1;
+    }
+    if (rows <= 0 || rows > p.max_blocks << p.page_shift) continue;
+    const int* from = p.block_table + h * p.max_blocks + skip;
+    int* to = a.rest_table + h * p.max_blocks;
+    const int left = ((rows + P - 1) >> p.page_shift) - skip;
+    for (int j = lane; j < left; j += 64) to[j] = from[j];
+  }
+}
+
+// ---------------------------------------------------------------- common rows
+template <int DT, int D>
+struct ShShape {
+  using T = Tile<DT, D>;
+  static constexpr int kTiles = kStageBytes / (2 * T::kTileBytes);   // tiles of 32 rows in a stage
+  static constexpr int kStageRows = 32 * kTiles;
+  static constexpr int kHalves = 2 * kTiles;                          // half tiles, 16 rows each: within a page
+  static constexpr int kMine = kHalves / kShWaves > 0 ? kHalves / kShWaves : 1;   // half tiles of a stage whose pages a wavefront holds
+  static constexpr int kDBlocks = D / 32;
+};
+
+// 16 values of bf16 V^T as the left operand, for rows 16 s .. 16 s + 15 of a tile and columns 32 dblk ..: two reads of four rows
+// each; `even` and `odd`: addresses for even and odd dblk.
+template <int D, int S>
+__device__ __forceinline__ void read_v(unsigned int even, unsigned int odd, u32x4 (&v)[D / 32]) {
+  constexpr int R = D * 2, o = 16 * S * R;
+  typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+  u32x2 x[D / 16];
+  if constexpr (D == 128) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %1, %8 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %2, %9 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %3, %9 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %4, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %5, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %6, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %7, %9 offset:%13\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(even), "v"(odd), "n"(o), "n"(o + 8 * R), "n"(o + 128), "n"(o + 8 * R + 128)
+        : "memory");
+  } else {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
+        "ds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+        "ds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
+        "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+        : "v"(even), "v"(odd), "n"(o), "n"(o + 8 * R)
+        : "memory");
+  }
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) v[d] = u32x4{x[2 * d].x, x[2 * d].y, x[2 * d + 1].x, x[2 * d + 1].y};
+}
+
+// Four 32-bit values at one offset from four addresses.
+template <int OFF>
+__device__ __forceinline__ void lds_read32x4_at(const unsigned int (&a)[4], unsigned int base, float (&o)[4]) {
+  unsigned int x0 = a[0] + base, x1 = a[1] + base, x2 = a[2] + base, x3 = a[3] + base;
+  asm volatile(
+      "ds_read_b32 %0, %4 offset:%8\n\t"
+      "ds_read_b32 %1, %5 offset:%8\n\t"
+      "ds_read_b32 %2, %6 offset:%8\n\t"
+      "ds_read_b32 %3, %7 offset:%8\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3])
+      : "v"(x0), "v"(x1), "v"(x2), "v"(x3), "n"(OFF)
+      : "memory");
+}
+
+template <int DT, int D, bool OPT>
+__global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const SharedArgs a) {
+  using S = ShShape<DT, D>;
+  using T = Tile<DT, D>;
+  __shared__ u32x4 s_stage[2][kStageBytes / 16];               // keys' tiles, then values'; between units: float [kShWaves][32][D]
+  __shared__ __attribute__((aligned(16))) int s_pos[2][OPT ? S::kStageRows : 4];
+  __shared__ float s_m[kShWaves][32], s_l[kShWaves][32];
+  __shared__ int s_wrong;
+  const PagedDecodeArgs& p = a.p;
+  const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 31, half = lane >> 5;
+  const int n_items = a.n_items[0];
+  // stages of all items, items that have any
+  auto stages_of = [&](int i) { return i < n_items ? (a.items[i].rows + S::kStageRows - 1) / S::kStageRows : 0; };
+  unsigned int total = 0u, full = 0u;
+  for (int i = lane; i < n_items; i += 64) {
+    const int n = stages_of(i);
+    total += (unsigned int)n;
+    full += n > 0 ? 1u : 0u;
+  }
+  total = lane_value(wave_incl(total), 63);
+  full = lane_value(wave_incl(full), 63);
+  if (total == 0u) return;
+  // units of `share` stages of one item: no more units than workgroups where items are few
+  const unsigned int wgs = gridDim.x;
+  const unsigned int cut = 2u * full <= wgs ? wgs - full : 2u * wgs;
+  const int share = (int)((total + cut - 1u) / cut);
+
+  TileDma<DT, D> dma;
+  dma.init(lane);
+  FragReader<DT, D> frags;
+  frags.init(lane);
+  const unsigned int ring = lds_addr(&s_stage[0][0]);
+  constexpr unsigned int kVOff = S::kTiles * T::kTileBytes;
+  // bf16: where this lane's four columns of row 4 half + (lane % 16) / 4 lie, for even and odd blocks of 32 columns.  32 bits: this lane's
+  // column of rows 4 half + 0 .. 3.
+  unsigned int v_at[4] = {0u, 0u, 0u, 0u};
+  if constexpr (DT == LAVA_BF16) {
+    const int i = lane & 15, r = 4 * half + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) v_at[e] = (unsigned int)(r * T::kRowBytes + (((4 * e + c) ^ r) << 4) + 8 * (i & 1));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 4 * half + e;
+      v_at[e] = (unsigned int)(r * T::kRowBytes + (((col >> 2) ^ r) << 4) + 4 * (col & 3));
+    }
+  }
+  const float inv_cap = p.cap > 0.0f ? 1.0f / p.cap : 0.0f;
+  const unsigned int window = p.window > 0 ? (unsigned int)p.window : 0x80000000u;
+
+  for (unsigned int u = blockIdx.x;; u += wgs) {
+    // ---------------- the unit: its item, its part of the item, where its rows go
+    int item = -1, part = 0, units = 0, row0 = 0;
+    {
+      unsigned int at = 0u, rows = 0u;
+      for (int i0 = 0; i0 < n_items && item < 0; i0 += 64) {
+        const int n = (stages_of(i0 + lane) + share - 1) / share;
+        const int mine = n > 0 ? n * a.items[i0 + lane].n_seq * p.G : 0;
+        const unsigned int incl = wave_incl((unsigned int)n), r_incl = wave_incl((unsigned int)mine);
+        const unsigned long long after = __ballot(at + incl > u);
+        if (after != 0ull) {
+          const int l = __builtin_ctzll(after);
+          item = i0 + l;
+          units = (int)lane_value((unsigned int)n, l);
+          part = (int)(u - (at + lane_value(incl, l) - (unsigned int)units));
+          row0 = (int)(rows + lane_value(r_incl, l) - lane_value((unsigned int)mine, l));
+        } else {
+          at += lane_value(incl, 63);
+          rows += lane_value(r_incl, 63);
+        }
+      }
+    }
+    if (item < 0) return;                                      // uniform: no unit left
+    const SharedItem it = a.items[item];
+    const int q_rows = it.n_seq * p.G;
+    if (part == 0 && threadIdx.x == 0) a.parts[item] = SharedParts{row0, units};
+    const int row_tiles = q_rows <= 32 ? 1 : q_rows <= 64 ? 2 : q_rows <= 128 ? 4 : 8;
+    const int rt = wave & (row_tiles - 1), kp = wave / row_tiles, key_parts = kShWaves / row_tiles;
+    const int s0 = part * share, s_all = (it.rows + S::kStageRows - 1) / S::kStageRows, s1 = s0 + share < s_all ? s0 + share : s_all;
+    const int* table = p.block_table + ((long long)it.lead * p.H_kv + it.head) * p.max_blocks;
+
+    // ---------------- the queries of this lane's column
+    const int qr = rt * 32 + col;
+    const bool real = qr < q_rows;
+    const int q_seq = it.first_seq + (real ? qr / p.G : 0), q_head = it.head * p.G + (real ? qr % p.G : 0);
+    u32x4 qf[T::kSteps];
+#pragma unroll
+    for (int j = 0; j < T::kSteps; ++j) {
+      u32x4 x = u32x4{0u, 0u, 0u, 0u};
+      if (real) x = reinterpret_cast<const u32x4*>(p.q)[((long long)q_seq * p.H + q_head) * T::kCpr + 2 * j + half];
+      qf[j] = x;
+    }
+    const int q_pos = OPT && p.pos != nullptr ? p.q_pos[q_seq] : 0;
+    const float slope = OPT && p.slopes != nullptr ? p.slopes[q_head] * kLog2e : 0.0f;
+
+    float m_run = -INFINITY, l_run = 0.0f;
+    f32x16 acc[S::kDBlocks];
+#pragma unroll
+    for (int d = 0; d < S::kDBlocks; ++d) acc[d] = f32x16{0};
+    if (threadIdx.x == 0) s_wrong = 0;
+    __syncthreads();                                           // LDS is free, s_wrong is set
+
+    // pages of this wavefront's half tiles of stages sb .. sb + 63, a lane each
+    int page[S::kMine];
+    auto load_pages = [&](int sb) {
+#pragma unroll
+      for (int x = 0; x < S::kMine; ++x) {
+        const int hh = (wave + kShWaves * x) % S::kHalves, r = (sb + lane) * S::kStageRows + 16 * hh;
+        page[x] = sb + lane < s1 && r < it.rows ? table[r >> p.page_shift] : -2;
+      }
+#pragma unroll
+      for (int x = 0; x < S::kMine; ++x) {
+        if (page[x] == -2) page[x] = 0;                        // behind the last row: masked, any page will do
+        else if (page[x] < 0 || page[x] >= p.n_pages) {
+          page[x] = 0;
+          s_wrong = 2;
+        }
+      }
+    };
+    int pos_next[S::kMine] = {};
+    auto issue = [&](int s, int sb) {                          // stage s of pages loaded from sb on
+      u32x4* dst = s_stage[s & 1];
+#pragma unroll
+      for (int x = 0; x < 4 * S::kTiles / kShWaves; ++x) {
+        const int k = wave + kShWaves * x, hh = k % S::kHalves;
+        const bool is_v = k >= S::kHalves;
+        const int r = s * S::kStageRows + 16 * hh;
+        const long long place = ((long long)(int)lane_value((unsigned int)page[x % S::kMine], s - sb) << p.page_shift) +
+                                (r < it.rows ? r & ((1 << p.page_shift) - 1) : 0);
+        const char* src = (is_v ? p.v : p.k) + place * T::kRowBytes;
+        u32x4* to = dst + (is_v ? S::kTiles * T::kTileChunks : 0) + hh * (T::kTileChunks / 2);
+#pragma unroll
+        for (int i = 0; i < T::kLoads / 2; ++i)
+          __builtin_amdgcn_global_load_lds((const LAVA_GLOBAL_AS void*)(src + i * 1024 + dma.loff[i % TileDma<DT, D>::kVariants]),
+                                           (LAVA_LDS_AS void*)(to + i * 64), 16, 0, 0);
+        if (OPT && p.pos != nullptr && !is_v) pos_next[x % S::kMine] = p.pos[place + (lane & 15)];
+      }
+    };
+
+    int sb = s0;
+    load_pages(sb);
+    issue(s0, sb);
+    for (int s = s0; s < s1; ++s) {
+      wait_vmcnt<0>();
+      if (OPT && p.pos != nullptr) {
+#pragma unroll
+        for (int x = 0; x < S::kMine; ++x) {
+          const int k = wave + kShWaves * x;
+          if (k < S::kHalves && lane < 16) lds_write32(lds_addr(&s_pos[s & 1][16 * k + lane]), __int_as_float(pos_next[x]));
+        }
+        lds_reads_done();
+      }
+      __syncthreads();                                         // stage s is there, the other one free
+      if (s + 1 < s1) {
+        if (s + 1 - sb == 64) {
+          sb = s + 1;
+          load_pages(sb);
+        }
+        issue(s + 1, sb);
+      }
+      asm volatile("" ::: "memory");
+      const unsigned int stage = ring + (unsigned int)(s & 1) * kStageBytes;
+      for (int t = kp; t < S::kTiles; t += key_parts) {
+        const int r0 = s * S::kStageRows + 32 * t;             // first row of the tile
+        if (r0 >= it.rows) break;                              // uniform
+        f32x16 z = {0}, z2 = {0};
+        {
+          u32x4 kf[T::kSteps];
+          frags.read(stage + (unsigned int)t * T::kTileBytes, kf);
+#pragma unroll
+          for (int j = 0; j < T::kSteps; j += 2) {
+            z = mfma_chunk<DT>(kf[j], qf[j], z);
+            z2 = mfma_chunk<DT>(kf[j + 1], qf[j + 1], z2);
+          }
+        }
+        float x[16];                                           // of rows 8 (v / 4) + 4 half + v % 4
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[v] = z[v] + z2[v];
+        if (OPT && p.cap > 0.0f) {                             // uniform
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = capped(x[v] * p.scale, p.cap, inv_cap) * kLog2e;
+        } else {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] *= a.c2;
+        }
+        if (OPT && p.pos != nullptr) {                         // uniform
+#pragma unroll
+          for (int v4 = 0; v4 < 4; ++v4) {
+            u32x4 at;
+            lds_read128(lds_addr(&s_pos[s & 1][32 * t + 8 * v4 + 4 * half]), at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned int back = (unsigned int)q_pos - at[e];   // a later row: 2^31 and more
+              const float y = x[4 * v4 + e] - slope * (float)back;
+              x[4 * v4 + e] = back < window ? y : -INFINITY;
+            }
+          }
+        }
+        if (r0 + 32 > it.rows) {                               // uniform: the second half tile is behind the last row
+#pragma unroll
+          for (int v = 8; v < 16; ++v) x[v] = -INFINITY;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+        {
+          const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+          top = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+        }
+        if (__ballot(top > m_run) != 0ull) {                   // uniform: a maximum moves
+          const float m_new = fmaxf(m_run, top), keep = m_new == -INFINITY ? 1.0f : fast_exp2(m_run - m_new);
+          m_run = m_new;
+          l_run *= keep;
+#pragma unroll
+          for (int d = 0; d < S::kDBlocks; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[d][v] *= keep;
+        }
+        const float base = m_run == -INFINITY ? 0.0f : m_run;
+        float e[16], sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          e[v] = fast_exp2(x[v] - base);
+          sum += e[v];
+        }
+        l_run += sum;
+        const unsigned int values = stage + kVOff + (unsigned int)t * T::kTileBytes;
+        if constexpr (DT == LAVA_BF16) {
+          static_for<2>([&](auto sc) {
+            constexpr int h = decltype(sc)::value;
+            u32x4 parts[3];
+            {
+              u32x4 lo, hi;
+#pragma unroll
+              for (int v = 0; v < 4; ++v) {
+                lo[v] = __float_as_uint(e[8 * h + v]);
+                hi[v] = __float_as_uint(e[8 * h + 4 + v]);
+              }
+              split8(lo, hi, parts[0], parts[1], parts[2]);
+            }
+            u32x4 vt[S::kDBlocks];
+            read_v<D, h>(values + v_at[0], values + v_at[1], vt);
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll
+              for (int d = 0; d < S::kDBlocks; ++d) acc[d] = mfma_bf16(vt[d], parts[k], acc[d]);
+          });
+        } else {
+          static_for<4 * S::kDBlocks>([&](auto ic) {
+            constexpr int v4 = decltype(ic)::value / S::kDBlocks, d = decltype(ic)::value % S::kDBlocks;
+            float vv[4];
+            lds_read32x4_at<8 * v4 * T::kRowBytes + 128 * d>(v_at, values, vv);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv[k], e[4 * v4 + k], acc[d], 0, 0, 0);
+          });
+        }
+      }
+      lds_reads_done();
+    }
+    // ---------------- the unit's part: wavefronts with the same queries put together
+    l_run = add_halves(l_run);
+    bool wrong = !(l_run < INFINITY);
+#pragma unroll
+    for (int d = 0; d < S::kDBlocks; ++d)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) wrong |= !(fabsf(acc[d][v]) < INFINITY);
+    wrong = wrong && real;
+    __syncthreads();                                           // every wavefront is done with the stages
+    if (__ballot(wrong) != 0ull && lane == 0) atomicOr(&s_wrong, 1);
+    constexpr int kChunks = D / 4;                             // 16-byte chunks of an output row
+    float* s_acc = reinterpret_cast<float*>(&s_stage[0][0]);
+    if (half == 0) {
+      s_m[wave][col] = m_run;
+      s_l[wave][col] = l_run;
+    }
+#pragma unroll
+    for (int d = 0; d < S::kDBlocks; ++d)
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const int c = 8 * d + 2 * v4 + half;                   // columns 32 d + 8 v4 + 4 half ..
+        *reinterpret_cast<float4*>(s_acc + (wave * 32 + col) * D + 4 * (c ^ (col & (kChunks - 1)))) =
+            make_float4(acc[d][4 * v4], acc[d][4 * v4 + 1], acc[d][4 * v4 + 2], acc[d][4 * v4 + 3]);
+      }
+    __syncthreads();
+    if (s_wrong != 0 && threadIdx.x == 0) atomicOr(&a.marked[item], s_wrong);
+    const long long out0 = (long long)row0 + (long long)part * q_rows;
+    for (int i = threadIdx.x; i < q_rows * kChunks; i += kShThreads) {
+      const int r = i / kChunks, c = i - r * kChunks, w0 = r >> 5, cr = r & 31;
+      float M = -INFINITY;
+      for (int k = 0; k < key_parts; ++k) M = fmaxf(M, s_m[w0 + k * row_tiles][cr]);
+      const float base = M == -INFINITY ? 0.0f : M;
+      float L = 0.0f;
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int k = 0; k < key_parts; ++k) {
+        const int w = w0 + k * row_tiles;
+        const float wgt = fast_exp2(s_m[w][cr] - base);
+        const float4 y = *reinterpret_cast<const float4*>(s_acc + (w * 32 + cr) * D + 4 * (c ^ (cr & (kChunks - 1))));
+        L += wgt * s_l[w][cr];
+        sum.x += wgt * y.x;
+        sum.y += wgt * y.y;
+        sum.z += wgt * y.z;
+        sum.w += wgt * y.w;
+      }
+      *reinterpret_cast<float4*>(a.part_acc + (out0 + r) * D + 4 * c) = sum;
+      if (c == 0) a.part_ml[out0 + r] = make_float2(M, L);
+    }
+    __syncthreads();                                           // the next unit may use LDS
+  }
+}
+
+// ---------------------------------------------------------------- merge
+constexpr int kMergeThreads = 256;
+
+// One head's output from all its rows, one after another: where a value in a masked row may be infinite or no number.
+template <int DT, int D>
+__device__ __forceinline__ void whole_head(const SharedArgs& a, int b, int g, float* s_red) {
+  const PagedDecodeArgs& p = a.p;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = p.head_rows[(long long)b * p.H_kv + g];
+  constexpr int kWaves = kMergeThreads / 64, kEach = D / 64;
+  const int* table = p.block_table + ((long long)b * p.H_kv + g) * p.max_blocks;
+  const int q_pos = p.pos != nullptr ? p.q_pos[b] : 0;
+  const unsigned int window = p.window > 0 ? (unsigned int)p.window : 0x80000000u;
+  auto load = [&](const char* from, long long place, float (&y)[kEach]) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const long long at = place * D + lane * kEach + e;
+      y[e] = DT == LAVA_BF16 ? __uint_as_float((unsigned int)reinterpret_cast<const unsigned short*>(from)[at] << 16)
+                             : reinterpret_cast<const float*>(from)[at];
+    }
+  };
+  for (int t = 0; t < p.G; ++t) {
+    const long long row = (long long)b * p.H + (long long)g * p.G + t;
+    const float slope = p.slopes != nullptr ? p.slopes[g * p.G + t] * kLog2e : 0.0f;
+    float q[kEach], acc[kEach] = {}, M = -INFINITY, L = 0.0f;
+    load(p.q, row, q);
+    bool bad = false;
+    for (int r = wave; r < rows; r += kWaves) {
+      const int page = table[r >> p.page_shift];
+      if (page < 0 || page >= p.n_pages) {
+        bad = true;
+        continue;
+      }
+      const long long place = ((long long)page << p.page_shift) + (r & ((1 << p.page_shift) - 1));
+      const unsigned int back = p.pos != nullptr ? (unsigned int)q_pos - (unsigned int)p.pos[place] : 0u;
+      if (back >= window) continue;
+      float k[kEach], v[kEach], x = 0.0f;
+      load(p.k, place, k);
+      load(p.v, place, v);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) x = fmaf(q[e], k[e], x);
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+      x = p.cap > 0.0f ? capped(x * p.scale, p.cap, 1.0f / p.cap) * kLog2e : x * a.c2;
+      x -= slope * (float)back;
+      const float m_new = fmaxf(M, x), base = m_new == -INFINITY ? 0.0f : m_new;
+      const float keep = fast_exp2(M - base), w = fast_exp2(x - base);
+      M = m_new;
+      L = L * keep + w;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) acc[e] = acc[e] * keep + w * v[e];
+    }
+    if (bad) L = NAN;
+    __syncthreads();
+    if (lane == 0) {
+      s_red[2 * wave] = M;
+      s_red[2 * wave + 1] = L;
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) s_red[2 * kWaves + wave * D + lane * kEach + e] = acc[e];
+    __syncthreads();
+    if ((int)threadIdx.x < D) {
+      float top = -INFINITY, sum = 0.0f, y = 0.0f;
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_red[2 * w]);
+      const float base = top == -INFINITY ? 0.0f : top;
+      for (int w = 0; w < kWaves; ++w) {
+        const float wgt = fast_exp2(s_red[2 * w] - base);
+        sum += wgt * s_red[2 * w + 1];
+        y += wgt * s_red[2 * kWaves + w * D + threadIdx.x];
+      }
+      p.out[row * D + threadIdx.x] = sum == 0.0f ? 0.0f : y / sum;
+      if (threadIdx.x == 0 && p.lse != nullptr) p.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    }
+  }
+}
+
+template <int DT, int D>
+__global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const SharedArgs a) {
+  __shared__ float s_red[(kMergeThreads / 64) * (D + 2)];
+  const PagedDecodeArgs& p = a.p;
+  const int b = blockIdx.x / p.H_kv, g = blockIdx.x - b * p.H_kv;
+  const int item = a.item_of[blockIdx.x];
+  const long long row0 = (long long)b * p.H + (long long)g * p.G;
+  if (item < 0) {                                              // nothing in common: the own rows were all
+    if (p.lse != nullptr && (int)threadIdx.x < p.G) p.lse[row0 + threadIdx.x] = a.rest_lse[row0 + threadIdx.x];
+    return;
+  }
+  const int marked = a.marked[item];
+  if (marked == 1) {                                           // no page was wrong: only values
+    whole_head<DT, D>(a, b, g, s_red);
+    return;
+  }
+  const SharedItem it = a.items[item];
+  const SharedParts parts = a.parts[item];
+  const int q_rows = it.n_seq * p.G;
+  for (int i = threadIdx.x; i < p.G * (D / 4); i += kMergeThreads) {
+    const int t = i / (D / 4), c = i - t * (D / 4);
+    const long long first = parts.row + (long long)(b - it.first_seq) * p.G + t;
+    const float own = a.rest_lse[row0 + t] * kLog2e;
+    float M = own;
+    for (int u = 0; u < parts.units; ++u) M = fmaxf(M, a.part_ml[first + (long long)u * q_rows].x);
+    const float base = M == -INFINITY ? 0.0f : M;
+    float4* out = reinterpret_cast<float4*>(p.out + (row0 + t) * D) + c;
+    const float4 mine = *out;
+    float wgt = fast_exp2(own - base), L = wgt;
+    float4 sum = make_float4(wgt * mine.x, wgt * mine.y, wgt * mine.z, wgt * mine.w);
+    for (int u = 0; u < parts.units; ++u) {
+      const long long r = first + (long long)u * q_rows;
+      const float2 ml = a.part_ml[r];
+      const float4 y = *reinterpret_cast<const float4*>(a.part_acc + r * D + 4 * c);
+      wgt = fast_exp2(ml.x - base);
+      L += wgt * ml.y;
+      sum.x += wgt * y.x;
+      sum.y += wgt * y.y;
+      sum.z += wgt * y.z;
+      sum.w += wgt * y.w;
+    }
+    if (marked != 0 || isnan(own)) L = NAN;                    // a page that is not in the pool, of the common ones or the own
+    const bool none = L == 0.0f;
+    *out = none ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x / L, sum.y / L, sum.z / L, sum.w / L);
+    if (c == 0 && p.lse != nullptr) p.lse[row0 + t] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  }
+}
+
+template <typename K>
+int resident_shared(K kernel) {
+  int per = 0;
+  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kShThreads, 0) != hipSuccess || per < 1) {
+    discard_stale_error();
+    per = 1;
+  }
+  return device_cus();                                         // a stage and the next one take more than half of a compute unit's LDS
+}
+
+struct SharedLayout {
+  size_t off_items, off_parts, off_marked, off_item_of, off_rest_rows, off_rest_table, off_rest_lse, off_ml, off_acc, off_decode, bytes;
+};
+SharedLayout shared_layout(const lava_layer_desc& d, int32_t batch, int32_t max_blocks) {
+  const size_t heads = (size_t)batch * d.n_kv_heads, G = d.n_q_heads / d.n_kv_heads;
+  const size_t widest = batch * G < (size_t)kShRows ? batch * G : (size_t)kShRows;
+  // parts: `cut` units of whole shares at most, of the widest items, and one more unit an item
+  const size_t rows = 2 * (size_t)device_cus() * widest + (size_t)batch * d.n_q_heads;
+  SharedLayout l;
+  l.off_items = align_up(sizeof(int));
+  l.off_parts = l.off_items + align_up(heads * sizeof(SharedItem));
+  l.off_marked = l.off_parts + align_up(heads * sizeof(SharedParts));
+  l.off_item_of = l.off_marked + align_up(heads * 4);
+  l.off_rest_rows = l.off_item_of + align_up(heads * 4);
+  l.off_rest_table = l.off_rest_rows + align_up(heads * 4);
+  l.off_rest_lse = l.off_rest_table + align_up(heads * max_blocks * 4);
+  l.off_ml = l.off_rest_lse + align_up((size_t)batch * d.n_q_heads * 4);
+  l.off_acc = l.off_ml + align_up(rows * sizeof(float2));
+  l.off_decode = l.off_acc + align_up(rows * d.head_dim * sizeof(float));
+  l.bytes = l.off_decode + paged_decode_bytes(d);
+  return l;
+}
+
+template <int DT, int D>
+int32_t launch_common(const SharedArgs& a, hipStream_t s) {
+  ProfScope ps(KID_SHARED_DECODE, s);
+  if (a.p.pos != nullptr || a.p.cap > 0.0f) {
+    static const int wgs = resident_shared(shared_common_kernel<DT, D, true>);
+    hipLaunchKernelGGL((shared_common_kernel<DT, D, true>), dim3((unsigned)wgs), dim3(kShThreads), 0, s, a);
+  } else {
+    static const int wgs = resident_shared(shared_common_kernel<DT, D, false>);
+    hipLaunchKernelGGL((shared_common_kernel<DT, D, false>), dim3((unsigned)wgs), dim3(kShThreads), 0, s, a);
+  }
+  return launch_status();
+}
+
+template <int DT, int D>
+int32_t launch_merge(const SharedArgs& a, hipStream_t s) {
+  ProfScope ps(KID_SHARED_MERGE, s);
+  hipLaunchKernelGGL((shared_merge_kernel<DT, D>), dim3((unsigned)(a.p.batch * a.p.H_kv)), dim3(kMergeThreads), 0, s, a);
+  return launch_status();
+}
+
+}  // namespace
+
+size_t shared_decode_bytes(const lava_layer_desc& d, int32_t batch, int32_t max_blocks) { return shared_layout(d, batch, max_blocks).bytes; }
+
+int32_t launch_shared_decode(const lava_layer_desc& d, const PagedDecodeArgs& p, int32_t n_groups, const int32_t* group_start, void* ws,
+                             hipStream_t s) {
+  SharedArgs a;
+  a.p = p;
+  a.n_groups = n_groups;
+  a.group_start = group_start;
+  a.c2 = p.scale * kLog2e;
+  const SharedLayout l = shared_layout(d, p.batch, p.max_blocks);
+  char* w = static_cast<char*>(ws);
+  a.n_items = reinterpret_cast<int*>(w);
+  a.items = reinterpret_cast<SharedItem*>(w + l.off_items);
+  a.parts = reinterpret_cast<SharedParts*>(w + l.off_parts);
+  a.marked = reinterpret_cast<int*>(w + l.off_marked);
+  a.item_of = reinterpret_cast<int*>(w + l.off_item_of);
+  a.rest_rows = reinterpret_cast<int*>(w + l.off_rest_rows);
+  a.rest_table = reinterpret_cast<int*>(w + l.off_rest_table);
+  a.rest_lse = reinterpret_cast<float*>(w + l.off_rest_lse);
+  a.part_ml = reinterpret_cast<float2*>(w + l.off_ml);
+  a.part_acc = reinterpret_cast<float*>(w + l.off_acc);
+  {
+    ProfScope ps(KID_SHARED_PLAN, s);
+    hipLaunchKernelGGL(shared_plan_kernel, dim3((unsigned)(n_groups * p.H_kv)), dim3(kPlanShThreads), 0, s, a);
+  }
+  int32_t st = launch_status();
+  const bool bf16 = d.dtype == LAVA_BF16, wide = d.head_dim == 128;
+  if (st == LAVA_OK)
+    st = bf16 ? (wide ? launch_common<LAVA_BF16, 128>(a, s) : launch_common<LAVA_BF16, 64>(a, s))
+              : (wide ? launch_common<LAVA_F32, 128>(a, s) : launch_common<LAVA_F32, 64>(a, s));
+  if (st == LAVA_OK) {
+    PagedDecodeArgs own = p;
+    own.block_table = a.rest_table;
+    own.head_rows = a.rest_rows;
+    own.lse = a.rest_lse;
+    st = launch_paged_decode(d, own, w + l.off_decode, s);
+  }
+  if (st == LAVA_OK)
+    st = bf16 ? (wide ? launch_merge<LAVA_BF16, 128>(a, s) : launch_merge<LAVA_BF16, 64>(a, s))
+              : (wide ? launch_merge<LAVA_F32, 128>(a, s) : launch_merge<LAVA_F32, 64>(a, s));
+  return st;
+}
+
+}  // namespace lava

@@ -21,7 +21,8 @@ struct ProfState {
 
 const char* const kKernelNames[KID_COUNT] = {
     "vnorm", "stats", "scores", "sweep", "prepass", "poolstat", "sel_init", "sel_fused", "sel_steps", "compact", "budgets",
-    "decode", "page_plan", "page_fill", "rotary", "paged_decode"};
+    "decode", "page_plan", "page_fill", "rotary", "paged_decode", "beam", "page_mark",
+    "page_apply", "shared_plan", "shared_decode", "shared_merge"};
 
 void prof_collect() {
   (void)hipDeviceSynchronize();

@@ -33,6 +33,8 @@ EXPORTS = [
     "lava_decode_workspace_bytes", "lava_decode_attention",
     "lava_page_tables_workspace_bytes", "lava_page_tables", "lava_compact_paged", "lava_rotary_turns", "lava_rotary",
     "lava_rotary_append", "lava_paged_decode_workspace_bytes", "lava_paged_decode",
+    "lava_beam_step_workspace_bytes", "lava_beam_step", "lava_page_fork_workspace_bytes", "lava_page_fork", "lava_page_compact",
+    "lava_shared_decode_workspace_bytes", "lava_shared_decode",
     "lava_prof_kernel_count", "lava_prof_kernel_name", "lava_prof_enable", "lava_prof_reset",
     "lava_prof_read", "lava_probe_stream",
 ]
@@ -154,6 +156,20 @@ def _load() -> ctypes.CDLL:
     lib.lava_paged_decode_workspace_bytes.argtypes = [dp]
     lib.lava_paged_decode.restype = i32
     lib.lava_paged_decode.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lava_beam_step_workspace_bytes.restype = sz
+    lib.lava_beam_step_workspace_bytes.argtypes = [i32, i32, i64, i32]
+    lib.lava_beam_step.restype = i32
+    lib.lava_beam_step.argtypes = [i32, i32, i32, i64, vp, i64, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+    lib.lava_page_fork_workspace_bytes.restype = sz
+    lib.lava_page_fork_workspace_bytes.argtypes = [i32, i32, i32, i64]
+    lib.lava_page_fork.restype = i32
+    lib.lava_page_fork.argtypes = [dp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.lava_page_compact.restype = i32
+    lib.lava_page_compact.argtypes = [dp, vp, i32, vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.lava_shared_decode_workspace_bytes.restype = sz
+    lib.lava_shared_decode_workspace_bytes.argtypes = [dp, i32, i32]
+    lib.lava_shared_decode.restype = i32
+    lib.lava_shared_decode.argtypes = [dp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lava_prof_kernel_count.restype = i32
     lib.lava_prof_kernel_name.restype = ctypes.c_char_p
     lib.lava_prof_kernel_name.argtypes = [i32]
@@ -938,12 +954,9 @@ def lava_paged_decode_workspace_bytes(desc: LayerDesc) -> int:
     return int(lib.lava_paged_decode_workspace_bytes(ctypes.byref(desc)))
 
 
-def lava_paged_decode(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_table: torch.Tensor, head_rows: torch.Tensor,
-                      options: Optional[DecodeOptions] = None, q_pos: Optional[torch.Tensor] = None, out=None, lse=None,
-                      workspace=None, stream=None):
-    """One new token per sequence, q [batch, H, d_h], attends to the pages of its heads; block_table
-    [batch, H_kv, pool.max_blocks], head_rows [batch, H_kv], q_pos [batch] int32.  Returns (out, lse).  Where n_new of the step is zero for some
-    sequences, q is q_out.index_select(0, (n_new.cumsum(0) - 1).clamp(min=0)) of lava_rotary_append's."""
+def _decode_tensors(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_table: torch.Tensor, head_rows: torch.Tensor, options, q_pos, out,
+                    lse, stream):
+    """The checks of a decode step over pages.  Returns (batch, out, lse)."""
     _dev(q, "q", desc.torch_dtype), _dev(block_table, "block_table", torch.int32), _dev(head_rows, "head_rows", torch.int32)
     _here(q)
     batch = q.numel() // (desc.n_q_heads * desc.head_dim)
@@ -965,12 +978,140 @@ def lava_paged_decode(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_ta
     for name, t, n in (("out", out, q.numel()), ("lse", lse, batch * desc.n_q_heads)):
         if _dev(t, name, torch.float32).numel() != n:
             raise ValueError(f"{name} must hold {n} values")
+    return batch, out, lse
+
+
+def lava_paged_decode(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_table: torch.Tensor, head_rows: torch.Tensor,
+                      options: Optional[DecodeOptions] = None, q_pos: Optional[torch.Tensor] = None, out=None, lse=None,
+                      workspace=None, stream=None):
+    """One new token per sequence, q [batch, H, d_h], attends to the pages of its heads; block_table
+    [batch, H_kv, pool.max_blocks], head_rows [batch, H_kv], q_pos [batch] int32.  Returns (out, lse).  Where n_new of the step is zero for some
+    sequences, q is q_out.index_select(0, (n_new.cumsum(0) - 1).clamp(min=0)) of lava_rotary_append's."""
+    batch, out, lse = _decode_tensors(desc, q, pool, block_table, head_rows, options, q_pos, out, lse, stream)
     if workspace is None:
         workspace = _empty(max(lava_paged_decode_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device, stream=stream)
     st = lib.lava_paged_decode(ctypes.byref(desc), batch, _ptr(q), pool._ref, _ptr(block_table), _ptr(head_rows),
                                ctypes.byref(options) if options is not None else None, _ptr(q_pos), _ptr(out), _ptr(lse),
                                _ptr(workspace), workspace.numel(), _stream(stream))
     _check(st, "lava_paged_decode")
+    return out, lse
+
+
+# ------------------------------------------------------------------------------ sequences that share pages
+def lava_beam_step_workspace_bytes(batch: int, beams: int, vocab: int, n_out: int) -> int:
+    return int(lib.lava_beam_step_workspace_bytes(int(batch), int(beams), int(vocab), int(n_out)))
+
+
+def lava_beam_step(logits: torch.Tensor, scores: torch.Tensor, n_out: Optional[int] = None, done: Optional[torch.Tensor] = None,
+                   end_token: int = -1, pad_token: int = 0, parents=None, tokens=None, scores_out=None, done_out=None,
+                   sources: Optional[torch.Tensor] = None, workspace=None, stream=None):
+    """The best n_out (None: as many as there are) continuations of every group of beams: logits [batch, beams, V] float32 or bfloat16 (rows of
+    any distance), scores [batch, beams] float32, done [batch, beams] int32 or None.  sources [n_tables, batch * n_out] int32, if given, receives the
+    parents for a state that holds n_tables layers as sequences of their own.  Returns (parents, tokens, scores_out, done_out), each
+    [batch, n_out]; parents are rows b * beams + i, what lava_page_fork takes."""
+    if logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda or logits.dim() != 3 or logits.stride(2) != 1:
+        raise ValueError("logits must be a device tensor [batch, beams, V] of float32 or bfloat16 with contiguous rows")
+    batch, beams, vocab = logits.shape
+    if batch > 1 and beams > 1 and logits.stride(0) != beams * logits.stride(1):
+        raise ValueError("the rows of logits must all be the same distance apart")
+    stride = logits.stride(1) if beams > 1 else logits.stride(0)
+    _here(logits)
+    n_out = beams if n_out is None else int(n_out)
+    if _dev(scores, "scores", torch.float32).numel() != batch * beams:
+        raise ValueError("scores must be [batch, beams]")
+    if done is not None and _dev(done, "done", torch.int32).numel() != batch * beams:
+        raise ValueError("done must be [batch, beams]")
+    new = lambda dtype: _empty(batch, n_out, dtype=dtype, device=logits.device, stream=stream)
+    parents = new(torch.int32) if parents is None else parents
+    tokens = new(torch.int32) if tokens is None else tokens
+    scores_out = new(torch.float32) if scores_out is None else scores_out
+    done_out = new(torch.int32) if done_out is None else done_out
+    for name, t, dt in (("parents", parents, torch.int32), ("tokens", tokens, torch.int32), ("scores_out", scores_out, torch.float32),
+                        ("done_out", done_out, torch.int32)):
+        if _dev(t, name, dt).numel() != batch * n_out:
+            raise ValueError(f"{name} must be [batch, n_out]")
+    n_tables = 0
+    if sources is not None:
+        n_tables = _dev(sources, "sources", torch.int32).numel() // max(batch * n_out, 1)
+        if sources.numel() != n_tables * batch * n_out or n_tables < 1:
+            raise ValueError("sources must be [n_tables, batch * n_out]")
+    if workspace is None:
+        need = lava_beam_step_workspace_bytes(batch, beams, vocab, n_out)
+        workspace = _empty(max(need, 256), dtype=torch.uint8, device=logits.device, stream=stream)
+    st = lib.lava_beam_step(LAVA_BF16 if logits.dtype == torch.bfloat16 else LAVA_F32, batch, beams, vocab, _ptr(logits), stride, _ptr(scores),
+                            _ptr(done), int(end_token), int(pad_token), n_out, _ptr(parents), _ptr(tokens), _ptr(scores_out), _ptr(done_out),
+                            _ptr(sources), n_tables, _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "lava_beam_step")
+    return parents, tokens, scores_out, done_out
+
+
+def lava_page_fork_workspace_bytes(batch: int, n_kv_heads: int, max_blocks: int, n_pages: int) -> int:
+    return int(lib.lava_page_fork_workspace_bytes(int(batch), int(n_kv_heads), int(max_blocks), int(n_pages)))
+
+
+def _change_tensors(desc: LayerDesc, pool: PagePool, state: PageState, block_table_out, free_pages_out, workspace, stream):
+    """The checks of a change of a state's sequences.  Returns the workspace."""
+    pool._check(desc)
+    _here(state.block_table)
+    if (state.n_kv_heads, state.max_blocks, state.n_pages, state.page_rows) != (desc.n_kv_heads, pool.max_blocks, *pool.k.shape[:2]):
+        raise ValueError("the state's heads, blocks or pages are not those of the descriptor and the pool")
+    for name, t, n in (("block_table_out", block_table_out, state.block_table.numel()), ("free_pages_out", free_pages_out, state.n_pages)):
+        if t is not None and _dev(t, name, torch.int32).numel() != n:
+            raise ValueError(f"{name} must hold {n} values")
+    if workspace is None:
+        need = lava_page_fork_workspace_bytes(state.batch, state.n_kv_heads, state.max_blocks, state.n_pages)
+        workspace = _empty(max(need, 256), dtype=torch.uint8, device=state.block_table.device, stream=stream)
+    return workspace
+
+
+def lava_page_fork(desc: LayerDesc, pool: PagePool, state: PageState, source: torch.Tensor, block_table_out: Optional[torch.Tensor] = None,
+                   free_pages_out: Optional[torch.Tensor] = None, workspace=None, stream=None) -> None:
+    """Sequence b of the state becomes what sequence source[b] was ([batch] int32; -1: empty); full pages are shared.  In place, or into
+    block_table_out / free_pages_out and the state's *_out tensors."""
+    workspace = _change_tensors(desc, pool, state, block_table_out, free_pages_out, workspace, stream)
+    if _dev(source, "source", torch.int32).numel() != state.batch:
+        raise ValueError("source must be [batch]")
+    st = lib.lava_page_fork(ctypes.byref(desc), pool._ref, state.batch, state._ref, _ptr(source), _ptr(block_table_out), _ptr(free_pages_out),
+                            _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "lava_page_fork")
+
+
+def lava_page_compact(desc: LayerDesc, pool: PagePool, state: PageState, head_counts: torch.Tensor, kept_idx: torch.Tensor,
+                      evict: Optional[torch.Tensor] = None, block_table_out: Optional[torch.Tensor] = None,
+                      free_pages_out: Optional[torch.Tensor] = None, workspace=None, stream=None) -> None:
+    """Every head of the sequences with evict[b] != 0 (None: of all) keeps head_counts[b, g] of its rows: kept_idx [batch, capacity] int32, a
+    sequence's heads one after another, ascending in each.  In place, or into the outputs as for lava_page_fork."""
+    workspace = _change_tensors(desc, pool, state, block_table_out, free_pages_out, workspace, stream)
+    if _dev(head_counts, "head_counts", torch.int32).numel() != state.batch * state.n_kv_heads:
+        raise ValueError("head_counts must be [batch, H_kv]")
+    if _dev(kept_idx, "kept_idx", torch.int32).dim() != 2 or kept_idx.shape[0] != state.batch:
+        raise ValueError("kept_idx must be [batch, capacity]")
+    if evict is not None and _dev(evict, "evict", torch.int32).numel() != state.batch:
+        raise ValueError("evict must be [batch]")
+    st = lib.lava_page_compact(ctypes.byref(desc), pool._ref, state.batch, state._ref, _ptr(head_counts), _ptr(kept_idx), kept_idx.shape[1],
+                               _ptr(evict), _ptr(block_table_out), _ptr(free_pages_out), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "lava_page_compact")
+
+
+def lava_shared_decode_workspace_bytes(desc: LayerDesc, batch: int, max_blocks: int) -> int:
+    return int(lib.lava_shared_decode_workspace_bytes(ctypes.byref(desc), int(batch), int(max_blocks)))
+
+
+def lava_shared_decode(desc: LayerDesc, q: torch.Tensor, pool: PagePool, block_table: torch.Tensor, head_rows: torch.Tensor,
+                       group_start: torch.Tensor, options: Optional[DecodeOptions] = None, q_pos: Optional[torch.Tensor] = None, out=None,
+                       lse=None, workspace=None, stream=None):
+    """lava_paged_decode for groups of sequences (group i is group_start[i] .. group_start[i + 1] - 1, [n_groups + 1] int32): pages that a group's
+    tables begin with alike are read once for all of it.  Returns (out, lse)."""
+    batch, out, lse = _decode_tensors(desc, q, pool, block_table, head_rows, options, q_pos, out, lse, stream)
+    if _dev(group_start, "group_start", torch.int32).numel() < 2:
+        raise ValueError("group_start must be [n_groups + 1]")
+    if workspace is None:
+        need = lava_shared_decode_workspace_bytes(desc, batch, pool.max_blocks)
+        workspace = _empty(max(need, 256), dtype=torch.uint8, device=q.device, stream=stream)
+    st = lib.lava_shared_decode(ctypes.byref(desc), batch, _ptr(q), pool._ref, _ptr(block_table), _ptr(head_rows), group_start.numel() - 1,
+                                _ptr(group_start), ctypes.byref(options) if options is not None else None, _ptr(q_pos), _ptr(out),
+                                _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "lava_shared_decode")
     return out, lse
 
 
