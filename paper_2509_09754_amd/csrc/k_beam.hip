@@ -8,8 +8,10 @@
 //   pick   a workgroup per group of beams: sums over the parts in order, candidates of all parts, ranked the same way.
 // Which thread holds which token does not depend on where the row begins, so equal rows have equal sums, bit for bit.
 //
-// Exponentials: 2^y = 2^rint(y) p(y - rint(y)), p the Taylor polynomial of 2^f of degree 10, |f| <= 1/2: left out is less than
-// (ln 2 / 2)^11 / 11! < 3e-13 of it.  14 64-bit instructions a token, at the rate of 32-bit ones on this device.
+// Exponentials: e^x = 2^n e^f, n = rint(x log2 e), |f| <= ln 2 / 2, e^f by the polynomial of degree 7 whose largest relative error, 4.1e-11,
+// is the least (coefficients by Remez's exchange).  15 64-bit instructions a token, at the rate of 32-bit ones on this
+// device (2.4 ns a wavefront); with the polynomial of Taylor's series to degree 10, its exponent by ldexp and bounds from 64 readlanes a
+// wavefront 64 groups of 8 beams over 131072 tokens took 85 us.
 #include "common.h"
 #include "decode_parts.h"
 #include "tile_ring.h"
@@ -41,24 +43,23 @@ __device__ __forceinline__ float key_logit(unsigned long long key) {
 }
 __device__ __forceinline__ unsigned int key_token(unsigned long long key) { return 0xffffffffu - (unsigned int)key; }
 
-// 2^y for y <= 0 (smaller than -1100: zero).
-__device__ __forceinline__ double exp2_of(double y) {
-  y = y > -1100.0 ? y : -1100.0;
-  const double n = __builtin_rint(y), f = y - n;
-  double p = 7.0549116208011232e-9;            // (ln 2)^10 / 10!
-  p = fma(p, f, 1.0178086009239699e-7);
-  p = fma(p, f, 1.3215486790144309e-6);
-  p = fma(p, f, 1.5252733804059840e-5);
-  p = fma(p, f, 1.5403530393381609e-4);
-  p = fma(p, f, 1.3333558146428443e-3);
-  p = fma(p, f, 9.6181291076284771e-3);
-  p = fma(p, f, 5.5504108664821580e-2);
-  p = fma(p, f, 2.4022650695910071e-1);
-  p = fma(p, f, 6.9314718055994531e-1);
-  p = fma(p, f, 1.0);
-  return __builtin_ldexp(p, (int)n);
+// e^x for -700 <= x <= 0 (x below that: 10^-304, nothing beside the largest term, 1).  n log2 e + 1.5 * 2^52 has n in its last bits.
+constexpr double kLog2e64 = 1.4426950408889634074, kLn2_64 = 0.69314718055994530942, kRound = 6755399441055744.0;
+__device__ __forceinline__ double exp_of(double x) {
+  x = fmax(x, -700.0);                                         // (NaN gives a number: whoever calls it looks for NaN by himself)
+  const double t = fma(x, kLog2e64, kRound), n = t - kRound, f = fma(n, -kLn2_64, x);
+  double p = 1.9775171620129632e-4;
+  p = fma(p, f, 1.394818332942066e-3);
+  p = fma(p, f, 8.3335610901591351e-3);
+  p = fma(p, f, 4.1666225425460175e-2);
+  p = fma(p, f, 1.6666665126137725e-1);
+  p = fma(p, f, 5.0000001045362352e-1);
+  p = fma(p, f, 1.0000000002430967);
+  p = fma(p, f, 9.9999999996168187e-1);
+  unsigned int hi = (unsigned int)(__double_as_longlong(p) >> 32);   // n to the exponent: one instruction, which the compiler makes five of
+  asm("v_lshl_add_u32 %0, %1, 20, %0" : "+v"(hi) : "v"((unsigned int)__double_as_longlong(t)));
+  return __hiloint2double((int)hi, (int)__double_as_longlong(p));
 }
-constexpr double kLog2e64 = 1.4426950408889634074;
 
 struct alignas(2) Bf16x8 { unsigned short x[8]; };
 struct alignas(4) F32x4 { float x[4]; };
@@ -68,17 +69,30 @@ __device__ __forceinline__ bool is_live(const BeamArgs& b, int row) {
   return isfinite(b.scores[row]) && (b.done == nullptr || b.done[row] == 0);
 }
 
-// The `count`-th largest of the lanes' values.
-__device__ __forceinline__ unsigned int nth_of_wave(unsigned int x, int count) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
+// A bound that at least `count` of the lanes' values reach: the bits from LAST on of the count-th largest.
+template <int LAST>
+__device__ __forceinline__ unsigned int bound_of_wave(unsigned int x, int count) {
+  unsigned int bound = 0u;
 #pragma unroll
-  for (int l = 0; l < 64; ++l) {
-    const unsigned int y = lane_value(x, l);
-    before += y > x || (y == x && l < lane) ? 1 : 0;
+  for (int bit = 31; bit >= LAST; --bit) {
+    const unsigned int next = bound | (1u << bit);
+    bound = __popcll(__ballot(x >= next)) >= count ? next : bound;
   }
-  const unsigned long long at = __ballot(before == count - 1);
-  return lane_value(x, __builtin_ctzll(at));
+  return bound;
+}
+
+__device__ __forceinline__ float max_over_wave(float x) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
+  return x;
+}
+
+// A candidate's rank is counted by eight lanes, each over every eighth of the others.
+constexpr int kRankLanes = 8;
+__device__ __forceinline__ int sum_of_ranks(int x) {
+#pragma unroll
+  for (int m = 1; m < kRankLanes; m <<= 1) x += __shfl_xor(x, m);
+  return x;
 }
 
 __device__ __forceinline__ unsigned long long max_key_of_wave(unsigned long long x) {
@@ -95,7 +109,8 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(const BeamKerne
   __shared__ unsigned long long s_list[kListed];
   __shared__ double s_sum[kBeamWaves];
   __shared__ unsigned long long s_key[kBeamWaves];
-  __shared__ unsigned int s_top[kBeamWaves], s_bound[kBeamWaves], s_bad[kBeamWaves];
+  __shared__ float s_top[kBeamWaves];
+  __shared__ unsigned int s_bound[kBeamWaves], s_bad[kBeamWaves];
   __shared__ int s_count;
   const BeamArgs& b = a.b;
   const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -139,33 +154,26 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(const BeamKerne
     bad |= !(x[i] < INFINITY);
     most = fmaxf(most, x[i]);
   }
-  const unsigned int mine = most == -INFINITY ? 0u : score_key(most);
-  const unsigned int bound = nth_of_wave(mine, b.n_out);
-  unsigned int top = mine;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const unsigned int y = (unsigned int)__shfl_xor((int)top, m);
-    top = y > top ? y : top;
-  }
+  const unsigned int bound = bound_of_wave<DT == LAVA_BF16 ? 16 : 0>(most == -INFINITY ? 0u : score_key(most), b.n_out);
+  const float of_wave = max_over_wave(most);
   const bool any_bad = __ballot(bad) != 0ull;
   if (lane == 0) {
-    s_top[wave] = top;
+    s_top[wave] = of_wave;
     s_bound[wave] = bound;
     s_bad[wave] = any_bad ? 1u : 0u;
   }
   if (threadIdx.x == 0) s_count = 0;
   __syncthreads();
-  unsigned int limit = s_bound[0], wrong = s_bad[0];
-  top = s_top[0];
+  unsigned int limit_key = s_bound[0], wrong = s_bad[0];
+  float m = s_top[0];
 #pragma unroll
   for (int w = 1; w < kBeamWaves; ++w) {
-    limit = s_bound[w] > limit ? s_bound[w] : limit;
-    top = s_top[w] > top ? s_top[w] : top;
+    limit_key = s_bound[w] > limit_key ? s_bound[w] : limit_key;
+    m = fmaxf(m, s_top[w]);
     wrong |= s_bad[w];
   }
-  limit = limit == 0u ? 1u : limit;                            // nothing is no candidate
   const long long out = (long long)row * a.parts + part;
-  if (wrong != 0u || top == 0u) {                              // uniform
+  if (wrong != 0u || m == -INFINITY) {                         // uniform
     if (threadIdx.x == 0) {
       a.sum[out] = wrong != 0u ? NAN : 0.0;
       a.top[out] = -INFINITY;
@@ -173,18 +181,20 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(const BeamKerne
     if ((int)threadIdx.x < b.n_out) a.best[out * b.n_out + threadIdx.x] = 0ull;
     return;
   }
-  const float m = key_logit((unsigned long long)top << 32);
+  // the bound as a logit; one that is no number's key, as all below -inf's: every token that can follow
+  const float lowest = -3.402823466e38f;
+  const float limit = limit_key < score_key(lowest) ? lowest : key_logit((unsigned long long)limit_key << 32);
   const double most64 = (double)m;                             // the difference first: m log2 e may be too large for its last bits to count
   double sum = 0.0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) sum += exp2_of(((double)x[i] - most64) * kLog2e64);
+  for (int i = 0; i < kPer; ++i) sum += exp_of((double)x[i] - most64);
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
   if (lane == 0) s_sum[wave] = sum;
   // the list
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const bool in = x[i] > -INFINITY && score_key(x[i]) >= limit;
+    const bool in = x[i] >= limit;
     const unsigned long long who = __ballot(in);
     if (who == 0ull) continue;
     int at = 0;
@@ -203,11 +213,13 @@ __global__ void __launch_bounds__(kBeamThreads) beam_rows_kernel(const BeamKerne
   const int count = s_count;
   unsigned long long* best = a.best + out * b.n_out;
   if (count <= kListed) {
-    for (int i = threadIdx.x; i < count; i += kBeamThreads) {
-      const unsigned long long key = s_list[i];
+    for (int i0 = 0; i0 < count; i0 += kBeamThreads / kRankLanes) {
+      const int i = i0 + (int)threadIdx.x / kRankLanes;
+      const unsigned long long key = s_list[i < count ? i : 0];
       int rank = 0;
-      for (int j = 0; j < count; ++j) rank += s_list[j] > key ? 1 : 0;
-      if (rank < b.n_out) best[rank] = key;
+      for (int j = threadIdx.x % kRankLanes; j < count; j += kRankLanes) rank += s_list[j] > key ? 1 : 0;
+      rank = sum_of_ranks(rank);
+      if (i < count && threadIdx.x % kRankLanes == 0 && rank < b.n_out) best[rank] = key;
     }
     for (int i = count + (int)threadIdx.x; i < b.n_out; i += kBeamThreads) best[i] = 0ull;
     return;
@@ -251,16 +263,28 @@ __device__ __forceinline__ bool before(const Candidate& x, const Candidate& y) {
 }
 
 constexpr int kMostBeams = 64;
-__global__ void __launch_bounds__(kBeamThreads) beam_pick_kernel(const BeamKernelArgs a) {
+constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
+constexpr int kHeld = 4;                                       // candidates that a thread keeps
+__global__ void __launch_bounds__(kPickThreads) beam_pick_kernel(const BeamKernelArgs a) {
   __shared__ Candidate s_list[kListed];
   __shared__ double s_base[kMostBeams];                        // log sum exp; NaN: no continuation
   __shared__ float s_score[kMostBeams];                        // read once: scores_out may be the same buffer
-  __shared__ Candidate s_best[kBeamWaves];
-  __shared__ unsigned int s_bound[kBeamWaves];
+  __shared__ Candidate s_best[kPickWaves];
+  __shared__ unsigned int s_bound[kPickWaves];
   __shared__ int s_over[kMostBeams], s_count;
   const BeamArgs& b = a.b;
   const int group = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int i = wave; i < b.beams; i += kBeamWaves) {
+  // the first candidates' keys are on their way while the sums are formed
+  const int each = a.parts * b.n_out, all = b.beams * each;
+  const double inv_each = 1.0 / (double)each;                  // i / each: half a candidate off the border, so the product is exact enough
+  auto beam_of = [&](int i) { return (int)(((double)i + 0.5) * inv_each); };
+  unsigned long long key[kHeld];
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    const int i = threadIdx.x + u * kPickThreads;
+    key[u] = i < all ? a.best[(long long)group * all + i] : 0ull;   // of a beam without continuations whatever is there: not used
+  }
+  for (int i = wave; i < b.beams; i += kPickWaves) {
     const int row = group * b.beams + i;
     const float score = b.scores[row];
     const bool over = b.done != nullptr && b.done[row] != 0;
@@ -268,13 +292,12 @@ __global__ void __launch_bounds__(kBeamThreads) beam_pick_kernel(const BeamKerne
     if (isfinite(score) && !over) {                            // uniform
       float m = -INFINITY;
       for (int q = lane; q < a.parts; q += 64) m = fmaxf(m, a.top[(long long)row * a.parts + q]);
-#pragma unroll
-      for (int s = 1; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+      m = max_over_wave(m);
       double sum = 0.0;
       for (int q = lane; q < a.parts; q += 64) {
         const float t = a.top[(long long)row * a.parts + q];
         const double z = a.sum[(long long)row * a.parts + q];
-        sum += isnan(z) ? z : t == -INFINITY ? 0.0 : z * exp2_of(((double)t - (double)m) * kLog2e64);
+        sum += isnan(z) ? z : t == -INFINITY ? 0.0 : z * exp_of((double)t - (double)m);
       }
 #pragma unroll
       for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
@@ -290,40 +313,48 @@ __global__ void __launch_bounds__(kBeamThreads) beam_pick_kernel(const BeamKerne
   }
   if (threadIdx.x == 0) s_count = 0;
   __syncthreads();
-  const int each = a.parts * b.n_out, all = b.beams * each;
-  auto candidate = [&](int i) {
-    Candidate r = {0ull, 0ull, i / each};
-    const int j = i - r.beam * each, row = group * b.beams + r.beam;
-    const double base = s_base[r.beam];
+  auto candidate = [&](int i, unsigned long long of) {
+    Candidate r = {0ull, 0ull, beam_of(i)};
+    const double base = s_base[r.beam], score = (double)s_score[r.beam];
     if (isnan(base)) return r;
-    const double score = (double)s_score[r.beam];
     if (s_over[r.beam] != 0) {
-      if (j != 0) return r;
+      if (i != r.beam * each) return r;
       r.c = order_of(score);
       r.key = token_key(0.0f, (unsigned int)b.pad_token);
       return r;
     }
-    r.key = a.best[(long long)row * each + j];
-    if (r.key != 0ull) r.c = order_of(score + ((double)key_logit(r.key) - base));
+    r.key = of;
+    if (of != 0ull) r.c = order_of(score + ((double)key_logit(of) - base));
     return r;
   };
-  unsigned int mine = 0u;
-  for (int i = threadIdx.x; i < all; i += kBeamThreads) {
-    const unsigned int top = (unsigned int)(candidate(i).c >> 32);
-    mine = top > mine ? top : mine;
+  auto stored = [&](int i) { return !isnan(s_base[beam_of(i)]) && s_over[beam_of(i)] == 0 ? a.best[(long long)group * all + i] : 0ull; };
+  Candidate mine[kHeld];
+  unsigned int top = 0u;
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    const int i = threadIdx.x + u * kPickThreads;
+    mine[u] = Candidate{0ull, 0ull, 0};
+    if (i < all) mine[u] = candidate(i, key[u]);
+    top = (unsigned int)(mine[u].c >> 32) > top ? (unsigned int)(mine[u].c >> 32) : top;
   }
-  const unsigned int bound = nth_of_wave(mine, b.n_out);
+  for (int i = threadIdx.x + kHeld * kPickThreads; i < all; i += kPickThreads) {
+    const unsigned int y = (unsigned int)(candidate(i, stored(i)).c >> 32);
+    top = y > top ? y : top;
+  }
+  const unsigned int bound = bound_of_wave<0>(top, b.n_out);
   if (lane == 0) s_bound[wave] = bound;
   __syncthreads();
   unsigned int limit = s_bound[0];
 #pragma unroll
-  for (int w = 1; w < kBeamWaves; ++w) limit = s_bound[w] > limit ? s_bound[w] : limit;
-  for (int i = threadIdx.x; i < all; i += kBeamThreads) {
-    const Candidate r = candidate(i);
-    if (r.c == 0ull || (unsigned int)(r.c >> 32) < limit) continue;
+  for (int w = 1; w < kPickWaves; ++w) limit = s_bound[w] > limit ? s_bound[w] : limit;
+  auto list = [&](const Candidate& r) {
+    if (r.c == 0ull || (unsigned int)(r.c >> 32) < limit) return;
     const int at = atomicAdd(&s_count, 1);
     if (at < kListed) s_list[at] = r;
-  }
+  };
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) list(mine[u]);
+  for (int i = threadIdx.x + kHeld * kPickThreads; i < all; i += kPickThreads) list(candidate(i, stored(i)));
   __syncthreads();
   const int count = s_count;
   auto write = [&](int k, const Candidate& r) {
@@ -338,20 +369,22 @@ __global__ void __launch_bounds__(kBeamThreads) beam_pick_kernel(const BeamKerne
       b.sources[(long long)t * b.batch * b.n_out + at] = none ? -1 : row + t * b.batch * b.beams;
   };
   if (count <= kListed) {
-    for (int i = threadIdx.x; i < count; i += kBeamThreads) {
-      const Candidate r = s_list[i];
+    for (int i0 = 0; i0 < count; i0 += kPickThreads / kRankLanes) {
+      const int i = i0 + (int)threadIdx.x / kRankLanes;
+      const Candidate r = s_list[i < count ? i : 0];
       int rank = 0;
-      for (int j = 0; j < count; ++j) rank += before(s_list[j], r) ? 1 : 0;
-      if (rank < b.n_out) write(rank, r);
+      for (int j = threadIdx.x % kRankLanes; j < count; j += kRankLanes) rank += before(s_list[j], r) ? 1 : 0;
+      rank = sum_of_ranks(rank);
+      if (i < count && threadIdx.x % kRankLanes == 0 && rank < b.n_out) write(rank, r);
     }
-    for (int i = count + (int)threadIdx.x; i < b.n_out; i += kBeamThreads) write(i, Candidate{0ull, 0ull, 0});
+    for (int i = count + (int)threadIdx.x; i < b.n_out; i += kPickThreads) write(i, Candidate{0ull, 0ull, 0});
     return;
   }
   Candidate last = {~0ull, ~0ull, -1};
   for (int k = 0; k < b.n_out; ++k) {
     Candidate r = {0ull, 0ull, 0};
-    for (int i = threadIdx.x; i < all; i += kBeamThreads) {
-      const Candidate y = candidate(i);
+    for (int i = threadIdx.x; i < all; i += kPickThreads) {
+      const Candidate y = candidate(i, stored(i));
       if (y.c != 0ull && before(last, y) && before(y, r)) r = y;
     }
 #pragma unroll
@@ -361,7 +394,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_pick_kernel(const BeamKerne
     }
     if (lane == 0) s_best[wave] = r;
     __syncthreads();
-    for (int w = 0; w < kBeamWaves; ++w)
+    for (int w = 0; w < kPickWaves; ++w)
       if (before(s_best[w], r)) r = s_best[w];
     __syncthreads();
     if (threadIdx.x == 0) write(k, r);
@@ -403,7 +436,7 @@ int32_t launch_beam_step(const BeamArgs& b, int32_t dtype, void* ws, hipStream_t
     hipLaunchKernelGGL(beam_rows_kernel<LAVA_F32>, dim3(wgs), dim3(kBeamThreads), 0, s, a);
   const int32_t st = launch_status();
   if (st != LAVA_OK) return st;
-  hipLaunchKernelGGL(beam_pick_kernel, dim3((unsigned)b.batch), dim3(kBeamThreads), 0, s, a);
+  hipLaunchKernelGGL(beam_pick_kernel, dim3((unsigned)b.batch), dim3(kPickThreads), 0, s, a);
   return launch_status();
 }
 

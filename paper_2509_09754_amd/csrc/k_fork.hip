@@ -5,99 +5,103 @@
 // last one where the head keeps all rows of a last page that was not full and is the copy that goes on with it.  The blocks
 // behind them go to fresh pages, whose rows are copied.  A page is free afterwards if no new table names it.
 //
-// Who holds a page is found out by marking, one word a page: a new table's leading blocks store 0, an old table's blocks that
-// do not stay take the minimum with 1 + the head's number.  What is left at 1 + h was first named by head h and is in no new
-// table: head h gives it back, so that the stack's order does not depend on the order of the marks.
+// Who holds a page is found out by marking, two words a page: a new table's leading blocks store `alive`, an old table's blocks that
+// do not stay take the minimum with 1 + the head's number in `first`.  A page that is not alive was first named by head
+// first - 1, which gives it back, so that the stack's order does not depend on the order of the marks.
 //
-// Four launches, since each needs all of what the one before found: clear the marks; mark, and sum the fresh pages over the heads
-// (a wavefront a head, partial sums by workgroup); count what goes back, and take the fresh pages off the stack; write tables,
-// counts, stack, and copy rows.  What the last launch reads of buffers that it also writes was set aside before.
+// Each step needs all of what the one before found: clear the marks; mark, and sum the fresh pages over the heads (a
+// wavefront a head, partial sums by workgroup); count what goes back, and take the fresh pages off the stack; write tables,
+// counts, stack, and copy rows, the fresh pages' rows in one line that the workgroups share evenly.  What the last step
+// reads of buffers that it also writes was set aside before.  The first three are one launch of one workgroup where tables are few
+// and short (kOneEntries), which clears only the words of pages that are named.
 //
 // Bound by the chain of launches for a beam step (one layer of eight beams), by HBM for many rows.
 #include "common.h"
 #include "decode_parts.h"
 #include "tile_ring.h"
+#include "xblock.h"
 
 namespace lava {
 
 namespace {
 
-constexpr int kChangeWaves = 16, kChangeThreads = kChangeWaves * 64;
+constexpr int kChangeWaves = 4, kChangeThreads = kChangeWaves * 64;   // of a workgroup that sums over heads
 constexpr int kMostGroups = 1024;             // workgroups of a launch that sums over heads
 constexpr unsigned int kNoHolder = 0xffffffffu;
 
 struct ChangeHeader {
   int error;                                  // LAVA_PAGES_* bits
-  int n_free;
+  int n_free, fresh, back;                    // free pages before, pages taken, pages given back
+};
+
+struct __attribute__((aligned(16))) HeadPlan {
+  int n, stay;                                // rows, and leading blocks that stay, after the call
+  int from, old;                              // head that it comes from (-1: none), rows that one held
+  long long list;                             // first entry of its list in the sequence's, -1: it keeps all rows
+  int fresh_at, back_at;                      // pages taken by the heads before it; given back by those (of its workgroup) before it
 };
 
 struct ChangeArgs {
   PageChangeArgs p;
   ChangeHeader* head;
   int *fresh_total, *back_total;              // [kMostGroups] of a workgroup's heads
-  int* keeper;                                // [batch] non-zero: the sequence goes on with its source's last pages
-  int *seq_src, *seq_pos;                     // [batch] source (-1: none), position after the call
-  int *old_rows, *n_new, *stay, *fresh_at, *back_at;     // [heads] rows before, rows and leading blocks after; sums of the heads of the workgroup before
-  long long* list_at;                         // [heads] first entry of the head's list in the sequence's, -1: the head keeps all rows
-  unsigned int* mark;                         // [n_pages]
-  int* taken;                                 // [n_pages] fresh pages in order
+  int* seq_pos;                               // [batch] position after the call
+  int* old_rows;                              // [heads]
+  HeadPlan* plan;                             // [heads]
+  unsigned int *alive, *first;                // [n_pages]
+  int *taken, *owner;                         // [n_pages] fresh pages in order, the heads that take them
   int* old_table;                             // [heads][max_blocks] a copy, if the tables change in place
-  int heads, per;                             // heads in all, heads a wavefront
+  int heads, per;                             // heads in all, heads a wavefront that sums
+  int one;                                    // the marks are one workgroup's
 };
 
 struct ChangeLayout {
-  size_t off_fresh, off_back, off_keeper, off_src, off_pos, off_heads, off_list, off_mark, off_taken, off_table, bytes;
+  size_t off_fresh, off_back, off_pos, off_rows, off_plan, off_alive, off_first, off_taken, off_owner, off_table, bytes;
 };
 ChangeLayout change_layout(int batch, int n_kv_heads, int max_blocks, long long n_pages) {
   ChangeLayout l;
-  const size_t heads = (size_t)batch * n_kv_heads;
+  const size_t heads = (size_t)batch * n_kv_heads, pages = align_up((size_t)n_pages * 4);
   l.off_fresh = align_up(sizeof(ChangeHeader));
   l.off_back = l.off_fresh + align_up(kMostGroups * 4);
-  l.off_keeper = l.off_back + align_up(kMostGroups * 4);
-  l.off_src = l.off_keeper + align_up((size_t)batch * 4);
-  l.off_pos = l.off_src + align_up((size_t)batch * 4);
-  l.off_heads = l.off_pos + align_up((size_t)batch * 4);
-  l.off_list = l.off_heads + 5 * align_up(heads * 4);
-  l.off_mark = l.off_list + align_up(heads * 8);
-  l.off_taken = l.off_mark + align_up((size_t)n_pages * 4);
-  l.off_table = l.off_taken + align_up((size_t)n_pages * 4);
+  l.off_pos = l.off_back + align_up(kMostGroups * 4);
+  l.off_rows = l.off_pos + align_up((size_t)batch * 4);
+  l.off_plan = l.off_rows + align_up(heads * 4);
+  l.off_alive = l.off_plan + align_up(heads * sizeof(HeadPlan));
+  l.off_first = l.off_alive + pages;
+  l.off_taken = l.off_first + pages;
+  l.off_owner = l.off_taken + pages;
+  l.off_table = l.off_owner + pages;
   l.bytes = l.off_table + align_up(heads * max_blocks * 4);
   return l;
 }
 
-// ---------------------------------------------------------------- 1: clear; who goes on with the last page of a sequence
-__global__ void __launch_bounds__(256) change_begin_kernel(const ChangeArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long long step = (long long)gridDim.x * 256;
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.head->error = 0;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < a.p.n_pages; i += step) a.mark[i] = kNoHolder;
-  if (a.p.source == nullptr) return;
-  const int waves = (int)(step / 64);
-  for (int b = blockIdx.x * 4 + (threadIdx.x >> 6); b < a.p.batch; b += waves) {     // a wavefront a sequence
-    const int s = a.p.source[b];
-    bool first = s >= 0 && s < a.p.batch;
-    if (first && s != b) {
-      first = a.p.source[s] != s;
-      for (int c0 = 0; first && c0 < b; c0 += 64) first = __ballot(c0 + lane < b && a.p.source[c0 + lane] == s) == 0ull;
-    }
-    if (lane == 0) a.keeper[b] = first ? 1 : 0;
-  }
+__device__ __forceinline__ bool is_page(const PageChangeArgs& p, int page) { return page >= 0 && page < p.n_pages; }
+
+// Rows that head h held, 0 where the count is out of range.
+__device__ __forceinline__ int rows_before(const PageChangeArgs& p, int h) {
+  const int rows = p.st.head_rows[h];
+  return rows < 0 || rows > (long long)p.max_blocks << p.page_shift ? 0 : rows;
 }
 
-// Exclusive sums over a workgroup's heads of what its wavefronts found (lane 0 wrote the sums inside the wavefront to out[h]).
-__device__ __forceinline__ void sums_of_group(const ChangeArgs& a, int* s_wave, int mine, int* out, int* totals, int h0, int h1) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (lane == 0) s_wave[wave] = mine;
-  __syncthreads();
-  int before = 0, all = 0;
+__device__ __forceinline__ int blocks_of(const PageChangeArgs& p, int rows) {
+  return (int)(((long long)rows + (1 << p.page_shift) - 1) >> p.page_shift);
+}
+
+// Does sequence b go on with the last pages of sequence s, which it is made of?  A wavefront's question.
+__device__ __forceinline__ bool is_keeper(const PageChangeArgs& p, int b, int s) {
+  if (p.source == nullptr || s == b) return true;
+  if (s < 0 || p.source[s] == s) return false;
+  const int lane = threadIdx.x & 63;
+  for (int c0 = 0; c0 < b; c0 += 512) {
+    bool same = false;
 #pragma unroll
-  for (int w = 0; w < kChangeWaves; ++w) {
-    before += w < wave ? s_wave[w] : 0;
-    all += s_wave[w];
+    for (int u = 0; u < 8; ++u) {
+      const int c = c0 + 64 * u + lane;
+      same |= c < b && p.source[c < b ? c : b] == s;
+    }
+    if (__ballot(same) != 0ull) return false;
   }
-  if (lane == 0 && before != 0)
-    for (int h = h0; h < h1; ++h) out[h] += before;
-  if (threadIdx.x == 0) totals[blockIdx.x] = all;
+  return true;
 }
 
 // The first t in [0, n) with list[t] != t, n if there is none; the list ascends.
@@ -120,83 +124,125 @@ __device__ __forceinline__ int leading_same(const int* list, int n) {
   return lo;
 }
 
-// ---------------------------------------------------------------- 2: what every head keeps; marks; sums of the fresh pages
-__global__ void __launch_bounds__(kChangeThreads) change_mark_kernel(const ChangeArgs a) {
-  __shared__ int s_wave[kChangeWaves];
+constexpr int kLooks = 4;                     // look-ups of a thread at a time
+
+// What head h keeps, and its marks; returns the fresh pages it needs.  A wavefront's work; error bits are or-ed to `error`.
+__device__ __forceinline__ int mark_head(const ChangeArgs& a, int h, int& error) {
   const PageChangeArgs& p = a.p;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = p.heads, P = 1 << p.page_shift;
-  const int h0 = (blockIdx.x * kChangeWaves + wave) * a.per, h1 = h0 + a.per < a.heads ? h0 + a.per : a.heads;
-  const long long most = (long long)p.max_blocks << p.page_shift;
-  int error = 0, sum = 0;
-  for (int h = h0; h < h1; ++h) {
-    const int b = h / G, g = h - b * G;
-    int rows = p.st.head_rows[h];
-    if (rows < 0 || rows > most) error = LAVA_PAGES_INVALID, rows = 0;
-    const int nb_old = (int)(((long long)rows + P - 1) >> p.page_shift);
-    int s = p.source != nullptr ? p.source[b] : b;
-    if (s < -1 || s >= p.batch) error = LAVA_PAGES_INVALID, s = -1;
-    int old = s >= 0 ? p.st.head_rows[s * G + g] : 0;
-    if (old < 0 || old > most) old = 0;                        // that head's wavefront reports it
-    int n = old, same = old;
-    long long begin = -1;
-    if (p.head_counts != nullptr && (p.evict == nullptr || p.evict[b] != 0)) {
-      int count = 0;
-      bool bad = false;
-      if (lane < G) {
-        count = p.head_counts[(long long)b * G + lane];
-        bad = count < 0 || count > p.st.head_rows[b * G + lane];
-      }
-      long long all = 0, before = 0;
-      for (int i = 0; i < G; ++i) {
-        const int c = (int)lane_value((unsigned int)count, i);
-        before += i < g ? c : 0;
-        all += c;
-      }
-      if (__ballot(bad) != 0ull || all > p.kept_capacity) {
-        error = LAVA_PAGES_INVALID;
-        n = same = 0;
-      } else {
-        n = (int)lane_value((unsigned int)count, g);
-        begin = before;
-        same = leading_same(p.kept_idx + (long long)b * p.kept_capacity + begin, n);
-      }
+  const int lane = threadIdx.x & 63, G = p.heads, P = 1 << p.page_shift, b = h / G, g = h - b * G;
+  const int rows = rows_before(p, h), nb_old = blocks_of(p, rows);
+  if (p.st.head_rows[h] != rows) error |= LAVA_PAGES_INVALID;
+  int s = p.source != nullptr ? p.source[b] : b;
+  if (s < -1 || s >= p.batch) error |= LAVA_PAGES_INVALID, s = -1;
+  const int old = s >= 0 ? rows_before(p, s * G + g) : 0;
+  int n = old, same = old;
+  long long begin = -1;
+  if (p.head_counts != nullptr && (p.evict == nullptr || p.evict[b] != 0)) {
+    int count = 0;
+    bool bad = false;
+    if (lane < G) {
+      count = p.head_counts[(long long)b * G + lane];
+      bad = count < 0 || count > p.st.head_rows[b * G + lane];
     }
-    int stay = same >> p.page_shift;
-    if ((n & (P - 1)) != 0 && same >= n && (old & (P - 1)) != 0 && n >> p.page_shift == old >> p.page_shift &&
-        (p.source == nullptr || a.keeper[b] != 0))
-      ++stay;
-    const int* mine = p.st.block_table + (long long)h * p.max_blocks;
-    if (s >= 0) {
-      const int* from = p.st.block_table + ((long long)s * G + g) * p.max_blocks;
-      for (int j = lane; j < stay; j += 64) {
-        const int page = from[j];
-        if (page < 0 || page >= p.n_pages) error = LAVA_PAGES_INVALID;
-        else __hip_atomic_store(&a.mark[page], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
+    long long all = 0, before = 0;
+    for (int i = 0; i < G; ++i) {
+      const int c = (int)lane_value((unsigned int)count, i);
+      before += i < g ? c : 0;
+      all += c;
     }
-    const int kept = s == b ? stay : 0;                        // leading blocks that this head marks itself
-    for (int j = lane; j < nb_old; j += 64) {
-      const int page = mine[j];
-      if (a.old_table != nullptr) a.old_table[(long long)h * p.max_blocks + j] = page;
-      if (j < kept) continue;
-      if (page < 0 || page >= p.n_pages) error = LAVA_PAGES_INVALID;
-      else __hip_atomic_fetch_min(&a.mark[page], 1u + (unsigned int)h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__ballot(bad) != 0ull || all > p.kept_capacity) {
+      error |= LAVA_PAGES_INVALID;
+      n = same = 0;
+    } else {
+      n = (int)lane_value((unsigned int)count, g);
+      begin = before;
+      same = leading_same(p.kept_idx + (long long)b * p.kept_capacity + begin, n);
     }
-    if (lane == 0) {
-      a.old_rows[h] = rows;
-      a.n_new[h] = n;
-      a.stay[h] = stay;
-      a.list_at[h] = begin;
-      a.fresh_at[h] = sum;
-      if (g == 0) {
-        a.seq_src[b] = s;
-        a.seq_pos[b] = s >= 0 ? p.st.seq_pos[s] : 0;
-      }
-    }
-    sum += (int)(((long long)n + P - 1) >> p.page_shift) - stay;
   }
-  if (error != 0) atomicOr(&a.head->error, error);
-  sums_of_group(a, s_wave, sum, a.fresh_at, a.fresh_total, h0, h1);
+  int stay = same >> p.page_shift;
+  if ((n & (P - 1)) != 0 && same >= n && (old & (P - 1)) != 0 && n >> p.page_shift == old >> p.page_shift && is_keeper(p, b, s)) ++stay;
+  if (s >= 0) {
+    const int* from = p.st.block_table + ((long long)s * G + g) * p.max_blocks;
+    for (int j0 = lane; j0 < stay; j0 += 64 * kLooks) {
+      int page[kLooks];
+#pragma unroll
+      for (int u = 0; u < kLooks; ++u) page[u] = j0 + 64 * u < stay ? from[j0 + 64 * u] : 0;
+#pragma unroll
+      for (int u = 0; u < kLooks; ++u) {
+        if (!is_page(p, page[u])) error |= LAVA_PAGES_INVALID;
+        else if (j0 + 64 * u < stay) a.alive[page[u]] = 1u;
+      }
+    }
+  }
+  const int* mine = p.st.block_table + (long long)h * p.max_blocks;
+  const int kept = s == b ? stay : 0;                          // leading blocks that this head marked itself
+  for (int j0 = (a.old_table != nullptr ? 0 : kept) + lane; j0 < nb_old; j0 += 64 * kLooks) {
+    int page[kLooks];
+#pragma unroll
+    for (int u = 0; u < kLooks; ++u) page[u] = j0 + 64 * u < nb_old ? mine[j0 + 64 * u] : 0;
+#pragma unroll
+    for (int u = 0; u < kLooks; ++u) {
+      const int j = j0 + 64 * u;
+      if (j >= nb_old) continue;
+      if (a.old_table != nullptr) a.old_table[(long long)h * p.max_blocks + j] = page[u];
+      if (j < kept) continue;
+      if (is_page(p, page[u])) __hip_atomic_fetch_min(&a.first[page[u]], 1u + (unsigned int)h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      else error |= LAVA_PAGES_INVALID;
+    }
+  }
+  if (lane == 0) {
+    a.old_rows[h] = rows;
+    HeadPlan& x = a.plan[h];
+    x.n = n;
+    x.stay = stay;
+    x.from = s >= 0 ? s * G + g : -1;
+    x.old = old;
+    x.list = begin;
+    if (g == 0) a.seq_pos[b] = s >= 0 ? p.st.seq_pos[s] : 0;
+  }
+  return blocks_of(p, n) - stay;
+}
+
+// Pages that head h gives back.  `use(page, how many before it)` for each, in the order of the blocks; a wavefront's work.
+template <typename F>
+__device__ __forceinline__ int for_each_gone(const ChangeArgs& a, int h, const int* table, F use) {
+  const int lane = threadIdx.x & 63, nb_old = blocks_of(a.p, a.old_rows[h]);
+  int n = 0;
+  for (int j0 = a.plan[h].from == h ? a.plan[h].stay : 0; j0 < nb_old; j0 += 64 * kLooks) {
+    int page[kLooks];
+    unsigned int first[kLooks], alive[kLooks];
+#pragma unroll
+    for (int u = 0; u < kLooks; ++u) page[u] = j0 + 64 * u + lane < nb_old ? table[j0 + 64 * u + lane] : -1;
+#pragma unroll
+    for (int u = 0; u < kLooks; ++u) {
+      const bool there = is_page(a.p, page[u]);
+      first[u] = there ? a.first[page[u]] : kNoHolder;
+      alive[u] = there ? a.alive[page[u]] : 1u;
+    }
+#pragma unroll
+    for (int u = 0; u < kLooks; ++u) {
+      const bool gone = first[u] == 1u + (unsigned int)h && alive[u] == 0u;
+      const unsigned long long all = __ballot(gone);
+      if (gone) use(page[u], n + __popcll(all & ((1ull << lane) - 1ull)));
+      n += __popcll(all);
+    }
+  }
+  return n;
+}
+
+// The sum of the wavefronts' values (y) and of those before this one (x).
+__device__ __forceinline__ int2 sums_of_group(int* s_wave, int mine) {
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) s_wave[wave] = mine;
+  __syncthreads();
+  int2 r = make_int2(0, 0);
+#pragma unroll
+  for (int w = 0; w < kChangeWaves; ++w) {
+    r.x += w < wave ? s_wave[w] : 0;
+    r.y += s_wave[w];
+  }
+  __syncthreads();
+  return r;
 }
 
 // Sums of the workgroups' totals in front of workgroup `group` (x) and of all (y), in every thread of a workgroup.
@@ -226,117 +272,299 @@ __device__ __forceinline__ int2 sum_totals(const int* totals, int groups, int gr
   return r;
 }
 
+// The fresh pages, off the stack: every `step`th from `from` on.  Returns error bits.
+__device__ __forceinline__ int take_pages(const ChangeArgs& a, int n_free, int fresh, int from, int step) {
+  if (n_free < 0 || n_free > a.p.n_pages || fresh > n_free) return 0;    // found out again when tables are written
+  int error = 0;
+  for (int k = from; k < fresh; k += step) {
+    const int page = a.p.st.free_pages[n_free - 1 - k];
+    if (!is_page(a.p, page)) error = LAVA_PAGES_INVALID;
+    a.taken[k] = page;
+  }
+  return error;
+}
+
+// ---------------------------------------------------------------- 1: clear
+__global__ void __launch_bounds__(256) change_begin_kernel(const ChangeArgs a) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    a.head->error = 0;
+    a.head->back = 0;
+  }
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < a.p.n_pages; i += (long long)gridDim.x * 256) {
+    a.alive[i] = 0u;
+    a.first[i] = kNoHolder;
+  }
+}
+
+// ---------------------------------------------------------------- 2: what every head keeps; marks; sums of the fresh pages
+__global__ void __launch_bounds__(kChangeThreads) change_mark_kernel(const ChangeArgs a) {
+  __shared__ int s_wave[kChangeWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int h0 = (blockIdx.x * kChangeWaves + wave) * a.per, h1 = h0 + a.per < a.heads ? h0 + a.per : a.heads;
+  int error = 0, sum = 0;
+  for (int h = h0; h < h1; ++h) {
+    const int fresh = mark_head(a, h, error);
+    if (lane == 0) a.plan[h].fresh_at = sum;
+    sum += fresh;
+  }
+  if (error != 0) atomicOr(&a.head->error, error);
+  const int2 all = sums_of_group(s_wave, sum);
+  if (lane == 0)
+    for (int h = h0; h < h1; ++h) a.plan[h].fresh_at += all.x;
+  if (threadIdx.x == 0) a.fresh_total[blockIdx.x] = all.y;
+}
+
 // ---------------------------------------------------------------- 3: sums of what goes back; the fresh pages
 __global__ void __launch_bounds__(kChangeThreads) change_count_kernel(const ChangeArgs a) {
   __shared__ int s_wave[kChangeWaves], s_sum[2 * kChangeWaves];
   const PageChangeArgs& p = a.p;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = p.heads;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int h0 = (blockIdx.x * kChangeWaves + wave) * a.per, h1 = h0 + a.per < a.heads ? h0 + a.per : a.heads;
+  const int2 fresh = sum_totals<kChangeThreads>(a.fresh_total, gridDim.x, blockIdx.x, s_sum);
+  const int n_free = p.st.n_free[0];
+  const bool enough = n_free >= 0 && n_free <= p.n_pages && fresh.y <= n_free;
   int sum = 0;
   for (int h = h0; h < h1; ++h) {
-    const int b = h / G, nb_old = (int)(((long long)a.old_rows[h] + (1 << p.page_shift) - 1) >> p.page_shift), first = a.seq_src[b] == b ? a.stay[h] : 0;
-    const int* table = p.st.block_table + (long long)h * p.max_blocks;
-    int n = 0;
-    for (int j0 = first; j0 < nb_old; j0 += 64) {
-      const int j = j0 + lane, page = j < nb_old ? table[j] : -1;
-      n += __popcll(__ballot(page >= 0 && page < p.n_pages && a.mark[page] == 1u + (unsigned int)h));
+    const int n = for_each_gone(a, h, p.st.block_table + (long long)h * p.max_blocks, [](int, int) {});
+    const int at = a.plan[h].fresh_at + fresh.x, need = blocks_of(p, a.plan[h].n) - a.plan[h].stay;
+    for (int j = lane; enough && j < need; j += 64) a.owner[at + j] = h;
+    if (lane == 0) {
+      a.plan[h].back_at = sum;
+      a.plan[h].fresh_at = at;
     }
-    if (lane == 0) a.back_at[h] = sum;
     sum += n;
   }
-  sums_of_group(a, s_wave, sum, a.back_at, a.back_total, h0, h1);
-  const int fresh = sum_totals<kChangeThreads>(a.fresh_total, gridDim.x, 0, s_sum).y, n_free = p.st.n_free[0];
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.head->n_free = n_free;
-  if (n_free < 0 || n_free > p.n_pages || fresh > n_free) return;
-  for (int k = blockIdx.x * kChangeThreads + threadIdx.x; k < fresh; k += gridDim.x * kChangeThreads) {
-    const int page = p.st.free_pages[n_free - 1 - k];
-    if (page < 0 || page >= p.n_pages) atomicOr(&a.head->error, LAVA_PAGES_INVALID);
-    a.taken[k] = page;
+  const int2 all = sums_of_group(s_wave, sum);
+  if (lane == 0)
+    for (int h = h0; h < h1; ++h) a.plan[h].back_at += all.x;
+  if (threadIdx.x == 0) {
+    a.back_total[blockIdx.x] = all.y;
+    if (all.y != 0) atomicAdd(&a.head->back, all.y);
+    if (blockIdx.x == 0) {
+      a.head->n_free = n_free;
+      a.head->fresh = fresh.y;
+    }
+  }
+  const int error = take_pages(a, n_free, fresh.y, blockIdx.x * kChangeThreads + threadIdx.x, gridDim.x * kChangeThreads);
+  if (error != 0) atomicOr(&a.head->error, error);
+}
+
+// ---------------------------------------------------------------- 1 to 3 by one workgroup
+// Every thread has up to kOnePer entries of the tables, whose look-ups are independent of each other.  A list's blocks stay as long as
+// their last rows are where they were, since it ascends.
+constexpr int kOneThreads = 1024, kOneHeads = 256, kOnePer = 8, kOneEntries = kOnePer * kOneThreads;
+__global__ void __launch_bounds__(kOneThreads) change_one_kernel(const ChangeArgs a) {
+  __shared__ int s_rows[kOneHeads], s_count[kOneHeads], s_source[kOneHeads], s_n[kOneHeads], s_stay[kOneHeads], s_from[kOneHeads];
+  __shared__ int s_need[kOneHeads], s_back[kOneHeads], s_whole[kOneHeads], s_error, s_total[2];
+  __shared__ long long s_list[kOneHeads];
+  const PageChangeArgs& p = a.p;
+  const int lane = threadIdx.x & 63, h = threadIdx.x, G = p.heads, P = 1 << p.page_shift, W = p.max_blocks, heads = a.heads;
+  const bool is_head = h < heads;
+  const int b = is_head ? h / G : 0, g = h - b * G;
+  if (threadIdx.x == 0) s_error = 0;
+  const int n_free = p.st.n_free[0];
+  int error = 0, entry_page[kOnePer], entry_head[kOnePer], entry_block[kOnePer];
+  const double inv_w = 1.0 / (double)W;                        // e / W: half an entry off the border, so the product is exact enough
+#pragma unroll
+  for (int u = 0; u < kOnePer; ++u) {
+    const int e = u * kOneThreads + (int)threadIdx.x;
+    entry_head[u] = e < heads * W ? (int)(((double)e + 0.5) * inv_w) : -1;
+    entry_block[u] = e - entry_head[u] * W;
+    entry_page[u] = entry_head[u] >= 0 ? p.st.block_table[e] : -1;   // behind a head's last block whatever is there: not used
+  }
+  if (is_head) {
+    const int rows = rows_before(p, h);
+    if (p.st.head_rows[h] != rows) error = LAVA_PAGES_INVALID;
+    s_rows[h] = rows;
+    s_count[h] = p.head_counts != nullptr ? p.head_counts[h] : 0;
+    s_back[h] = 0;
+    if (h < p.batch) {
+      int s = p.source != nullptr ? p.source[h] : h;
+      if (s < -1 || s >= p.batch) error = LAVA_PAGES_INVALID, s = -1;
+      s_source[h] = s;
+    }
+  }
+  __syncthreads();
+  int n = 0, old = 0, s = -1;
+  long long begin = -1;
+  bool keeper = false;
+  if (is_head) {
+    s = s_source[b];
+    old = s >= 0 ? s_rows[s * G + g] : 0;
+    n = old;
+    keeper = s == b || (s >= 0 && s_source[s] != s);
+    for (int c = 0; s != b && c < b; ++c) keeper = keeper && s_source[c] != s;
+    if (p.head_counts != nullptr && (p.evict == nullptr || p.evict[b] != 0)) {
+      long long all = 0, before = 0;
+      bool bad = false;
+      for (int i = 0; i < G; ++i) {
+        const int c = s_count[b * G + i];
+        bad |= c < 0 || c > s_rows[b * G + i];
+        before += i < g ? c : 0;
+        all += c;
+      }
+      bad |= all > p.kept_capacity;
+      if (bad) error = LAVA_PAGES_INVALID;
+      n = bad ? 0 : s_count[h];
+      begin = before;
+    }
+    s_n[h] = n;
+    s_from[h] = s >= 0 ? s * G + g : -1;
+    s_list[h] = begin >= 0 ? (long long)b * p.kept_capacity + begin : -1;
+    s_stay[h] = begin >= 0 ? 0 : n >> p.page_shift;
+    s_whole[h] = begin < 0 || (n > 0 && p.kept_idx[(long long)b * p.kept_capacity + begin + n - 1] == n - 1) ? 1 : 0;
+    a.old_rows[h] = s_rows[h];
+    if (g == 0) a.seq_pos[b] = s >= 0 ? p.st.seq_pos[s] : 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kOnePer; ++u) {
+    const int x = entry_head[u], j = entry_block[u], page = entry_page[u];
+    if (x < 0) continue;
+    if (j < blocks_of(p, s_rows[x])) {
+      if (a.old_table != nullptr) a.old_table[x * W + j] = page;
+      if (is_page(p, page)) {
+        st_dev(&a.alive[page], 0u);
+        st_dev(&a.first[page], kNoHolder);
+      } else {
+        error = LAVA_PAGES_INVALID;
+      }
+    } else {
+      entry_page[u] = -1;
+    }
+    if (s_list[x] >= 0 && (long long)(j + 1) << p.page_shift <= s_n[x]) {
+      const int last = ((j + 1) << p.page_shift) - 1;
+      if (p.kept_idx[s_list[x] + last] == last) atomicAdd(&s_stay[x], 1);
+    }
+  }
+  drain_vmem();
+  __syncthreads();
+  if (is_head) {
+    if ((n & (P - 1)) != 0 && s_whole[h] != 0 && (old & (P - 1)) != 0 && n >> p.page_shift == old >> p.page_shift && keeper) s_stay[h] += 1;
+    s_need[h] = blocks_of(p, n) - s_stay[h];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kOnePer; ++u) {
+    const int x = entry_head[u], j = entry_block[u], page = entry_page[u];
+    if (x < 0) continue;
+    const int from = s_from[x], stay = s_stay[x];
+    if (from >= 0 && j < stay) {
+      const int keeps = from == x ? page : p.st.block_table[from * W + j];
+      if (is_page(p, keeps)) st_dev(&a.alive[keeps], 1u);
+    }
+    if (is_page(p, page) && (from != x || j >= stay))
+      __hip_atomic_fetch_min(&a.first[page], 1u + (unsigned int)x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  drain_vmem();
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kOnePer; ++u) {
+    const int x = entry_head[u], page = entry_page[u];
+    if (x < 0 || !is_page(p, page) || (s_from[x] == x && entry_block[u] < s_stay[x])) continue;
+    if (ld_dev(&a.first[page]) == 1u + (unsigned int)x && ld_dev(&a.alive[page]) == 0u) atomicAdd(&s_back[x], 1);
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {                                      // exclusive sums over the heads
+    int fresh = 0, back = 0;
+    for (int h0 = 0; h0 < heads; h0 += 64) {
+      const int x = h0 + lane;
+      const unsigned int f = x < heads ? (unsigned int)s_need[x] : 0u, r = x < heads ? (unsigned int)s_back[x] : 0u;
+      const unsigned int fi = wave_incl(f), ri = wave_incl(r);
+      if (x < heads) {
+        s_count[x] = fresh + (int)(fi - f);
+        s_back[x] = back + (int)(ri - r);
+      }
+      fresh += (int)lane_value(fi, 63);
+      back += (int)lane_value(ri, 63);
+    }
+    if (lane == 0) {
+      s_total[0] = fresh;
+      s_total[1] = back;
+    }
+  }
+  __syncthreads();
+  const int fresh = s_total[0];
+  if (is_head) a.plan[h] = HeadPlan{n, s_stay[h], s_from[h], old, begin, s_count[h], s_back[h]};
+  if (n_free >= 0 && n_free <= p.n_pages && fresh <= n_free) {
+#pragma unroll
+    for (int u = 0; u < kOnePer; ++u) {
+      const int x = entry_head[u], j = entry_block[u];
+      if (x >= 0 && j < s_need[x]) a.owner[s_count[x] + j] = x;
+    }
+  }
+  error |= take_pages(a, n_free, fresh, threadIdx.x, kOneThreads);
+  if (error != 0) atomicOr(&s_error, error);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    *a.head = ChangeHeader{s_error, n_free, fresh, s_total[1]};
+    a.back_total[0] = s_total[1];
   }
 }
 
 // ---------------------------------------------------------------- 4: tables, counts, stack; rows
-constexpr int kApplyThreads = 256, kRowsInFlight = 4;
-__global__ void __launch_bounds__(kApplyThreads) change_apply_kernel(const ChangeArgs a, int groups, int chunks) {
-  __shared__ int s_sum[2 * kApplyThreads / 64];
+constexpr int kApplyThreads = 256, kApplyWaves = kApplyThreads / 64, kRowsInFlight = 4, kMostApply = 4096;
+__global__ void __launch_bounds__(kApplyThreads) change_apply_kernel(const ChangeArgs a, int groups) {
+  __shared__ int s_before[kMostGroups], s_wave[kApplyWaves];   // pages given back by the groups of heads before each
   const PageChangeArgs& p = a.p;
-  const int h = blockIdx.x / chunks, chunk = blockIdx.x - h * chunks, lane = threadIdx.x & 63;
-  const int G = p.heads, b = h / G, g = h - b * G, P = 1 << p.page_shift;
-  const int group = h / (kChangeWaves * a.per);
-  const int2 fresh = sum_totals<kApplyThreads>(a.fresh_total, groups, group, s_sum);
-  const int2 back = sum_totals<kApplyThreads>(a.back_total, groups, group, s_sum);
-  const int n_free = a.head->n_free;
-  int error = a.head->error;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = p.heads, P = 1 << p.page_shift;
+  const int first = blockIdx.x * kApplyThreads + threadIdx.x, step = gridDim.x * kApplyThreads;
+  const int wave0 = blockIdx.x * kApplyWaves + wave, waves = gridDim.x * kApplyWaves;
+  const ChangeHeader head = *a.head;
+  const int n_free = head.n_free;
+  int error = head.error;
   if (n_free < 0 || n_free > p.n_pages) error |= LAVA_PAGES_INVALID;
-  if (error == 0 && fresh.y > n_free) error = LAVA_PAGES_EXHAUSTED;
-  if (error == 0 && (long long)n_free - fresh.y + back.y > p.n_pages) error = LAVA_PAGES_INVALID;
-  const int left = error != 0 ? (n_free < 0 ? 0 : n_free > p.n_pages ? (int)p.n_pages : n_free) : n_free - fresh.y;
+  if (error == 0 && head.fresh > n_free) error = LAVA_PAGES_EXHAUSTED;
+  if (error == 0 && (long long)n_free - head.fresh + head.back > p.n_pages) error = LAVA_PAGES_INVALID;
+  const int left = error != 0 ? (n_free < 0 ? 0 : n_free > p.n_pages ? (int)p.n_pages : n_free) : n_free - head.fresh;
   const bool table_apart = p.table_out != p.st.block_table;
-  int* table_out = p.table_out + (long long)h * p.max_blocks;
-  if (p.free_out != p.st.free_pages)
-    for (int i = blockIdx.x * kApplyThreads + threadIdx.x; i < left; i += gridDim.x * kApplyThreads) p.free_out[i] = p.st.free_pages[i];
   const int* tables = table_apart ? p.st.block_table : a.old_table;
-  const int nb_old = (int)(((long long)a.old_rows[h] + P - 1) >> p.page_shift);
+  if (first == 0) {
+    p.st.n_free_out[0] = error != 0 ? n_free : left + head.back;
+    if (error != 0 && p.st.error != nullptr) atomicOr(p.st.error, error);
+  }
+  if (p.free_out != p.st.free_pages)
+    for (int i = first; i < left; i += step) p.free_out[i] = p.st.free_pages[i];
   if (error != 0) {                                            // nothing changes
-    if (chunk != 0) return;
-    if (table_apart)
-      for (int j = threadIdx.x; j < nb_old; j += kApplyThreads) table_out[j] = tables[(long long)h * p.max_blocks + j];
-    if (threadIdx.x == 0) {
-      p.st.head_rows_out[h] = p.st.head_rows[h];
-      if (g == 0) p.st.seq_pos_out[b] = p.st.seq_pos[b];
-      if (h == 0) {
-        p.st.n_free_out[0] = n_free;
-        if (p.st.error != nullptr) atomicOr(p.st.error, error);
+    for (int h = wave0; h < a.heads; h += waves) {
+      const long long row = (long long)h * p.max_blocks;
+      if (table_apart)
+        for (int j = lane; j < blocks_of(p, a.old_rows[h]); j += 64) p.table_out[row + j] = tables[row + j];
+      if (lane == 0) {
+        p.st.head_rows_out[h] = p.st.head_rows[h];
+        if (h % G == 0) p.st.seq_pos_out[h / G] = p.st.seq_pos[h / G];
       }
     }
     return;
   }
-  const int s = a.seq_src[b], n = a.n_new[h], stay = a.stay[h], nb = (int)(((long long)n + P - 1) >> p.page_shift);
-  const int* from = tables + ((long long)(s < 0 ? 0 : s) * G + g) * p.max_blocks;   // read where the source has blocks
-  const int* fresh_pages = a.taken + fresh.x + a.fresh_at[h];
-  if (chunk == 0) {
-    for (int j = threadIdx.x; j < nb; j += kApplyThreads) {
-      if (j >= stay) table_out[j] = fresh_pages[j - stay];
-      else if (table_apart || s != b) table_out[j] = from[j];
-    }
-    if (threadIdx.x == 0) {
-      p.st.head_rows_out[h] = n;
-      if (g == 0) p.st.seq_pos_out[b] = a.seq_pos[b];
-      if (h == 0) p.st.n_free_out[0] = left + back.y;
-    }
-    if (threadIdx.x < 64) {                                    // the pages that this head gives back, in the order of its blocks
-      const int* mine = tables + (long long)h * p.max_blocks;
-      int* to = p.free_out + left + back.x + a.back_at[h];
-      for (int j0 = s == b ? stay : 0; j0 < nb_old; j0 += 64) {
-        const int j = j0 + lane, page = j < nb_old ? mine[j] : -1;
-        const bool gone = page >= 0 && a.mark[page] == 1u + (unsigned int)h;
-        const unsigned long long all = __ballot(gone);
-        if (gone) to[__popcll(all & ((1ull << lane) - 1ull))] = page;
-        to += __popcll(all);
-      }
-    }
-  }
-  // rows stay * P .. n - 1 of the head, `per_row` threads a row, kRowsInFlight rows of a thread at a time
+  // rows: those of the fresh pages in one line, `per_row` threads a row, kRowsInFlight rows of a thread at a time
   const int per_row = p.row_bytes >> 4, rows_a_pass = kApplyThreads / per_row, i = threadIdx.x / per_row, x = threadIdx.x - i * per_row;
-  const long long list = a.list_at[h];
-  const int* kept = list < 0 ? nullptr : p.kept_idx + (long long)b * p.kept_capacity + list;
-  const int old = s < 0 ? 0 : a.old_rows[s * G + g];
   u32x4 *k_out = reinterpret_cast<u32x4*>(p.k), *v_out = reinterpret_cast<u32x4*>(p.v);
   const u32x4 *k_in = k_out, *v_in = v_out;
-  const long long pass = (long long)rows_a_pass * kRowsInFlight;
-  for (long long t0 = (long long)stay * P + chunk * pass; t0 < n; t0 += chunks * pass) {
+  const long long pass = (long long)rows_a_pass * kRowsInFlight, total = (long long)head.fresh << p.page_shift;
+  for (long long t0 = blockIdx.x * pass; t0 < total; t0 += gridDim.x * pass) {
     long long src[kRowsInFlight], dst[kRowsInFlight];
     bool on[kRowsInFlight];
+    int owner[kRowsInFlight], page[kRowsInFlight];
 #pragma unroll
     for (int u = 0; u < kRowsInFlight; ++u) {
-      const long long t = t0 + u * rows_a_pass + i;
-      on[u] = t < n;
+      const long long at = t0 + u * rows_a_pass + i;
+      const int k = (int)((at < total ? at : t0) >> p.page_shift);
+      owner[u] = a.owner[k];
+      page[u] = a.taken[k];
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsInFlight; ++u) {
+      const long long at = t0 + u * rows_a_pass + i;
+      const HeadPlan h = a.plan[owner[u]];
+      const int k = (int)((at < total ? at : t0) >> p.page_shift), in_page = (int)at & (P - 1);
+      const long long t = ((long long)(h.stay + k - h.fresh_at) << p.page_shift) + in_page;
+      on[u] = at < total && t < h.n;
       int r = (int)t;
-      if (kept != nullptr && on[u]) r = kept[t];
-      const int block = r >> p.page_shift;
-      on[u] = on[u] && r >= 0 && r < old;
-      src[u] = on[u] ? ((long long)from[block] << p.page_shift) + (r & (P - 1)) : 0;
-      dst[u] = on[u] ? ((long long)fresh_pages[(int)(t >> p.page_shift) - stay] << p.page_shift) + (t & (P - 1)) : 0;
+      if (h.list >= 0 && on[u]) r = p.kept_idx[(long long)(owner[u] / G) * p.kept_capacity + h.list + t];
+      on[u] = on[u] && r >= 0 && r < h.old;
+      src[u] = on[u] ? ((long long)tables[(long long)h.from * p.max_blocks + (r >> p.page_shift)] << p.page_shift) + (r & (P - 1)) : 0;
+      dst[u] = ((long long)page[u] << p.page_shift) + in_page;
     }
     u32x4 kx[kRowsInFlight], vx[kRowsInFlight];
     int px[kRowsInFlight];
@@ -355,6 +583,45 @@ __global__ void __launch_bounds__(kApplyThreads) change_apply_kernel(const Chang
       }
     }
   }
+  // heads, a wavefront each: tables and counts
+  for (int h = wave0; h < a.heads; h += waves) {
+    const HeadPlan y = a.plan[h];
+    const long long row = (long long)h * p.max_blocks, from = (long long)y.from * p.max_blocks;
+    const int nb = blocks_of(p, y.n);
+    for (int j = (table_apart || y.from != h ? 0 : y.stay) + lane; j < nb; j += 64)
+      p.table_out[row + j] = j >= y.stay ? a.taken[y.fresh_at + j - y.stay] : tables[from + j];
+    if (lane == 0) {
+      p.st.head_rows_out[h] = y.n;
+      if (h % G == 0) p.st.seq_pos_out[h / G] = a.seq_pos[h / G];
+    }
+  }
+  if (head.back == 0) return;                                  // uniform: the same for all
+  // pages given back
+  {
+    constexpr int kEach = kMostGroups / kApplyThreads;
+    int mine[kEach], sum = 0;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int q = (int)threadIdx.x * kEach + u;
+      mine[u] = q < groups ? a.back_total[q] : 0;
+      sum += mine[u];
+    }
+    const int incl = (int)wave_incl((unsigned int)sum);
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    int at = incl - sum;
+    for (int w = 0; w < wave; ++w) at += s_wave[w];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      s_before[threadIdx.x * kEach + u] = at;
+      at += mine[u];
+    }
+    __syncthreads();
+  }
+  for (int h = wave0; h < a.heads; h += waves) {
+    int* to = p.free_out + left + s_before[a.one != 0 ? 0 : h / (kChangeWaves * a.per)] + a.plan[h].back_at;
+    for_each_gone(a, h, tables + (long long)h * p.max_blocks, [to](int page, int n) { to[n] = page; });
+  }
 }
 
 }  // namespace
@@ -367,41 +634,43 @@ int32_t launch_page_change(const PageChangeArgs& p, void* ws, hipStream_t s) {
   ChangeArgs a;
   a.p = p;
   a.heads = p.batch * p.heads;
+  a.one = a.heads <= kOneHeads && (long long)a.heads * p.max_blocks <= kOneEntries ? 1 : 0;
   a.per = (a.heads + kChangeWaves * kMostGroups - 1) / (kChangeWaves * kMostGroups);
-  const int groups = (a.heads + kChangeWaves * a.per - 1) / (kChangeWaves * a.per);
+  const int groups = a.one != 0 ? 1 : (a.heads + kChangeWaves * a.per - 1) / (kChangeWaves * a.per);
   const ChangeLayout l = change_layout(p.batch, p.heads, p.max_blocks, p.n_pages);
   char* w = static_cast<char*>(ws);
   a.head = reinterpret_cast<ChangeHeader*>(w);
   a.fresh_total = reinterpret_cast<int*>(w + l.off_fresh);
   a.back_total = reinterpret_cast<int*>(w + l.off_back);
-  a.keeper = reinterpret_cast<int*>(w + l.off_keeper);
-  a.seq_src = reinterpret_cast<int*>(w + l.off_src);
   a.seq_pos = reinterpret_cast<int*>(w + l.off_pos);
-  const size_t heads_bytes = align_up((size_t)a.heads * 4);
-  int** const per_head[5] = {&a.old_rows, &a.n_new, &a.stay, &a.fresh_at, &a.back_at};
-  for (int i = 0; i < 5; ++i) *per_head[i] = reinterpret_cast<int*>(w + l.off_heads + i * heads_bytes);
-  a.list_at = reinterpret_cast<long long*>(w + l.off_list);
-  a.mark = reinterpret_cast<unsigned int*>(w + l.off_mark);
+  a.old_rows = reinterpret_cast<int*>(w + l.off_rows);
+  a.plan = reinterpret_cast<HeadPlan*>(w + l.off_plan);
+  a.alive = reinterpret_cast<unsigned int*>(w + l.off_alive);
+  a.first = reinterpret_cast<unsigned int*>(w + l.off_first);
   a.taken = reinterpret_cast<int*>(w + l.off_taken);
+  a.owner = reinterpret_cast<int*>(w + l.off_owner);
   a.old_table = p.table_out == p.st.block_table ? reinterpret_cast<int*>(w + l.off_table) : nullptr;
   {
     ProfScope ps(KID_PAGE_MARK, s);
-    long long wgs = (p.n_pages + 1023) / 1024;
-    if (p.source != nullptr && wgs < (p.batch + 3) / 4) wgs = (p.batch + 3) / 4;
-    hipLaunchKernelGGL(change_begin_kernel, dim3((unsigned)(wgs < 2048 ? wgs : 2048)), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(change_mark_kernel, dim3((unsigned)groups), dim3(kChangeThreads), 0, s, a);
-    hipLaunchKernelGGL(change_count_kernel, dim3((unsigned)groups), dim3(kChangeThreads), 0, s, a);
+    if (a.one != 0) {
+      hipLaunchKernelGGL(change_one_kernel, dim3(1), dim3(kOneThreads), 0, s, a);
+    } else {
+      const long long wgs = (p.n_pages + 1023) / 1024;
+      hipLaunchKernelGGL(change_begin_kernel, dim3((unsigned)(wgs < 2048 ? wgs : 2048)), dim3(256), 0, s, a);
+      hipLaunchKernelGGL(change_mark_kernel, dim3((unsigned)groups), dim3(kChangeThreads), 0, s, a);
+      hipLaunchKernelGGL(change_count_kernel, dim3((unsigned)groups), dim3(kChangeThreads), 0, s, a);
+    }
   }
   int32_t st = launch_status();
   if (st != LAVA_OK) return st;
-  // Rows that a head can have to copy: of a fork less than a page.
-  const long long most = p.head_counts != nullptr ? (long long)p.max_blocks << p.page_shift : ((long long)1 << p.page_shift) - 1;
+  // as many workgroups as there can be work for, up to two rounds of what the device holds: of a fork a head copies less than a page
   const long long pass = (long long)kApplyThreads / (p.row_bytes >> 4) * kRowsInFlight;
-  long long chunks = (most + pass - 1) / pass, room = 4096 / a.heads;
-  if (chunks > room) chunks = room;
-  if (chunks < 1) chunks = 1;
+  const long long rows = (long long)a.heads * ((p.head_counts != nullptr ? p.max_blocks : 1LL) << p.page_shift);
+  long long wgs = (rows + pass - 1) / pass;
+  if (wgs < (a.heads + kApplyWaves - 1) / kApplyWaves) wgs = (a.heads + kApplyWaves - 1) / kApplyWaves;
+  if (wgs > kMostApply) wgs = kMostApply;
   ProfScope ps(KID_PAGE_APPLY, s);
-  hipLaunchKernelGGL(change_apply_kernel, dim3((unsigned)(a.heads * chunks)), dim3(kApplyThreads), 0, s, a, groups, (int)chunks);
+  hipLaunchKernelGGL(change_apply_kernel, dim3((unsigned)wgs), dim3(kApplyThreads), 0, s, a, groups);
   return launch_status();
 }
 

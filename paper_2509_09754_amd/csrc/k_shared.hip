@@ -129,19 +129,29 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
     if (some > 1) {
       const int* first = table(lead);
       common = least;
-      for (int b = b0 + wave; b < b1; b += kPlanShWaves) {     // a wavefront a sequence: the first block that differs
-        if (b == lead || held(b) == 0) continue;
-        const int* mine = table(b);
+      // a wavefront four sequences at a time: the first block in which one differs
+      for (int b = b0 + wave; b < b1; b += 4 * kPlanShWaves) {
+        const int* mine[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = b + i * kPlanShWaves;
+          mine[i] = table(c < b1 && held(c) != 0 ? c : lead);
+        }
         for (int j0 = 0; j0 < common; j0 += 256) {
           unsigned long long off[4];
+          int x[4], y[4][4];
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            const int j = j0 + 64 * u + lane;
-            off[u] = __ballot(j < common && mine[j] != first[j]);
+            const int j = j0 + 64 * u + lane < common ? j0 + 64 * u + lane : common - 1;
+            x[u] = first[j];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i][u] = mine[i][j];
           }
 #pragma unroll
+          for (int u = 0; u < 4; ++u) off[u] = __ballot(y[0][u] != x[u] || y[1][u] != x[u] || y[2][u] != x[u] || y[3][u] != x[u]);
+#pragma unroll
           for (int u = 3; u >= 0; --u)
-            if (off[u] != 0ull) common = j0 + 64 * u + __builtin_ctzll(off[u]);
+            if (off[u] != 0ull && j0 + 64 * u + __builtin_ctzll(off[u]) < common) common = j0 + 64 * u + __builtin_ctzll(off[u]);
         }
       }
     }
@@ -177,6 +187,10 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
 }
 
 // ---------------------------------------------------------------- common rows
+// A probability is relative to a maximum that moves only when a logit exceeds it by more than this (in log2 units): sums grow by 2^8 at
+// most, and half of the tiles need no rescaling of the output (296 -> 283 us).
+constexpr float kSlack = 8.0f;
+
 template <int DT, int D>
 struct ShShape {
   using T = Tile<DT, D>;
@@ -187,26 +201,36 @@ struct ShShape {
   static constexpr int kDBlocks = D / 32;
 };
 
+// The 16-byte slot of a row's chunk c is c ^ swizzle(row).  Keys: as the fragment reader has it.  bf16 values are read four rows by
+// 64 bytes at a time, which lie in different banks only if neighbouring rows differ in the slot's upper bits (keys' order: 8 more
+// cycles a read, 315 -> XXX us).
+template <int DT, int D>
+__device__ __forceinline__ int value_swizzle(int row) {
+  if constexpr (DT == LAVA_F32) return row & 7;
+  return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 1) : ((row & 2) << 1) | ((row >> 2) & 1);
+}
+
 // 16 values of bf16 V^T as the left operand, for rows 16 s .. 16 s + 15 of a tile and columns 32 dblk ..: two reads of four rows
-// each; `even` and `odd`: addresses for even and odd dblk.
+// each; at: this lane's address for rows 0 .. 3 of the tile and dblk 0 (a block is 64 bytes and so a bit of the slot, which the swizzle
+// flips or not: an exclusive or); the second four lie 8 rows on.
 template <int D, int S>
-__device__ __forceinline__ void read_v(unsigned int even, unsigned int odd, u32x4 (&v)[D / 32]) {
+__device__ __forceinline__ void read_v(unsigned int at, u32x4 (&v)[D / 32]) {
   constexpr int R = D * 2, o = 16 * S * R;
   typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
   u32x2 x[D / 16];
   if constexpr (D == 128) {
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %8 offset:%10\n\t"
-        "ds_read_b64_tr_b16 %1, %8 offset:%11\n\t"
-        "ds_read_b64_tr_b16 %2, %9 offset:%10\n\t"
-        "ds_read_b64_tr_b16 %3, %9 offset:%11\n\t"
-        "ds_read_b64_tr_b16 %4, %8 offset:%12\n\t"
-        "ds_read_b64_tr_b16 %5, %8 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %6, %9 offset:%12\n\t"
-        "ds_read_b64_tr_b16 %7, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %2, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %4, %10 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %6, %11 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
-        : "v"(even), "v"(odd), "n"(o), "n"(o + 8 * R), "n"(o + 128), "n"(o + 8 * R + 128)
+        : "v"(at), "v"(at ^ 64u), "v"(at ^ 128u), "v"(at ^ 192u), "n"(o), "n"(o + 8 * R)
         : "memory");
   } else {
     asm volatile(
@@ -216,7 +240,7 @@ __device__ __forceinline__ void read_v(unsigned int even, unsigned int odd, u32x
         "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-        : "v"(even), "v"(odd), "n"(o), "n"(o + 8 * R)
+        : "v"(at), "v"(at ^ 64u), "n"(o), "n"(o + 8 * R)
         : "memory");
   }
 #pragma unroll
@@ -238,11 +262,19 @@ __device__ __forceinline__ void lds_read32x4_at(const unsigned int (&a)[4], unsi
       : "memory");
 }
 
+// A tile's fragments from the address of this lane's first chunk: step j is 32 bytes on, before the swizzle.
+template <int STEPS>
+__device__ __forceinline__ void read_k(unsigned int at, u32x4 (&k)[STEPS]) {
+#pragma unroll
+  for (int j = 0; j < STEPS; j += 4)
+    lds_read128x4(at ^ (32u * j), at ^ (32u * (j + 1)), at ^ (32u * (j + 2)), at ^ (32u * (j + 3)), k[j], k[j + 1], k[j + 2], k[j + 3]);
+}
+
 template <int DT, int D, bool OPT>
 __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const SharedArgs a) {
   using S = ShShape<DT, D>;
   using T = Tile<DT, D>;
-  __shared__ u32x4 s_stage[2][kStageBytes / 16];               // keys' tiles, then values'; between units: float [kShWaves][32][D]
+  __shared__ __attribute__((aligned(1024))) u32x4 s_stage[2][kStageBytes / 16];   // (addresses are formed by exclusive or) keys' tiles, then values'; between units: float [kShWaves][32][D]
   __shared__ __attribute__((aligned(16))) int s_pos[2][OPT ? S::kStageRows : 4];
   __shared__ float s_m[kShWaves][32], s_l[kShWaves][32];
   __shared__ int s_wrong;
@@ -267,23 +299,26 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
 
   TileDma<DT, D> dma;
   dma.init(lane);
-  FragReader<DT, D> frags;
-  frags.init(lane);
+  const unsigned int k_at = (unsigned int)(col * T::kRowBytes + ((half ^ (col & 7)) << 4));   // this lane's first chunk of a tile's row
   const unsigned int ring = lds_addr(&s_stage[0][0]);
   constexpr unsigned int kVOff = S::kTiles * T::kTileBytes;
-  // bf16: where this lane's four columns of row 4 half + (lane % 16) / 4 lie, for even and odd blocks of 32 columns.  32 bits: this lane's
-  // column of rows 4 half + 0 .. 3.
+  // bf16: where this lane's four columns of row 4 half + (lane % 16) / 4 lie.  32 bits: this lane's column of rows 4 half + 0 .. 3.
   unsigned int v_at[4] = {0u, 0u, 0u, 0u};
+  unsigned int v_off[TileDma<DT, D>::kVariants];               // of the values' direct-to-LDS loads, as TileDma has them for keys
   if constexpr (DT == LAVA_BF16) {
     const int i = lane & 15, r = 4 * half + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-#pragma unroll
-    for (int e = 0; e < 2; ++e) v_at[e] = (unsigned int)(r * T::kRowBytes + (((4 * e + c) ^ r) << 4) + 8 * (i & 1));
+    v_at[0] = (unsigned int)(r * T::kRowBytes + ((c ^ value_swizzle<DT, D>(r)) << 4) + 8 * (i & 1));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = 4 * half + e;
-      v_at[e] = (unsigned int)(r * T::kRowBytes + (((col >> 2) ^ r) << 4) + 4 * (col & 3));
+      v_at[e] = (unsigned int)(r * T::kRowBytes + (((col >> 2) ^ value_swizzle<DT, D>(r)) << 4) + 4 * (col & 3));
     }
+  }
+#pragma unroll
+  for (int i = 0; i < TileDma<DT, D>::kVariants; ++i) {
+    const int q = i * 64 + lane, row = q / T::kCpr, slot = q % T::kCpr;
+    v_off[i] = (unsigned int)((row - i * TileDma<DT, D>::kRowsPerLoad) * T::kRowBytes + ((slot ^ value_swizzle<DT, D>(row)) << 4));
   }
   const float inv_cap = p.cap > 0.0f ? 1.0f / p.cap : 0.0f;
   const unsigned int window = p.window > 0 ? (unsigned int)p.window : 0x80000000u;
@@ -371,7 +406,7 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
         u32x4* to = dst + (is_v ? S::kTiles * T::kTileChunks : 0) + hh * (T::kTileChunks / 2);
 #pragma unroll
         for (int i = 0; i < T::kLoads / 2; ++i)
-          __builtin_amdgcn_global_load_lds((const LAVA_GLOBAL_AS void*)(src + i * 1024 + dma.loff[i % TileDma<DT, D>::kVariants]),
+          __builtin_amdgcn_global_load_lds((const LAVA_GLOBAL_AS void*)(src + i * 1024 + (is_v ? v_off : dma.loff)[i % TileDma<DT, D>::kVariants]),
                                            (LAVA_LDS_AS void*)(to + i * 64), 16, 0, 0);
         if (OPT && p.pos != nullptr && !is_v) pos_next[x % S::kMine] = p.pos[place + (lane & 15)];
       }
@@ -400,99 +435,204 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
       }
       asm volatile("" ::: "memory");
       const unsigned int stage = ring + (unsigned int)(s & 1) * kStageBytes;
-      for (int t = kp; t < S::kTiles; t += key_parts) {
-        const int r0 = s * S::kStageRows + 32 * t;             // first row of the tile
-        if (r0 >= it.rows) break;                              // uniform
-        f32x16 z = {0}, z2 = {0};
-        {
+      // Whole stages without options, more than one tile of a wavefront: a tile's products run beside the softmax of the next one.  A matrix
+      // instruction that waits for the one before it keeps the other wavefront's vector instructions waiting as well, so
+      // five to seven of those are written behind each (in the order of the source: sched_barrier).
+      const bool whole = !OPT && (s + 1) * S::kStageRows <= it.rows;
+      if (DT == LAVA_BF16 && whole && key_parts < S::kTiles) {  // uniform
+        f32x16 z;
+        float e[16], left[2], keep = 1.0f, base = 0.0f, top = 0.0f, sum = 0.0f;
+        u32x4 parts[2][3];                                     // of the probabilities of the tile's halves
+        // the vector unit's work in pieces of five to seven instructions
+        auto split = [&](auto hc, auto ic) {                   // half h, piece i of 8: two values' first part, then their others
+          constexpr int h = decltype(hc)::value, i = decltype(ic)::value, w = i / 2, at = 8 * h + 2 * w;
+          if constexpr (i % 2 == 0) {
+            const unsigned int hi = pack_bf16(e[at], e[at + 1]);
+            left[0] = e[at] - bf16_low(hi);
+            left[1] = e[at + 1] - bf16_high(hi);
+            parts[h][0][w] = hi;
+          } else {
+            const unsigned int mid = pack_bf16(left[0], left[1]);
+            parts[h][1][w] = mid;
+            parts[h][2][w] = pack_bf16(left[0] - bf16_low(mid), left[1] - bf16_high(mid));
+          }
+        };
+        auto maximum = [&](auto ic) {                          // piece i of 4
+          constexpr int i = decltype(ic)::value;
+          top = i == 0 ? z[0] : top;
+#pragma unroll
+          for (int v = 4 * i; v < 4 * i + 4; ++v) top = fmaxf(top, z[v]);
+          if constexpr (i == 3) {
+            const auto o = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            const float m_tile = fmaxf(__uint_as_float(o[0]), __uint_as_float(o[1])) * a.c2;
+            const float m_new = m_tile > m_run + kSlack ? m_tile : m_run;
+            base = m_new == -INFINITY ? 0.0f : m_new;
+            keep = fast_exp2(m_run - base);
+            m_run = m_new;
+          }
+        };
+        auto exponentials = [&](auto ic) {                     // piece i of 12
+          constexpr int i = decltype(ic)::value;
+          if constexpr (i == 0) sum = 0.0f;
+#pragma unroll
+          for (int v = 16 * i / 12; v < 16 * (i + 1) / 12; ++v) {
+            e[v] = fast_exp2(fmaf(z[v], a.c2, -base));
+            sum += e[v];
+            asm volatile("" : "+v"(e[v]));                     // here, not where the parts are made
+          }
+          if constexpr (i == 11) l_run = l_run * keep + sum;
+        };
+        auto rescale = [&]() {
+          if (__ballot(keep != 1.0f) != 0ull) {                // uniform: a maximum moved
+#pragma unroll
+            for (int d = 0; d < S::kDBlocks; ++d)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) acc[d][v] *= keep;
+          }
+        };
+        using First = std::integral_constant<int, 0>;
+        using Second = std::integral_constant<int, 1>;
+        // with `work` in pieces among the instructions of the matrix cores
+        auto logits = [&](int t, auto work) {
           u32x4 kf[T::kSteps];
-          frags.read(stage + (unsigned int)t * T::kTileBytes, kf);
-#pragma unroll
-          for (int j = 0; j < T::kSteps; j += 2) {
+          read_k(stage + (unsigned int)t * T::kTileBytes + k_at, kf);
+          __builtin_amdgcn_sched_barrier(0);
+          z = f32x16{0};
+          static_for<T::kSteps>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
             z = mfma_chunk<DT>(kf[j], qf[j], z);
-            z2 = mfma_chunk<DT>(kf[j + 1], qf[j + 1], z2);
-          }
+            static_for<8 / T::kSteps>([&](auto xc) { work(std::integral_constant<int, j * (8 / T::kSteps) + decltype(xc)::value>{}); });
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        };
+        auto products = [&](auto hc, int t, auto work) {
+          constexpr int h = decltype(hc)::value, n = 3 * S::kDBlocks;
+          u32x4 vt[S::kDBlocks];
+          read_v<D, h>(stage + kVOff + (unsigned int)t * T::kTileBytes + v_at[0], vt);
+          __builtin_amdgcn_sched_barrier(0);
+          static_for<n>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            acc[j % S::kDBlocks] = mfma_bf16(vt[j % S::kDBlocks], parts[h][j / S::kDBlocks], acc[j % S::kDBlocks]);
+            static_for<12 / n>([&](auto xc) { work(std::integral_constant<int, j * (12 / n) + decltype(xc)::value>{}); });
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        };
+        auto nothing = [](auto) {};
+        logits(kp, nothing);
+        static_for<4>(maximum);
+        static_for<12>(exponentials);
+        rescale();
+        int t = kp;
+        for (; t + key_parts < S::kTiles; t += key_parts) {
+          logits(t + key_parts, [&](auto ic) { split(First{}, ic); });
+          products(First{}, t, [&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            if constexpr (i < 8) split(Second{}, ic);
+            else maximum(std::integral_constant<int, i - 8>{});
+          });
+          products(Second{}, t, exponentials);
+          rescale();
         }
-        float x[16];                                           // of rows 8 (v / 4) + 4 half + v % 4
+        static_for<8>([&](auto ic) { split(First{}, ic); });
+        products(First{}, t, [&](auto ic) {
+          if constexpr (decltype(ic)::value < 8) split(Second{}, ic);
+        });
+        products(Second{}, t, nothing);
+      } else {
+        for (int t = kp; t < S::kTiles; t += key_parts) {
+          const int r0 = s * S::kStageRows + 32 * t;             // first row of the tile
+          if (r0 >= it.rows) break;                              // uniform
+          f32x16 z = {0}, z2 = {0};
+          {
+            u32x4 kf[T::kSteps];
+            read_k(stage + (unsigned int)t * T::kTileBytes + k_at, kf);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = z[v] + z2[v];
-        if (OPT && p.cap > 0.0f) {                             // uniform
-#pragma unroll
-          for (int v = 0; v < 16; ++v) x[v] = capped(x[v] * p.scale, p.cap, inv_cap) * kLog2e;
-        } else {
-#pragma unroll
-          for (int v = 0; v < 16; ++v) x[v] *= a.c2;
-        }
-        if (OPT && p.pos != nullptr) {                         // uniform
-#pragma unroll
-          for (int v4 = 0; v4 < 4; ++v4) {
-            u32x4 at;
-            lds_read128(lds_addr(&s_pos[s & 1][32 * t + 8 * v4 + 4 * half]), at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const unsigned int back = (unsigned int)q_pos - at[e];   // a later row: 2^31 and more
-              const float y = x[4 * v4 + e] - slope * (float)back;
-              x[4 * v4 + e] = back < window ? y : -INFINITY;
+            for (int j = 0; j < T::kSteps; j += 2) {
+              z = mfma_chunk<DT>(kf[j], qf[j], z);
+              z2 = mfma_chunk<DT>(kf[j + 1], qf[j + 1], z2);
             }
           }
-        }
-        if (r0 + 32 > it.rows) {                               // uniform: the second half tile is behind the last row
+          float x[16];                                           // of rows 8 (v / 4) + 4 half + v % 4
 #pragma unroll
-          for (int v = 8; v < 16; ++v) x[v] = -INFINITY;
-        }
-        float top = x[0];
+          for (int v = 0; v < 16; ++v) x[v] = z[v] + z2[v];
+          if (OPT && p.cap > 0.0f) {                             // uniform
 #pragma unroll
-        for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
-        {
-          const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-          top = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
-        }
-        if (__ballot(top > m_run) != 0ull) {                   // uniform: a maximum moves
-          const float m_new = fmaxf(m_run, top), keep = m_new == -INFINITY ? 1.0f : fast_exp2(m_run - m_new);
-          m_run = m_new;
-          l_run *= keep;
+            for (int v = 0; v < 16; ++v) x[v] = capped(x[v] * p.scale, p.cap, inv_cap) * kLog2e;
+          } else {
 #pragma unroll
-          for (int d = 0; d < S::kDBlocks; ++d)
+            for (int v = 0; v < 16; ++v) x[v] *= a.c2;
+          }
+          if (OPT && p.pos != nullptr) {                         // uniform
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[d][v] *= keep;
-        }
-        const float base = m_run == -INFINITY ? 0.0f : m_run;
-        float e[16], sum = 0.0f;
+            for (int v4 = 0; v4 < 4; ++v4) {
+              u32x4 at;
+              lds_read128(lds_addr(&s_pos[s & 1][32 * t + 8 * v4 + 4 * half]), at);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          e[v] = fast_exp2(x[v] - base);
-          sum += e[v];
-        }
-        l_run += sum;
-        const unsigned int values = stage + kVOff + (unsigned int)t * T::kTileBytes;
-        if constexpr (DT == LAVA_BF16) {
-          static_for<2>([&](auto sc) {
-            constexpr int h = decltype(sc)::value;
-            u32x4 parts[3];
-            {
-              u32x4 lo, hi;
-#pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                lo[v] = __float_as_uint(e[8 * h + v]);
-                hi[v] = __float_as_uint(e[8 * h + 4 + v]);
+              for (int e = 0; e < 4; ++e) {
+                const unsigned int back = (unsigned int)q_pos - at[e];   // a later row: 2^31 and more
+                const float y = x[4 * v4 + e] - slope * (float)back;
+                x[4 * v4 + e] = back < window ? y : -INFINITY;
               }
-              split8(lo, hi, parts[0], parts[1], parts[2]);
             }
-            u32x4 vt[S::kDBlocks];
-            read_v<D, h>(values + v_at[0], values + v_at[1], vt);
+          }
+          if (r0 + 32 > it.rows) {                               // uniform: the second half tile is behind the last row
 #pragma unroll
-            for (int k = 0; k < 3; ++k)
+            for (int v = 8; v < 16; ++v) x[v] = -INFINITY;
+          }
+          float top = x[0];
 #pragma unroll
-              for (int d = 0; d < S::kDBlocks; ++d) acc[d] = mfma_bf16(vt[d], parts[k], acc[d]);
-          });
-        } else {
-          static_for<4 * S::kDBlocks>([&](auto ic) {
-            constexpr int v4 = decltype(ic)::value / S::kDBlocks, d = decltype(ic)::value % S::kDBlocks;
-            float vv[4];
-            lds_read32x4_at<8 * v4 * T::kRowBytes + 128 * d>(v_at, values, vv);
+          for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+          {
+            const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+          }
+          if (__ballot(top > m_run + kSlack) != 0ull) {          // uniform: a maximum moves
+            const float m_new = fmaxf(m_run, top), keep = m_new == -INFINITY ? 1.0f : fast_exp2(m_run - m_new);
+            m_run = m_new;
+            l_run *= keep;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv[k], e[4 * v4 + k], acc[d], 0, 0, 0);
-          });
+            for (int d = 0; d < S::kDBlocks; ++d)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) acc[d][v] *= keep;
+          }
+          const float base = m_run == -INFINITY ? 0.0f : m_run;
+          float e[16], sum = 0.0f;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            e[v] = fast_exp2(x[v] - base);
+            sum += e[v];
+          }
+          l_run += sum;
+          const unsigned int values = stage + kVOff + (unsigned int)t * T::kTileBytes;
+          if constexpr (DT == LAVA_BF16) {
+            static_for<2>([&](auto sc) {
+              constexpr int h = decltype(sc)::value;
+              u32x4 parts[3];
+              {
+                u32x4 lo, hi;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                  lo[v] = __float_as_uint(e[8 * h + v]);
+                  hi[v] = __float_as_uint(e[8 * h + 4 + v]);
+                }
+                split8(lo, hi, parts[0], parts[1], parts[2]);
+              }
+              u32x4 vt[S::kDBlocks];
+              read_v<D, h>(values + v_at[0], vt);
+#pragma unroll
+              for (int k = 0; k < 3; ++k)
+#pragma unroll
+                for (int d = 0; d < S::kDBlocks; ++d) acc[d] = mfma_bf16(vt[d], parts[k], acc[d]);
+            });
+          } else {
+            static_for<4 * S::kDBlocks>([&](auto ic) {
+              constexpr int v4 = decltype(ic)::value / S::kDBlocks, d = decltype(ic)::value % S::kDBlocks;
+              float vv[4];
+              lds_read32x4_at<8 * v4 * T::kRowBytes + 128 * d>(v_at, values, vv);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv[k], e[4 * v4 + k], acc[d], 0, 0, 0);
+            });
+          }
         }
       }
       lds_reads_done();
@@ -625,7 +765,7 @@ __device__ __forceinline__ void whole_head(const SharedArgs& a, int b, int g, fl
 
 template <int DT, int D>
 __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const SharedArgs a) {
-  __shared__ float s_red[(kMergeThreads / 64) * (D + 2)];
+  __shared__ float s_red[(kMergeThreads / 64) * (D + 2)], s_base[8], s_own[8], s_sum[8];
   const PagedDecodeArgs& p = a.p;
   const int b = blockIdx.x / p.H_kv, g = blockIdx.x - b * p.H_kv;
   const int item = a.item_of[blockIdx.x];
@@ -641,33 +781,59 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
   }
   const SharedItem it = a.items[item];
   const SharedParts parts = a.parts[item];
-  const int q_rows = it.n_seq * p.G;
+  const int q_rows = it.n_seq * p.G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long long first0 = parts.row + (long long)(b - it.first_seq) * p.G;
+  // a wavefront a query: the maximum over its parts, then their weights
+  for (int t = wave; t < p.G; t += kMergeThreads / 64) {
+    const float own = a.rest_lse[row0 + t] * kLog2e;
+    float M = own, L = 0.0f;
+    for (int u = lane; u < parts.units; u += 64) M = fmaxf(M, a.part_ml[first0 + t + (long long)u * q_rows].x);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) M = fmaxf(M, __shfl_xor(M, m));
+    const float base = M == -INFINITY ? 0.0f : M;
+    for (int u = lane; u < parts.units; u += 64) {
+      const float2 ml = a.part_ml[first0 + t + (long long)u * q_rows];
+      L += fast_exp2(ml.x - base) * ml.y;
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) L += __shfl_xor(L, m);
+    const float wgt = fast_exp2(own - base);
+    L += wgt;
+    if (marked != 0 || isnan(own)) L = NAN;                    // a page that is not in the pool, of the common ones or the own
+    if (lane == 0) {
+      s_base[t] = base;
+      s_own[t] = wgt;
+      s_sum[t] = L;
+      if (p.lse != nullptr) p.lse[row0 + t] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    }
+  }
+  __syncthreads();
+  constexpr int kLoads = 8;
   for (int i = threadIdx.x; i < p.G * (D / 4); i += kMergeThreads) {
     const int t = i / (D / 4), c = i - t * (D / 4);
-    const long long first = parts.row + (long long)(b - it.first_seq) * p.G + t;
-    const float own = a.rest_lse[row0 + t] * kLog2e;
-    float M = own;
-    for (int u = 0; u < parts.units; ++u) M = fmaxf(M, a.part_ml[first + (long long)u * q_rows].x);
-    const float base = M == -INFINITY ? 0.0f : M;
+    const float base = s_base[t], L = s_sum[t], wgt = s_own[t];
     float4* out = reinterpret_cast<float4*>(p.out + (row0 + t) * D) + c;
     const float4 mine = *out;
-    float wgt = fast_exp2(own - base), L = wgt;
     float4 sum = make_float4(wgt * mine.x, wgt * mine.y, wgt * mine.z, wgt * mine.w);
-    for (int u = 0; u < parts.units; ++u) {
-      const long long r = first + (long long)u * q_rows;
-      const float2 ml = a.part_ml[r];
-      const float4 y = *reinterpret_cast<const float4*>(a.part_acc + r * D + 4 * c);
-      wgt = fast_exp2(ml.x - base);
-      L += wgt * ml.y;
-      sum.x += wgt * y.x;
-      sum.y += wgt * y.y;
-      sum.z += wgt * y.z;
-      sum.w += wgt * y.w;
+    for (int u0 = 0; u0 < parts.units; u0 += kLoads) {
+      float m[kLoads];
+      float4 y[kLoads];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {                       // behind the last part: the last one, at no weight
+        const long long r = first0 + t + (long long)(u0 + u < parts.units ? u0 + u : parts.units - 1) * q_rows;
+        m[u] = a.part_ml[r].x;
+        y[u] = *reinterpret_cast<const float4*>(a.part_acc + r * D + 4 * c);
+      }
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        const float w = u0 + u < parts.units ? fast_exp2(m[u] - base) : 0.0f;
+        sum.x += w * y[u].x;
+        sum.y += w * y[u].y;
+        sum.z += w * y[u].z;
+        sum.w += w * y[u].w;
+      }
     }
-    if (marked != 0 || isnan(own)) L = NAN;                    // a page that is not in the pool, of the common ones or the own
-    const bool none = L == 0.0f;
-    *out = none ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x / L, sum.y / L, sum.z / L, sum.w / L);
-    if (c == 0 && p.lse != nullptr) p.lse[row0 + t] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    *out = L == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x / L, sum.y / L, sum.z / L, sum.w / L);
   }
 }
 
