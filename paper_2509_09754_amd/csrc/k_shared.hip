@@ -9,15 +9,22 @@
 //   own     the decode step over pages, over the tables of what is left
 //   merge   the parts of the common rows and the own ones, per sequence and head
 //
-// Common rows: a workgroup of eight wavefronts.  A stage's keys and values come to LDS by direct-to-LDS loads, one stage ahead.  A wavefront
-// has 32 queries as the columns of its products and takes every n-th tile of 32 rows, n = 8 / tiles of queries:
+// Common rows: a workgroup of eight wavefronts.  A stage's keys and values come to LDS by direct-to-LDS loads, one stage ahead (in a
+// window only stages that hold a row of it).  A wavefront has 32 queries as the columns of its products and takes every n-th tile of
+// 32 rows, n = 8 / tiles of queries:
 //   logits  K_tile x Q^T: a lane has 16 of a query's 32 logits
 //   softmax online, in the exp2 domain; the other 16 are in lane ^ 32
 //   output  V_tile^T x P^T: in the order in which the first product leaves the rows to a lane they are the operand of the second, so
 //           probabilities stay in registers.  bf16: V is read transposed from LDS, a probability is three bf16 parts (8 + 8 +
-//           8 bits), so that products are exact and sums 32 bits, as in the decode step over pages
+//           8 bits), so that products are exact and sums 32 bits, as in the decode step over pages (with two parts an output
+//           would be off by 2.4e-6 of itself)
 // Rows that are masked may hold anything there.  A product cannot leave them out, so an item whose sums are not all
 // finite is marked, and merge computes its heads' outputs again, row by row.
+//
+// Bound by HBM for few queries: 4 groups of 2 sequences with 8 KV heads of 65536 rows (1.07 GB) 4.9 TB/s.  By the matrix cores for many: 64
+// sequences over 8 heads of 131072 rows need 275 GFLOP with the three parts, 265 us, 1.04 PFLOP/s, where a large matrix product of the
+// library reaches 1.12.  32 bits: by the 32-bit matrix instructions, which two or four of the eight wavefronts of few
+// queries issue.
 #include <math.h>
 
 #include "common.h"
@@ -127,31 +134,28 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
       some += s_some[w];
     }
     if (some > 1) {
+      // a wavefront 64 blocks: the first one in which a sequence differs, kCompared of them at a time
+      constexpr int kCompared = 16;
       const int* first = table(lead);
       common = least;
-      // a wavefront four sequences at a time: the first block in which one differs
-      for (int b = b0 + wave; b < b1; b += 4 * kPlanShWaves) {
-        const int* mine[4];
+      for (int j0 = 64 * wave; j0 < least; j0 += 64 * kPlanShWaves) {
+        const int j = j0 + lane < least ? j0 + lane : least - 1, x = first[j];
+        bool differs = false;
+        for (int c1 = b0; c1 < b1; c1 += 64) {
+          const unsigned long long there = __ballot(c1 + lane < b1 && held(c1 + lane < b1 ? c1 + lane : b0) != 0);
+          for (int c0 = 0; c0 < 64 && (there >> c0) != 0ull; c0 += kCompared) {
+            int y[kCompared];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c = b + i * kPlanShWaves;
-          mine[i] = table(c < b1 && held(c) != 0 ? c : lead);
-        }
-        for (int j0 = 0; j0 < common; j0 += 256) {
-          unsigned long long off[4];
-          int x[4], y[4][4];
+            for (int i = 0; i < kCompared; ++i) y[i] = table((there >> (c0 + i)) & 1ull ? c1 + c0 + i : lead)[j];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int j = j0 + 64 * u + lane < common ? j0 + 64 * u + lane : common - 1;
-            x[u] = first[j];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i][u] = mine[i][j];
+            for (int i = 0; i < kCompared; ++i) differs |= y[i] != x;
           }
-#pragma unroll
-          for (int u = 0; u < 4; ++u) off[u] = __ballot(y[0][u] != x[u] || y[1][u] != x[u] || y[2][u] != x[u] || y[3][u] != x[u]);
-#pragma unroll
-          for (int u = 3; u >= 0; --u)
-            if (off[u] != 0ull && j0 + 64 * u + __builtin_ctzll(off[u]) < common) common = j0 + 64 * u + __builtin_ctzll(off[u]);
+        }
+        const unsigned long long off = __ballot(differs);
+        if (off != 0ull) {
+          const int at = j0 + __builtin_ctzll(off);
+          common = at < common ? at : common;
+          break;
         }
       }
     }
@@ -171,18 +175,35 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
     a.items[item0 + i] = it;
     a.marked[item0 + i] = 0;
   }
-  for (int b = b0 + wave * step; b < b1; b += kPlanShWaves * step) {   // a wavefront a sequence: what is left
-    const long long h = (long long)b * p.H_kv + g;
-    const int rows = p.head_rows[h], skip = rows == 0 ? 0 : common;
-    if (lane == 0) {
-      a.rest_rows[h] = rows - (skip << p.page_shift);
-      a.item_of[h] = skip > 0 ? item0 + (b - b0) / seqs : -1;
+  // what is left: a wavefront four sequences at a time
+  for (int c0 = b0 + wave * step; c0 < b1; c0 += 4 * kPlanShWaves * step) {
+    long long h[4];
+    int rows[4], skip[4], left[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int b = c0 + i * kPlanShWaves * step;
+      h[i] = (long long)(b < b1 ? b : c0) * p.H_kv + g;
+      rows[i] = p.head_rows[h[i]];
     }
-    if (rows <= 0 || rows > p.max_blocks << p.page_shift) continue;
-    const int* from = p.block_table + h * p.max_blocks + skip;
-    int* to = a.rest_table + h * p.max_blocks;
-    const int left = ((rows + P - 1) >> p.page_shift) - skip;
-    for (int j = lane; j < left; j += 64) to[j] = from[j];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool there = c0 + i * kPlanShWaves * step < b1;
+      skip[i] = rows[i] == 0 ? 0 : common;
+      left[i] = !there || rows[i] <= 0 || rows[i] > p.max_blocks << p.page_shift ? 0 : ((rows[i] + P - 1) >> p.page_shift) - skip[i];
+      y[i] = lane < left[i] ? p.block_table[h[i] * p.max_blocks + skip[i] + lane] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int b = c0 + i * kPlanShWaves * step;
+      if (b >= b1) continue;
+      if (lane == 0) {
+        a.rest_rows[h[i]] = rows[i] - (skip[i] << p.page_shift);
+        a.item_of[h[i]] = skip[i] > 0 ? item0 + (b - b0) / seqs : -1;
+      }
+      int* to = a.rest_table + h[i] * p.max_blocks;
+      if (lane < left[i]) to[lane] = y[i];
+      for (int j = 64 + lane; j < left[i]; j += 64) to[j] = p.block_table[h[i] * p.max_blocks + skip[i] + j];
+    }
   }
 }
 
@@ -203,7 +224,7 @@ struct ShShape {
 
 // The 16-byte slot of a row's chunk c is c ^ swizzle(row).  Keys: as the fragment reader has it.  bf16 values are read four rows by
 // 64 bytes at a time, which lie in different banks only if neighbouring rows differ in the slot's upper bits (keys' order: 8 more
-// cycles a read, 315 -> XXX us).
+// cycles a read).
 template <int DT, int D>
 __device__ __forceinline__ int value_swizzle(int row) {
   if constexpr (DT == LAVA_F32) return row & 7;
@@ -277,6 +298,7 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
   __shared__ __attribute__((aligned(1024))) u32x4 s_stage[2][kStageBytes / 16];   // (addresses are formed by exclusive or) keys' tiles, then values'; between units: float [kShWaves][32][D]
   __shared__ __attribute__((aligned(16))) int s_pos[2][OPT ? S::kStageRows : 4];
   __shared__ float s_m[kShWaves][32], s_l[kShWaves][32];
+  __shared__ unsigned long long s_seen[kShWaves];
   __shared__ int s_wrong;
   const PagedDecodeArgs& p = a.p;
   const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 31, half = lane >> 5;
@@ -294,7 +316,9 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
   if (total == 0u) return;
   // units of `share` stages of one item: no more units than workgroups where items are few
   const unsigned int wgs = gridDim.x;
-  const unsigned int cut = 2u * full <= wgs ? wgs - full : 2u * wgs;
+  const bool windowed = OPT && p.window > 0;
+  // twice as many where parts of the rows are out of the window, so that they are spread
+  const unsigned int cut = 2u * full <= wgs && !windowed ? wgs - full : 2u * wgs;
   const int share = (int)((total + cut - 1u) / cut);
 
   TileDma<DT, D> dma;
@@ -393,8 +417,8 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
       }
     };
     int pos_next[S::kMine] = {};
-    auto issue = [&](int s, int sb) {                          // stage s of pages loaded from sb on
-      u32x4* dst = s_stage[s & 1];
+    auto issue = [&](int s, int sb, int buffer) {              // stage s of pages loaded from sb on
+      u32x4* dst = s_stage[buffer];
 #pragma unroll
       for (int x = 0; x < 4 * S::kTiles / kShWaves; ++x) {
         const int k = wave + kShWaves * x, hh = k % S::kHalves;
@@ -411,231 +435,185 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
         if (OPT && p.pos != nullptr && !is_v) pos_next[x % S::kMine] = p.pos[place + (lane & 15)];
       }
     };
+    // The stages of sb .. sb + 63 that hold rows in the window of any of the item's queries, as bits.
+    unsigned int reach = 0u, last = 0u;                        // last: the latest position; rows further back than `reach` are seen by nobody
+    if (windowed) {
+      int lo = 0x7fffffff, hi = -0x7fffffff - 1;
+      for (int i = lane; i < it.n_seq; i += 64) {
+        const int y = p.q_pos[it.first_seq + i];
+        lo = min(lo, y);
+        hi = max(hi, y);
+      }
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        lo = min(lo, __shfl_xor(lo, m));
+        hi = max(hi, __shfl_xor(hi, m));
+      }
+      last = (unsigned int)hi;
+      const unsigned int spread = (unsigned int)hi - (unsigned int)lo;
+      reach = spread < 0x80000000u - window ? window + spread : 0x80000000u;
+    }
+    auto seen_from = [&](int sb) -> unsigned long long {
+      const int here = s1 - sb;
+      const unsigned long long all = here >= 64 ? ~0ull : (1ull << here) - 1ull;
+      if (!windowed) return all;
+      bool any = false;
+#pragma unroll
+      for (int x = 0; x < S::kMine; ++x) {
+        const int hh = (wave + kShWaves * x) % S::kHalves, r = (sb + lane) * S::kStageRows + 16 * hh;
+        if (lane >= here || r >= it.rows) continue;
+        const u32x4* at = reinterpret_cast<const u32x4*>(p.pos + ((long long)page[x] << p.page_shift) + (r & ((1 << p.page_shift) - 1)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const u32x4 y = at[i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) any |= last - y[e] < reach;
+        }
+      }
+      const unsigned long long mine = __ballot(any);
+      if (lane == 0) s_seen[wave] = mine;
+      __syncthreads();
+      unsigned long long seen = 0ull;
+      for (int w = 0; w < kShWaves; ++w) seen |= s_seen[w];
+      __syncthreads();
+      return seen & all;
+    };
 
     int sb = s0;
     load_pages(sb);
-    issue(s0, sb);
-    for (int s = s0; s < s1; ++s) {
+    unsigned long long todo = seen_from(sb);
+    auto next_stage = [&]() -> int {                           // -1: none left
+      while (todo == 0ull) {                                   // uniform over the workgroup
+        sb += 64;
+        if (sb >= s1) return -1;
+        load_pages(sb);
+        todo = seen_from(sb);
+      }
+      const int j = __builtin_ctzll(todo);
+      todo &= todo - 1ull;
+      return sb + j;
+    };
+    int s = next_stage(), buffer = 0;
+    if (s >= 0) issue(s, sb, buffer);
+    while (s >= 0) {
       wait_vmcnt<0>();
       if (OPT && p.pos != nullptr) {
 #pragma unroll
         for (int x = 0; x < S::kMine; ++x) {
           const int k = wave + kShWaves * x;
-          if (k < S::kHalves && lane < 16) lds_write32(lds_addr(&s_pos[s & 1][16 * k + lane]), __int_as_float(pos_next[x]));
+          if (k < S::kHalves && lane < 16) lds_write32(lds_addr(&s_pos[buffer][16 * k + lane]), __int_as_float(pos_next[x]));
         }
         lds_reads_done();
       }
-      __syncthreads();                                         // stage s is there, the other one free
-      if (s + 1 < s1) {
-        if (s + 1 - sb == 64) {
-          sb = s + 1;
-          load_pages(sb);
-        }
-        issue(s + 1, sb);
-      }
+      __syncthreads();                                         // the stage is there, the other one free
+      const int next = next_stage();
+      if (next >= 0) issue(next, sb, buffer ^ 1);
       asm volatile("" ::: "memory");
-      const unsigned int stage = ring + (unsigned int)(s & 1) * kStageBytes;
-      // Whole stages without options, more than one tile of a wavefront: a tile's products run beside the softmax of the next one.  A matrix
-      // instruction that waits for the one before it keeps the other wavefront's vector instructions waiting as well, so
-      // five to seven of those are written behind each (in the order of the source: sched_barrier).
-      const bool whole = !OPT && (s + 1) * S::kStageRows <= it.rows;
-      if (DT == LAVA_BF16 && whole && key_parts < S::kTiles) {  // uniform
-        f32x16 z;
-        float e[16], left[2], keep = 1.0f, base = 0.0f, top = 0.0f, sum = 0.0f;
-        u32x4 parts[2][3];                                     // of the probabilities of the tile's halves
-        // the vector unit's work in pieces of five to seven instructions
-        auto split = [&](auto hc, auto ic) {                   // half h, piece i of 8: two values' first part, then their others
-          constexpr int h = decltype(hc)::value, i = decltype(ic)::value, w = i / 2, at = 8 * h + 2 * w;
-          if constexpr (i % 2 == 0) {
-            const unsigned int hi = pack_bf16(e[at], e[at + 1]);
-            left[0] = e[at] - bf16_low(hi);
-            left[1] = e[at + 1] - bf16_high(hi);
-            parts[h][0][w] = hi;
-          } else {
-            const unsigned int mid = pack_bf16(left[0], left[1]);
-            parts[h][1][w] = mid;
-            parts[h][2][w] = pack_bf16(left[0] - bf16_low(mid), left[1] - bf16_high(mid));
-          }
-        };
-        auto maximum = [&](auto ic) {                          // piece i of 4
-          constexpr int i = decltype(ic)::value;
-          top = i == 0 ? z[0] : top;
-#pragma unroll
-          for (int v = 4 * i; v < 4 * i + 4; ++v) top = fmaxf(top, z[v]);
-          if constexpr (i == 3) {
-            const auto o = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            const float m_tile = fmaxf(__uint_as_float(o[0]), __uint_as_float(o[1])) * a.c2;
-            const float m_new = m_tile > m_run + kSlack ? m_tile : m_run;
-            base = m_new == -INFINITY ? 0.0f : m_new;
-            keep = fast_exp2(m_run - base);
-            m_run = m_new;
-          }
-        };
-        auto exponentials = [&](auto ic) {                     // piece i of 12
-          constexpr int i = decltype(ic)::value;
-          if constexpr (i == 0) sum = 0.0f;
-#pragma unroll
-          for (int v = 16 * i / 12; v < 16 * (i + 1) / 12; ++v) {
-            e[v] = fast_exp2(fmaf(z[v], a.c2, -base));
-            sum += e[v];
-            asm volatile("" : "+v"(e[v]));                     // here, not where the parts are made
-          }
-          if constexpr (i == 11) l_run = l_run * keep + sum;
-        };
-        auto rescale = [&]() {
-          if (__ballot(keep != 1.0f) != 0ull) {                // uniform: a maximum moved
-#pragma unroll
-            for (int d = 0; d < S::kDBlocks; ++d)
-#pragma unroll
-              for (int v = 0; v < 16; ++v) acc[d][v] *= keep;
-          }
-        };
-        using First = std::integral_constant<int, 0>;
-        using Second = std::integral_constant<int, 1>;
-        // with `work` in pieces among the instructions of the matrix cores
-        auto logits = [&](int t, auto work) {
+      const unsigned int stage = ring + (unsigned int)buffer * kStageBytes;
+      for (int t = kp; t < S::kTiles; t += key_parts) {
+        const int r0 = s * S::kStageRows + 32 * t;             // first row of the tile
+        if (r0 >= it.rows) break;                              // uniform
+        f32x16 z = {0};
+        {
           u32x4 kf[T::kSteps];
           read_k(stage + (unsigned int)t * T::kTileBytes + k_at, kf);
-          __builtin_amdgcn_sched_barrier(0);
-          z = f32x16{0};
-          static_for<T::kSteps>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            z = mfma_chunk<DT>(kf[j], qf[j], z);
-            static_for<8 / T::kSteps>([&](auto xc) { work(std::integral_constant<int, j * (8 / T::kSteps) + decltype(xc)::value>{}); });
-            __builtin_amdgcn_sched_barrier(0);
-          });
-        };
-        auto products = [&](auto hc, int t, auto work) {
-          constexpr int h = decltype(hc)::value, n = 3 * S::kDBlocks;
-          u32x4 vt[S::kDBlocks];
-          read_v<D, h>(stage + kVOff + (unsigned int)t * T::kTileBytes + v_at[0], vt);
-          __builtin_amdgcn_sched_barrier(0);
-          static_for<n>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            acc[j % S::kDBlocks] = mfma_bf16(vt[j % S::kDBlocks], parts[h][j / S::kDBlocks], acc[j % S::kDBlocks]);
-            static_for<12 / n>([&](auto xc) { work(std::integral_constant<int, j * (12 / n) + decltype(xc)::value>{}); });
-            __builtin_amdgcn_sched_barrier(0);
-          });
-        };
-        auto nothing = [](auto) {};
-        logits(kp, nothing);
-        static_for<4>(maximum);
-        static_for<12>(exponentials);
-        rescale();
-        int t = kp;
-        for (; t + key_parts < S::kTiles; t += key_parts) {
-          logits(t + key_parts, [&](auto ic) { split(First{}, ic); });
-          products(First{}, t, [&](auto ic) {
-            constexpr int i = decltype(ic)::value;
-            if constexpr (i < 8) split(Second{}, ic);
-            else maximum(std::integral_constant<int, i - 8>{});
-          });
-          products(Second{}, t, exponentials);
-          rescale();
+#pragma unroll
+          for (int j = 0; j < T::kSteps; ++j) z = mfma_chunk<DT>(kf[j], qf[j], z);
         }
-        static_for<8>([&](auto ic) { split(First{}, ic); });
-        products(First{}, t, [&](auto ic) {
-          if constexpr (decltype(ic)::value < 8) split(Second{}, ic);
-        });
-        products(Second{}, t, nothing);
-      } else {
-        for (int t = kp; t < S::kTiles; t += key_parts) {
-          const int r0 = s * S::kStageRows + 32 * t;             // first row of the tile
-          if (r0 >= it.rows) break;                              // uniform
-          f32x16 z = {0}, z2 = {0};
-          {
-            u32x4 kf[T::kSteps];
-            read_k(stage + (unsigned int)t * T::kTileBytes + k_at, kf);
-#pragma unroll
-            for (int j = 0; j < T::kSteps; j += 2) {
-              z = mfma_chunk<DT>(kf[j], qf[j], z);
-              z2 = mfma_chunk<DT>(kf[j + 1], qf[j + 1], z2);
-            }
-          }
-          float x[16];                                           // of rows 8 (v / 4) + 4 half + v % 4
-#pragma unroll
-          for (int v = 0; v < 16; ++v) x[v] = z[v] + z2[v];
-          if (OPT && p.cap > 0.0f) {                             // uniform
-#pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] = capped(x[v] * p.scale, p.cap, inv_cap) * kLog2e;
-          } else {
-#pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] *= a.c2;
-          }
-          if (OPT && p.pos != nullptr) {                         // uniform
-#pragma unroll
-            for (int v4 = 0; v4 < 4; ++v4) {
-              u32x4 at;
-              lds_read128(lds_addr(&s_pos[s & 1][32 * t + 8 * v4 + 4 * half]), at);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const unsigned int back = (unsigned int)q_pos - at[e];   // a later row: 2^31 and more
-                const float y = x[4 * v4 + e] - slope * (float)back;
-                x[4 * v4 + e] = back < window ? y : -INFINITY;
-              }
-            }
-          }
-          if (r0 + 32 > it.rows) {                               // uniform: the second half tile is behind the last row
-#pragma unroll
-            for (int v = 8; v < 16; ++v) x[v] = -INFINITY;
-          }
-          float top = x[0];
-#pragma unroll
-          for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
-          {
-            const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            top = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
-          }
-          if (__ballot(top > m_run + kSlack) != 0ull) {          // uniform: a maximum moves
-            const float m_new = fmaxf(m_run, top), keep = m_new == -INFINITY ? 1.0f : fast_exp2(m_run - m_new);
-            m_run = m_new;
-            l_run *= keep;
-#pragma unroll
-            for (int d = 0; d < S::kDBlocks; ++d)
-#pragma unroll
-              for (int v = 0; v < 16; ++v) acc[d][v] *= keep;
-          }
-          const float base = m_run == -INFINITY ? 0.0f : m_run;
-          float e[16], sum = 0.0f;
+        float x[16];                                           // of rows 8 (v / 4) + 4 half + v % 4
+        if (OPT && p.cap > 0.0f) {                             // uniform
+          float most = 0.0f;
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
-            e[v] = fast_exp2(x[v] - base);
-            sum += e[v];
+            x[v] = z[v] * p.scale;
+            most = fmaxf(most, fabsf(x[v]));
           }
-          l_run += sum;
-          const unsigned int values = stage + kVOff + (unsigned int)t * T::kTileBytes;
-          if constexpr (DT == LAVA_BF16) {
-            static_for<2>([&](auto sc) {
-              constexpr int h = decltype(sc)::value;
-              u32x4 parts[3];
-              {
-                u32x4 lo, hi;
+          if (__ballot(!(most < 0.25f * p.cap)) == 0ull) {     // all near zero, as logits mostly are: without the exponential
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                  lo[v] = __float_as_uint(e[8 * h + v]);
-                  hi[v] = __float_as_uint(e[8 * h + 4 + v]);
-                }
-                split8(lo, hi, parts[0], parts[1], parts[2]);
-              }
-              u32x4 vt[S::kDBlocks];
-              read_v<D, h>(values + v_at[0], vt);
-#pragma unroll
-              for (int k = 0; k < 3; ++k)
-#pragma unroll
-                for (int d = 0; d < S::kDBlocks; ++d) acc[d] = mfma_bf16(vt[d], parts[k], acc[d]);
-            });
+            for (int v = 0; v < 16; ++v) x[v] = capped_near(x[v], p.cap * kLog2e, inv_cap);
           } else {
-            static_for<4 * S::kDBlocks>([&](auto ic) {
-              constexpr int v4 = decltype(ic)::value / S::kDBlocks, d = decltype(ic)::value % S::kDBlocks;
-              float vv[4];
-              lds_read32x4_at<8 * v4 * T::kRowBytes + 128 * d>(v_at, values, vv);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv[k], e[4 * v4 + k], acc[d], 0, 0, 0);
-            });
+            for (int v = 0; v < 16; ++v) x[v] = capped(x[v], p.cap, inv_cap) * kLog2e;
           }
+        } else {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = z[v] * a.c2;
+        }
+        if (OPT && p.pos != nullptr) {                         // uniform
+#pragma unroll
+          for (int v4 = 0; v4 < 4; ++v4) {
+            u32x4 at;
+            lds_read128(lds_addr(&s_pos[buffer][32 * t + 8 * v4 + 4 * half]), at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned int back = (unsigned int)q_pos - at[e];   // a later row: 2^31 and more
+              const float y = x[4 * v4 + e] - slope * (float)back;
+              x[4 * v4 + e] = back < window ? y : -INFINITY;
+            }
+          }
+        }
+        if (r0 + 32 > it.rows) {                               // uniform: the second half tile is behind the last row
+#pragma unroll
+          for (int v = 8; v < 16; ++v) x[v] = -INFINITY;
+        }
+        float top = x[0];
+#pragma unroll
+        for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+        {
+          const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+          top = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+        }
+        if (__ballot(top > m_run + kSlack) != 0ull) {          // uniform: a maximum moves
+          const float m_new = fmaxf(m_run, top), keep = m_new == -INFINITY ? 1.0f : fast_exp2(m_run - m_new);
+          m_run = m_new;
+          l_run *= keep;
+#pragma unroll
+          for (int d = 0; d < S::kDBlocks; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[d][v] *= keep;
+        }
+        const float base = m_run == -INFINITY ? 0.0f : m_run;
+        float e[16], sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          e[v] = fast_exp2(x[v] - base);
+          sum += e[v];
+        }
+        l_run += sum;
+        const unsigned int values = stage + kVOff + (unsigned int)t * T::kTileBytes;
+        if constexpr (DT == LAVA_BF16) {
+          static_for<2>([&](auto sc) {
+            constexpr int h = decltype(sc)::value;
+            u32x4 parts[3];
+            {
+              u32x4 lo, hi;
+#pragma unroll
+              for (int v = 0; v < 4; ++v) {
+                lo[v] = __float_as_uint(e[8 * h + v]);
+                hi[v] = __float_as_uint(e[8 * h + 4 + v]);
+              }
+              split8(lo, hi, parts[0], parts[1], parts[2]);
+            }
+            u32x4 vt[S::kDBlocks];
+            read_v<D, h>(values + v_at[0], vt);
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll
+              for (int d = 0; d < S::kDBlocks; ++d) acc[d] = mfma_bf16(vt[d], parts[k], acc[d]);
+          });
+        } else {
+          static_for<4 * S::kDBlocks>([&](auto ic) {
+            constexpr int v4 = decltype(ic)::value / S::kDBlocks, d = decltype(ic)::value % S::kDBlocks;
+            float vv[4];
+            lds_read32x4_at<8 * v4 * T::kRowBytes + 128 * d>(v_at, values, vv);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vv[k], e[4 * v4 + k], acc[d], 0, 0, 0);
+          });
         }
       }
       lds_reads_done();
+      s = next;
+      buffer ^= 1;
     }
     // ---------------- the unit's part: wavefronts with the same queries put together
     l_run = add_halves(l_run);
@@ -890,19 +868,28 @@ int32_t launch_merge(const SharedArgs& a, hipStream_t s) {
   return launch_status();
 }
 
+// Tables that have room for no more bytes of keys and values than this, counted once for every sequence, are decoded sequence by sequence: the
+// step over pages reads them, from the last-level cache mostly, before four launches have found out what is common.  bf16, d_h 128,
+// 8 KV heads, apart and shared: 8 sequences of 4096 rows (138 MB) 24 and 38 us, 16 (277 MB) 35 and 42, 8 of 16384 (541 MB) 57 and 43,
+// 32 of 4096 (554 MB) 54 and 44; 32 bits: 8 of 4096 (277 MB) 48 and 50, 4 of 16384 (541 MB) 80 and 76.
+constexpr long long kApartBytes = 400000000;
+
 }  // namespace
 
 size_t shared_decode_bytes(const lava_layer_desc& d, int32_t batch, int32_t max_blocks) { return shared_layout(d, batch, max_blocks).bytes; }
 
 int32_t launch_shared_decode(const lava_layer_desc& d, const PagedDecodeArgs& p, int32_t n_groups, const int32_t* group_start, void* ws,
                              hipStream_t s) {
+  const SharedLayout l = shared_layout(d, p.batch, p.max_blocks);
+  char* w = static_cast<char*>(ws);
+  const long long row_bytes = 2LL * d.head_dim * (d.dtype == LAVA_BF16 ? 2 : 4);
+  const double room = (double)p.batch * p.H_kv * ((double)p.max_blocks * (1 << p.page_shift)) * row_bytes;
+  if (n_groups == p.batch || room <= (double)kApartBytes) return launch_paged_decode(d, p, w + l.off_decode, s);
   SharedArgs a;
   a.p = p;
   a.n_groups = n_groups;
   a.group_start = group_start;
   a.c2 = p.scale * kLog2e;
-  const SharedLayout l = shared_layout(d, p.batch, p.max_blocks);
-  char* w = static_cast<char*>(ws);
   a.n_items = reinterpret_cast<int*>(w);
   a.items = reinterpret_cast<SharedItem*>(w + l.off_items);
   a.parts = reinterpret_cast<SharedParts*>(w + l.off_parts);

@@ -19,5 +19,14 @@ __device__ __forceinline__ float capped(float z, float cap, float inv_cap) {
   return cap * copysignf(a < 0.25f ? series : far, y);
 }
 
+// to * tanh(z / cap) where |z| < cap / 4: the series alone.
+__device__ __forceinline__ float capped_near(float z, float to, float inv_cap) {
+  const float y = z * inv_cap, s = y * y;
+  float series = fmaf(s, 2.1869489e-2f, -5.3968254e-2f);
+  series = fmaf(s, series, 1.3333333e-1f);
+  series = fmaf(s, series, -3.3333333e-1f);
+  return to * fmaf(y * s, series, y);
+}
+
 }  // namespace
 }  // namespace lava

@@ -24,6 +24,16 @@ def dev(a):
     return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
 
 
+ROOM = 410_000_000                                                   # bytes that tables must have room for to be looked at for common pages
+
+
+def widened(table, page, row_bytes):
+    """The same tables with room for more blocks."""
+    batch, heads, blocks = table.shape
+    wide = max(blocks, -(-ROOM // (batch * heads * page * row_bytes)))
+    return np.pad(table, ((0, 0), (0, 0), (0, wide - blocks)), constant_values=-1)
+
+
 def shared_tables(rng, sizes, Hkv, page, front, own_lo, own_hi, idle=()):
     """(table, rows, pages) of groups of those sizes; front(group, head): pages in common."""
     batch = sum(sizes)
@@ -60,8 +70,10 @@ def own_weight(lse):
 
 
 class Case:
-    def __init__(self, lava, rng, H, Hkv, d, dtype, page, sizes, table, rows, n_pages, softcap=0.0, window=0, bias=False, span=None):
+    def __init__(self, lava, rng, H, Hkv, d, dtype, page, sizes, table, rows, n_pages, softcap=0.0, window=0, bias=False, span=None, narrow=False):
         self.lava, self.batch = lava, len(rows)
+        if not narrow:
+            table = widened(table, page, 2 * d * (2 if dtype == "bf16" else 4))
         dt = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.desc = lava.LayerDesc.make(H, Hkv, d, 1, dtype)
         val = lambda *s: dev(rng.normal(size=s).astype(np.float32)).to(dt)
@@ -119,7 +131,7 @@ def test_shared(lava, H, Hkv, d, dtype, page, kw):
         front = lambda i, g: (blocks * 16 // page + (i + g) % 3) if blocks else 0
         table, rows, n_pages = shared_tables(rng, sizes, Hkv, page, front, 0, 40, idle=[0] if len(sizes) == 3 else [])
         c = Case(lava, rng, H, Hkv, d, dtype, page, sizes, table, rows, n_pages, **kw)
-        ws = torch.full((lava.lava_shared_decode_workspace_bytes(c.desc, c.batch, table.shape[2]),), 0xFF, dtype=torch.uint8, device=DEV)
+        ws = torch.full((lava.lava_shared_decode_workspace_bytes(c.desc, c.batch, c.table.shape[2]),), 0xFF, dtype=torch.uint8, device=DEV)
         c.check(*c.run(workspace=ws))
 
 
@@ -149,6 +161,7 @@ def test_every_row_counts_once(lava, G, d, dtype, page, load, kw):
     Hkv, rng = 3, np.random.default_rng(len(load) + G)
     table, rows, n_pages = shared_tables(rng, sizes, Hkv, page, front, 1, own)
     batch, window = len(rows), kw.get("window", 0)
+    table = widened(table, page, 2 * d * (2 if dtype == "bf16" else 4))
     pages = Pages(G + page, n_pages, page, d, device=DEV)
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
     desc = lava.LayerDesc.make(G * Hkv, Hkv, d, 1, dtype, softmax_scale=SCALE)
@@ -239,7 +252,7 @@ def test_groups_that_are_none(lava):
 def test_wrong_counts_and_pages(lava):
     rng = np.random.default_rng(10)
     table, rows, n_pages = shared_tables(rng, [4, 5], 2, 16, lambda i, g: 8, 1, 20)
-    for what, value in (("rows", -1), ("rows", table.shape[2] * 16 + 1), ("common", -1), ("common", n_pages), ("own", n_pages)):
+    for what, value in (("rows", -1), ("rows", widened(table, 16, 512).shape[2] * 16 + 1), ("common", -1), ("common", n_pages), ("own", n_pages)):
         t, r = table.copy(), rows.copy()
         if what == "rows":
             r[2, 1] = value
@@ -256,12 +269,27 @@ def test_wrong_counts_and_pages(lava):
         c.check(out, lse)
 
 
+@pytest.mark.parametrize("page,d,dtype", [(16, 128, "bf16"), (64, 64, "f32")])
+def test_little_room_is_decoded_apart(lava, launches, page, d, dtype):
+    """Which launches a step takes follows from the room its tables have and from the number of groups, never from what they hold."""
+    rng = np.random.default_rng(15)
+    table, rows, n_pages = shared_tables(rng, [3, 4], 2, page, lambda i, g: 5, 1, 20)
+    for narrow in (True, False):
+        c = Case(lava, rng, 8, 2, d, dtype, page, [3, 4], table, rows, n_pages, narrow=narrow)
+        (out, lse), n = launches(c.run)
+        c.check(out, lse)
+        assert n["paged_decode"] == 1 and n["shared_plan"] == n["shared_decode"] == n["shared_merge"] == (0 if narrow else 1)
+    (out, lse), n = launches(lambda: c.run(start=dev(np.arange(8, dtype=np.int32))))
+    c.check(out, lse)
+    assert n["paged_decode"] == 1 and n["shared_plan"] == 0
+
+
 def test_without_lse_and_replayed(lava):
     rng = np.random.default_rng(12)
     table, rows, n_pages = shared_tables(rng, [6, 1, 5], 4, 32, lambda i, g: 9 + g, 1, 70)
     c = Case(lava, rng, 16, 4, 128, "bf16", 32, [6, 1, 5], table, rows, n_pages, softcap=25.0, bias=True)
     want, want_lse = c.run()
-    ws = torch.empty(lava.lava_shared_decode_workspace_bytes(c.desc, c.batch, table.shape[2]), dtype=torch.uint8, device=DEV)
+    ws = torch.empty(lava.lava_shared_decode_workspace_bytes(c.desc, c.batch, c.table.shape[2]), dtype=torch.uint8, device=DEV)
     out, lse = torch.empty_like(want), torch.empty_like(want_lse)
     import ctypes
     status = lava.lib.lava_shared_decode(ctypes.byref(c.desc), c.batch, c.q.data_ptr(), c.pool._ref, c.table.data_ptr(), c.rows.data_ptr(), 3,
@@ -312,16 +340,18 @@ def test_binding_refuses(lava):
 
 # ------------------------------------------------------------------------------------------- all of them together
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_beam_search(lava, dtype):
+@pytest.mark.parametrize("room", ["narrow", "wide"])
+def test_beam_search(lava, dtype, room):
     """Two prompts of a small model of one layer: their evicted caches go to pages, become four beams each, and every step picks continuations,
     reorders, appends and attends; halfway the caches are evicted again, at the end one search is over.  Every beam's own history, kept as
     plain lists on the host, gives what it should see."""
-    H, Hkv, d, page, blocks, beams, prompts, V = 8, 2, 64, 16, 12, 4, 2, 97
+    H, Hkv, d, page, beams, prompts, V = 8, 2, 64, 16, 4, 2, 97
+    blocks = 12 if room == "narrow" else -(-ROOM // (8 * 2 * 16 * 2 * 64 * (2 if dtype == "bf16" else 4)))
     batch, heads = prompts * beams, Hkv
     rng = np.random.default_rng(31 if dtype == "bf16" else 32)
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
     desc = lava.LayerDesc.make(H, Hkv, d, 1, dtype)
-    n_pages = batch * heads * blocks
+    n_pages = batch * heads * 12
     k, v = (torch.full((n_pages, page, d), float("nan"), dtype=dt, device=DEV) for _ in range(2))
     pos = torch.full((n_pages, page), -1, dtype=torch.int32, device=DEV)
     pool = lava.PagePool(k, v, pos, max_blocks=blocks)
