@@ -3,13 +3,14 @@
 //   out = (e^(m_c) a_c + e^(m_o) a_o) / (e^(m_c) l_c + e^(m_o) l_o),   m, l, a: maximum, sum and weighted values of either,
 // and the common part of all n sequences of a group with G query heads a KV head is one matrix product of n * G queries.
 //
-//   plan    a workgroup per group and head: leading blocks that the tables of all its sequences have in common; tables of what is
-//           left, for the decode step over pages; the list of items: up to 256 / G sequences of a group, one head
-//   common  the items' rows, cut into equal units of stages (64 KiB of keys and values) for as many workgroups as the device holds
-//   own     the decode step over pages, over the tables of what is left
+//   plan    a workgroup per group and head: leading blocks that the tables of all its sequences have in common; what is left; the list
+//           of items: up to 256 / G sequences of a group, one head
+//   rows    the items' rows, cut into equal units of stages (64 KiB of keys and values) for as many workgroups as the device holds; then,
+//           of up to kOwnHeads heads, what is left of each, whose queries are the G of one sequence, by whoever is done
+//   own     of more heads: the decode step over pages, over tables of what is left
 //   merge   the parts of the common rows and the own ones, per sequence and head
 //
-// Common rows: a workgroup of eight wavefronts.  A stage's keys and values come to LDS by direct-to-LDS loads, one stage ahead (in a
+// Rows: a workgroup of eight wavefronts.  A stage's keys and values come to LDS by direct-to-LDS loads, one stage ahead (in a
 // window only stages that hold a row of it).  A wavefront has 32 queries as the columns of its products and takes every n-th tile of
 // 32 rows, n = 8 / tiles of queries:
 //   logits  K_tile x Q^T: a lane has 16 of a query's 32 logits
@@ -21,10 +22,10 @@
 // Rows that are masked may hold anything there.  A product cannot leave them out, so an item whose sums are not all
 // finite is marked, and merge computes its heads' outputs again, row by row.
 //
-// Bound by HBM for few queries: 4 groups of 2 sequences with 8 KV heads of 65536 rows (1.07 GB) 4.9 TB/s.  By the matrix cores for many: 64
-// sequences over 8 heads of 131072 rows need 275 GFLOP with the three parts, 265 us, 1.04 PFLOP/s, where a large matrix product of the
-// library reaches 1.12.  32 bits: by the 32-bit matrix instructions, which two or four of the eight wavefronts of few
-// queries issue.
+// Bound by HBM for few queries: 4 groups of 4 sequences with 8 KV heads of 65536 rows (1.07 GB) 208 us a step, 5.2 TB/s.  By the matrix
+// cores for many: 64 sequences over 8 heads of 131072 rows need 275 GFLOP with the three parts, 265 us, 1.04 PFLOP/s, where a large matrix
+// product of the library reaches 1.12; with own rows, 26 us by themselves, 294 in one launch.  32 bits: by the 32-bit matrix
+// instructions, which two or four of the eight wavefronts of few queries issue.
 #include <math.h>
 
 #include "common.h"
@@ -42,7 +43,7 @@ constexpr int kStageBytes = 65536;             // keys and values
 
 struct SharedItem {
   int first_seq, n_seq, head, rows;            // rows in common
-  int lead;                                    // a sequence that holds them
+  int lead, skip;                              // a sequence that holds them, its blocks before them
 };
 struct SharedParts {
   int row, units;                              // first row of its parts, number of parts (each n_seq * G rows)
@@ -53,13 +54,15 @@ struct SharedArgs {
   int n_groups;
   const int32_t* group_start;
   float c2;
-  int* n_items;
+  int own_here;                                // own rows are units too; else the decode step over pages has them
+  int own_base;                                // first row of the parts of own rows
+  int* n_items;                                // number of items; units that were taken out of turn
   SharedItem* items;
-  SharedParts* parts;                          // [items]
-  int* marked;                                 // [items] sums that are not finite
+  SharedParts *parts, *own_parts;              // [items], [batch][H_kv]
+  int *marked, *own_marked;                    // [items], [batch][H_kv] sums that are not finite
   int* item_of;                                // [batch][H_kv] item that has the sequence's common rows, -1: none
-  int* rest_rows;                              // [batch][H_kv]
-  int* rest_table;                             // [batch][H_kv][max_blocks]
+  int *rest_rows, *skip;                       // [batch][H_kv] rows that are left (as a unit's: -1 if there cannot be as many), blocks in common
+  int* rest_table;                             // [batch][H_kv][max_blocks] where own rows are decoded by themselves
   float* rest_lse;                             // [batch][H]
   float2* part_ml;                             // [rows] maximum (log2 units) and sum
   float* part_acc;                             // [rows][D]
@@ -98,7 +101,10 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
     before += s_before[w];
     all += s_all[w];
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.n_items[0] = bad ? 0 : all * p.H_kv;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    a.n_items[0] = bad ? 0 : all * p.H_kv;
+    a.n_items[1] = 0;
+  }
   // groups that are none: every sequence by itself
   const int b0 = bad ? group : a.group_start[group], b1 = bad ? p.batch : a.group_start[group + 1], step = bad ? a.n_groups : 1;
   int common = 0, lead = 0x7fffffff;
@@ -172,6 +178,7 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
     it.head = g;
     it.rows = common << p.page_shift;
     it.lead = common > 0 ? lead : b0;
+    it.skip = 0;
     a.items[item0 + i] = it;
     a.marked[item0 + i] = 0;
   }
@@ -189,7 +196,7 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
     for (int i = 0; i < 4; ++i) {
       const bool there = c0 + i * kPlanShWaves * step < b1;
       skip[i] = rows[i] == 0 ? 0 : common;
-      left[i] = !there || rows[i] <= 0 || rows[i] > p.max_blocks << p.page_shift ? 0 : ((rows[i] + P - 1) >> p.page_shift) - skip[i];
+      left[i] = a.own_here != 0 || !there || rows[i] <= 0 || rows[i] > p.max_blocks << p.page_shift ? 0 : ((rows[i] + P - 1) >> p.page_shift) - skip[i];
       y[i] = lane < left[i] ? p.block_table[h[i] * p.max_blocks + skip[i] + lane] : 0;
     }
 #pragma unroll
@@ -197,7 +204,10 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
       const int b = c0 + i * kPlanShWaves * step;
       if (b >= b1) continue;
       if (lane == 0) {
-        a.rest_rows[h[i]] = rows[i] - (skip[i] << p.page_shift);
+        const bool none = rows[i] < 0 || rows[i] > p.max_blocks << p.page_shift;
+        a.rest_rows[h[i]] = a.own_here != 0 && none ? -1 : rows[i] - (skip[i] << p.page_shift);
+        a.skip[h[i]] = skip[i];
+        a.own_marked[h[i]] = 0;
         a.item_of[h[i]] = skip[i] > 0 ? item0 + (b - b0) / seqs : -1;
       }
       int* to = a.rest_table + h[i] * p.max_blocks;
@@ -207,10 +217,14 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
   }
 }
 
-// ---------------------------------------------------------------- common rows
+// ---------------------------------------------------------------- rows
 // A probability is relative to a maximum that moves only when a logit exceeds it by more than this (in log2 units): sums grow by 2^8 at
 // most, and half of the tiles need no rescaling of the output (296 -> 283 us).
 constexpr float kSlack = 8.0f;
+
+// (sequence, head) pairs whose own rows are units of the same launch, at most.  A launch of their own costs more than it does (64 sequences
+// of 131072 rows 315 -> 304 us, ragged ones 90 -> 85); more are many small units, and their number is found again by every workgroup.
+constexpr int kOwnHeads = 512;
 
 template <int DT, int D>
 struct ShShape {
@@ -292,19 +306,27 @@ __device__ __forceinline__ void read_k(unsigned int at, u32x4 (&k)[STEPS]) {
 }
 
 template <int DT, int D, bool OPT>
-__global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const SharedArgs a) {
+__global__ void __launch_bounds__(kShThreads, 2) shared_rows_kernel(const SharedArgs a) {
   using S = ShShape<DT, D>;
   using T = Tile<DT, D>;
   __shared__ __attribute__((aligned(1024))) u32x4 s_stage[2][kStageBytes / 16];   // (addresses are formed by exclusive or) keys' tiles, then values'; between units: float [kShWaves][32][D]
   __shared__ __attribute__((aligned(16))) int s_pos[2][OPT ? S::kStageRows : 4];
   __shared__ float s_m[kShWaves][32], s_l[kShWaves][32];
   __shared__ unsigned long long s_seen[kShWaves];
-  __shared__ int s_wrong;
+  __shared__ int s_wrong, s_next, s_first[kOwnHeads];        // the next unit; of every head the units of own rows before it
   const PagedDecodeArgs& p = a.p;
   const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 31, half = lane >> 5;
   const int n_items = a.n_items[0];
-  // stages of all items, items that have any
-  auto stages_of = [&](int i) { return i < n_items ? (a.items[i].rows + S::kStageRows - 1) / S::kStageRows : 0; };
+  auto stages_in = [](int rows) { return rows > 0 ? (int)(((unsigned int)rows + S::kStageRows - 1u) / S::kStageRows) : 0; };
+  auto stages_of = [&](int i) { return i < n_items ? stages_in(a.items[i].rows) : 0; };
+  const unsigned int wgs = gridDim.x;
+  const bool windowed = OPT && p.window > 0;
+  // Units of `share` stages of one item or head: no more units than workgroups where those are few; twice as many where parts of the
+  // rows are out of the window, so that they are spread.
+  auto share_of = [&](unsigned int total, unsigned int full) {
+    const unsigned int cut = 2u * full <= wgs && !windowed ? wgs - full : 2u * wgs;
+    return (int)((total + cut - 1u) / cut);
+  };
   unsigned int total = 0u, full = 0u;
   for (int i = lane; i < n_items; i += 64) {
     const int n = stages_of(i);
@@ -313,13 +335,39 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
   }
   total = lane_value(wave_incl(total), 63);
   full = lane_value(wave_incl(full), 63);
-  if (total == 0u) return;
-  // units of `share` stages of one item: no more units than workgroups where items are few
-  const unsigned int wgs = gridDim.x;
-  const bool windowed = OPT && p.window > 0;
-  // twice as many where parts of the rows are out of the window, so that they are spread
-  const unsigned int cut = 2u * full <= wgs && !windowed ? wgs - full : 2u * wgs;
-  const int share = (int)((total + cut - 1u) / cut);
+  const int share = total > 0u ? share_of(total, full) : 1;
+  const int own_heads = a.own_here != 0 ? p.batch * p.H_kv : 0;   // <= kOwnHeads
+  constexpr int kOwnEach = kOwnHeads / 64;
+  unsigned int common_units = 0u, own_units = 0u;
+  int own_share = 1;
+  {
+    unsigned int n = 0u;
+    for (int i = lane; i < n_items; i += 64) n += (unsigned int)(stages_of(i) + share - 1) / (unsigned int)share;
+    common_units = lane_value(wave_incl(n), 63);
+  }
+  if (own_heads > 0) {                                         // uniform; every wavefront finds the same
+    int held[kOwnEach];
+    unsigned int own = 0u, some = 0u;
+#pragma unroll
+    for (int c = 0; c < kOwnEach; ++c) held[c] = 64 * c + lane < own_heads ? a.rest_rows[64 * c + lane] : 0;
+#pragma unroll
+    for (int c = 0; c < kOwnEach; ++c) {
+      held[c] = stages_in(held[c]);
+      own += (unsigned int)held[c];
+      some += held[c] > 0 ? 1u : 0u;
+    }
+    own = lane_value(wave_incl(own), 63);
+    some = lane_value(wave_incl(some), 63);
+    if (own > 0u) own_share = share_of(own, some);
+#pragma unroll
+    for (int c = 0; c < kOwnEach; ++c) {
+      const unsigned int n = (unsigned int)(held[c] + own_share - 1) / (unsigned int)own_share, incl = wave_incl(n);
+      if (wave == 0) s_first[64 * c + lane] = (int)(own_units + incl - n);
+      own_units += lane_value(incl, 63);
+    }
+    __syncthreads();
+  }
+  const unsigned int all_units = common_units + own_units;
 
   TileDma<DT, D> dma;
   dma.init(lane);
@@ -347,13 +395,16 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
   const float inv_cap = p.cap > 0.0f ? 1.0f / p.cap : 0.0f;
   const unsigned int window = p.window > 0 ? (unsigned int)p.window : 0x80000000u;
 
-  for (unsigned int u = blockIdx.x;; u += wgs) {
+  for (unsigned int u = blockIdx.x; u < all_units;) {
+    unsigned int next_unit = 0u;                               // of thread 0; asked for now, needed when this unit is done
+    if (threadIdx.x == 0) next_unit = wgs + __hip_atomic_fetch_add(reinterpret_cast<unsigned int*>(&a.n_items[1]), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     // ---------------- the unit: its item, its part of the item, where its rows go
-    int item = -1, part = 0, units = 0, row0 = 0;
-    {
+    int item = -1, part = 0, units = 0, row0 = 0, unit_share = share;
+    SharedItem it;
+    if (u < common_units) {
       unsigned int at = 0u, rows = 0u;
       for (int i0 = 0; i0 < n_items && item < 0; i0 += 64) {
-        const int n = (stages_of(i0 + lane) + share - 1) / share;
+        const int n = (int)((unsigned int)(stages_of(i0 + lane) + share - 1) / (unsigned int)share);
         const int mine = n > 0 ? n * a.items[i0 + lane].n_seq * p.G : 0;
         const unsigned int incl = wave_incl((unsigned int)n), r_incl = wave_incl((unsigned int)mine);
         const unsigned long long after = __ballot(at + incl > u);
@@ -368,15 +419,31 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
           rows += lane_value(r_incl, 63);
         }
       }
+      it = a.items[item];
+      if (part == 0 && threadIdx.x == 0) a.parts[item] = SharedParts{row0, units};
+    } else {
+      const int v = (int)(u - common_units);
+      int h = -1;
+#pragma unroll
+      for (int c = 0; c < kOwnEach; ++c)
+        h += __popcll(__ballot(64 * c + lane < own_heads && s_first[64 * c + lane] <= v));   // heads without units share the next one's number
+      const int end = h + 1 < own_heads ? s_first[h + 1] : (int)own_units;
+      part = v - s_first[h];
+      units = end - s_first[h];
+      row0 = a.own_base + s_first[h] * p.G;
+      unit_share = own_share;
+      it.first_seq = it.lead = h / p.H_kv;
+      it.n_seq = 1;
+      it.head = h - it.first_seq * p.H_kv;
+      it.rows = a.rest_rows[h];
+      it.skip = a.skip[h];
+      if (part == 0 && threadIdx.x == 0) a.own_parts[h] = SharedParts{row0, units};
     }
-    if (item < 0) return;                                      // uniform: no unit left
-    const SharedItem it = a.items[item];
     const int q_rows = it.n_seq * p.G;
-    if (part == 0 && threadIdx.x == 0) a.parts[item] = SharedParts{row0, units};
     const int row_tiles = q_rows <= 32 ? 1 : q_rows <= 64 ? 2 : q_rows <= 128 ? 4 : 8;
     const int rt = wave & (row_tiles - 1), kp = wave / row_tiles, key_parts = kShWaves / row_tiles;
-    const int s0 = part * share, s_all = (it.rows + S::kStageRows - 1) / S::kStageRows, s1 = s0 + share < s_all ? s0 + share : s_all;
-    const int* table = p.block_table + ((long long)it.lead * p.H_kv + it.head) * p.max_blocks;
+    const int s0 = part * unit_share, s_all = stages_in(it.rows), s1 = s0 + unit_share < s_all ? s0 + unit_share : s_all;
+    const int* table = p.block_table + ((long long)it.lead * p.H_kv + it.head) * p.max_blocks + it.skip;
 
     // ---------------- the queries of this lane's column
     const int qr = rt * 32 + col;
@@ -503,8 +570,20 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
           const int k = wave + kShWaves * x;
           if (k < S::kHalves && lane < 16) lds_write32(lds_addr(&s_pos[buffer][16 * k + lane]), __int_as_float(pos_next[x]));
         }
-        lds_reads_done();
       }
+      if ((s + 1) * S::kStageRows > it.rows) {                 // uniform: rows behind the last one weigh nothing, whatever was there
+#pragma unroll
+        for (int x = 0; x < 4 * S::kTiles / kShWaves; ++x) {
+          const int k = wave + kShWaves * x, hh = k % S::kHalves, left = it.rows - s * S::kStageRows - 16 * hh;
+          if (k < S::kHalves || left >= 16) continue;          // keys: their logits are masked
+          const unsigned int row = lds_addr(&s_stage[buffer][S::kTiles * T::kTileChunks + hh * (T::kTileChunks / 2)]) + (unsigned int)(lane >> 2) * T::kRowBytes;
+          const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          if ((lane >> 2) >= left)
+#pragma unroll
+            for (int c = 0; c < T::kRowBytes / 64; ++c) lds_write128(row + (unsigned int)(16 * (4 * c + (lane & 3))), zero);
+        }
+      }
+      lds_reads_done();
       __syncthreads();                                         // the stage is there, the other one free
       const int next = next_stage();
       if (next >= 0) issue(next, sb, buffer ^ 1);
@@ -552,9 +631,9 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
             }
           }
         }
-        if (r0 + 32 > it.rows) {                               // uniform: the second half tile is behind the last row
+        if (r0 + 32 > it.rows) {                               // uniform: some are behind the last row
 #pragma unroll
-          for (int v = 8; v < 16; ++v) x[v] = -INFINITY;
+          for (int v = 0; v < 16; ++v) x[v] = r0 + 8 * (v / 4) + 4 * half + v % 4 < it.rows ? x[v] : -INFINITY;
         }
         float top = x[0];
 #pragma unroll
@@ -640,7 +719,10 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
             make_float4(acc[d][4 * v4], acc[d][4 * v4 + 1], acc[d][4 * v4 + 2], acc[d][4 * v4 + 3]);
       }
     __syncthreads();
-    if (s_wrong != 0 && threadIdx.x == 0) atomicOr(&a.marked[item], s_wrong);
+    if (threadIdx.x == 0) {
+      if (s_wrong != 0) atomicOr(item >= 0 ? &a.marked[item] : &a.own_marked[it.first_seq * p.H_kv + it.head], s_wrong);
+      s_next = (int)next_unit;
+    }
     const long long out0 = (long long)row0 + (long long)part * q_rows;
     for (int i = threadIdx.x; i < q_rows * kChunks; i += kShThreads) {
       const int r = i / kChunks, c = i - r * kChunks, w0 = r >> 5, cr = r & 31;
@@ -663,6 +745,7 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_common_kernel(const Shar
       if (c == 0) a.part_ml[out0 + r] = make_float2(M, L);
     }
     __syncthreads();                                           // the next unit may use LDS
+    u = (unsigned int)__builtin_amdgcn_readfirstlane(s_next);
   }
 }
 
@@ -747,37 +830,54 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
   const PagedDecodeArgs& p = a.p;
   const int b = blockIdx.x / p.H_kv, g = blockIdx.x - b * p.H_kv;
   const int item = a.item_of[blockIdx.x];
+  const bool here = a.own_here != 0;
   const long long row0 = (long long)b * p.H + (long long)g * p.G;
-  if (item < 0) {                                              // nothing in common: the own rows were all
+  if (item < 0 && !here) {                                     // nothing in common: the own rows were all
     if (p.lse != nullptr && (int)threadIdx.x < p.G) p.lse[row0 + threadIdx.x] = a.rest_lse[row0 + threadIdx.x];
     return;
   }
-  const int marked = a.marked[item];
+  const int rest = here ? a.rest_rows[blockIdx.x] : 0;
+  const int marked = (item >= 0 ? a.marked[item] : 0) | (here ? a.own_marked[blockIdx.x] : 0);
   if (marked == 1) {                                           // no page was wrong: only values
     whole_head<DT, D>(a, b, g, s_red);
     return;
   }
-  const SharedItem it = a.items[item];
-  const SharedParts parts = a.parts[item];
-  const int q_rows = it.n_seq * p.G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long first0 = parts.row + (long long)(b - it.first_seq) * p.G;
+  // parts 0 .. n_common - 1 are the common rows', n_common .. n - 1 the own ones'
+  int n_common = 0, n = 0, common_step = 0;
+  long long common0 = 0, own0 = 0;
+  if (item >= 0) {
+    const SharedItem it = a.items[item];
+    const SharedParts x = a.parts[item];
+    common_step = it.n_seq * p.G;
+    common0 = x.row + (long long)(b - it.first_seq) * p.G;
+    n = n_common = x.units;
+  }
+  if (rest > 0) {
+    const SharedParts x = a.own_parts[blockIdx.x];
+    own0 = x.row;
+    n += x.units;
+  }
+  auto row_of = [&](int u, int t) {
+    return u < n_common ? common0 + t + (long long)u * common_step : own0 + t + (long long)(u - n_common) * p.G;
+  };
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // a wavefront a query: the maximum over its parts, then their weights
   for (int t = wave; t < p.G; t += kMergeThreads / 64) {
-    const float own = a.rest_lse[row0 + t] * kLog2e;
+    const float own = here ? -INFINITY : a.rest_lse[row0 + t] * kLog2e;
     float M = own, L = 0.0f;
-    for (int u = lane; u < parts.units; u += 64) M = fmaxf(M, a.part_ml[first0 + t + (long long)u * q_rows].x);
+    for (int u = lane; u < n; u += 64) M = fmaxf(M, a.part_ml[row_of(u, t)].x);
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) M = fmaxf(M, __shfl_xor(M, m));
     const float base = M == -INFINITY ? 0.0f : M;
-    for (int u = lane; u < parts.units; u += 64) {
-      const float2 ml = a.part_ml[first0 + t + (long long)u * q_rows];
+    for (int u = lane; u < n; u += 64) {
+      const float2 ml = a.part_ml[row_of(u, t)];
       L += fast_exp2(ml.x - base) * ml.y;
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) L += __shfl_xor(L, m);
     const float wgt = fast_exp2(own - base);
     L += wgt;
-    if (marked != 0 || isnan(own)) L = NAN;                    // a page that is not in the pool, of the common ones or the own
+    if (marked != 0 || isnan(own) || rest < 0) L = NAN;        // a page that is not in the pool, or rows that cannot be
     if (lane == 0) {
       s_base[t] = base;
       s_own[t] = wgt;
@@ -791,20 +891,23 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
     const int t = i / (D / 4), c = i - t * (D / 4);
     const float base = s_base[t], L = s_sum[t], wgt = s_own[t];
     float4* out = reinterpret_cast<float4*>(p.out + (row0 + t) * D) + c;
-    const float4 mine = *out;
-    float4 sum = make_float4(wgt * mine.x, wgt * mine.y, wgt * mine.z, wgt * mine.w);
-    for (int u0 = 0; u0 < parts.units; u0 += kLoads) {
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (!here) {
+      const float4 mine = *out;
+      sum = make_float4(wgt * mine.x, wgt * mine.y, wgt * mine.z, wgt * mine.w);
+    }
+    for (int u0 = 0; u0 < n; u0 += kLoads) {
       float m[kLoads];
       float4 y[kLoads];
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {                       // behind the last part: the last one, at no weight
-        const long long r = first0 + t + (long long)(u0 + u < parts.units ? u0 + u : parts.units - 1) * q_rows;
+        const long long r = row_of(u0 + u < n ? u0 + u : n - 1, t);
         m[u] = a.part_ml[r].x;
         y[u] = *reinterpret_cast<const float4*>(a.part_acc + r * D + 4 * c);
       }
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
-        const float w = u0 + u < parts.units ? fast_exp2(m[u] - base) : 0.0f;
+        const float w = u0 + u < n ? fast_exp2(m[u] - base) : 0.0f;
         sum.x += w * y[u].x;
         sum.y += w * y[u].y;
         sum.z += w * y[u].z;
@@ -815,32 +918,30 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
   }
 }
 
-template <typename K>
-int resident_shared(K kernel) {
-  int per = 0;
-  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kShThreads, 0) != hipSuccess || per < 1) {
-    discard_stale_error();
-    per = 1;
-  }
-  return device_cus();                                         // a stage and the next one take more than half of a compute unit's LDS
-}
+bool own_is_here(const lava_layer_desc& d, int32_t batch) { return (int64_t)batch * d.n_kv_heads <= kOwnHeads; }
 
 struct SharedLayout {
-  size_t off_items, off_parts, off_marked, off_item_of, off_rest_rows, off_rest_table, off_rest_lse, off_ml, off_acc, off_decode, bytes;
+  size_t off_items, off_parts, off_own_parts, off_marked, off_own_marked, off_item_of, off_rest_rows, off_skip, off_rest_table, off_rest_lse, off_ml, off_acc;
+  size_t off_decode, bytes, own_base;
 };
 SharedLayout shared_layout(const lava_layer_desc& d, int32_t batch, int32_t max_blocks) {
   const size_t heads = (size_t)batch * d.n_kv_heads, G = d.n_q_heads / d.n_kv_heads;
   const size_t widest = batch * G < (size_t)kShRows ? batch * G : (size_t)kShRows;
-  // parts: `cut` units of whole shares at most, of the widest items, and one more unit an item
-  const size_t rows = 2 * (size_t)device_cus() * widest + (size_t)batch * d.n_q_heads;
+  // parts: `cut` units of whole shares at most, of the widest items, and one more unit an item; the same of the heads' own rows
+  const size_t most = 2 * (size_t)device_cus(), all = (size_t)batch * d.n_q_heads;
   SharedLayout l;
-  l.off_items = align_up(sizeof(int));
+  l.own_base = most * widest + all;
+  const size_t rows = l.own_base + (own_is_here(d, batch) ? most * G + all : 0);
+  l.off_items = align_up(2 * sizeof(int));
   l.off_parts = l.off_items + align_up(heads * sizeof(SharedItem));
-  l.off_marked = l.off_parts + align_up(heads * sizeof(SharedParts));
-  l.off_item_of = l.off_marked + align_up(heads * 4);
+  l.off_own_parts = l.off_parts + align_up(heads * sizeof(SharedParts));
+  l.off_marked = l.off_own_parts + align_up(heads * sizeof(SharedParts));
+  l.off_own_marked = l.off_marked + align_up(heads * 4);
+  l.off_item_of = l.off_own_marked + align_up(heads * 4);
   l.off_rest_rows = l.off_item_of + align_up(heads * 4);
-  l.off_rest_table = l.off_rest_rows + align_up(heads * 4);
-  l.off_rest_lse = l.off_rest_table + align_up(heads * max_blocks * 4);
+  l.off_skip = l.off_rest_rows + align_up(heads * 4);
+  l.off_rest_table = l.off_skip + align_up(heads * 4);
+  l.off_rest_lse = l.off_rest_table + (own_is_here(d, batch) ? 0 : align_up(heads * max_blocks * 4));
   l.off_ml = l.off_rest_lse + align_up((size_t)batch * d.n_q_heads * 4);
   l.off_acc = l.off_ml + align_up(rows * sizeof(float2));
   l.off_decode = l.off_acc + align_up(rows * d.head_dim * sizeof(float));
@@ -848,16 +949,15 @@ SharedLayout shared_layout(const lava_layer_desc& d, int32_t batch, int32_t max_
   return l;
 }
 
+// A stage and the next one take more than half of a compute unit's LDS: one workgroup each.
 template <int DT, int D>
-int32_t launch_common(const SharedArgs& a, hipStream_t s) {
+int32_t launch_rows(const SharedArgs& a, hipStream_t s) {
   ProfScope ps(KID_SHARED_DECODE, s);
-  if (a.p.pos != nullptr || a.p.cap > 0.0f) {
-    static const int wgs = resident_shared(shared_common_kernel<DT, D, true>);
-    hipLaunchKernelGGL((shared_common_kernel<DT, D, true>), dim3((unsigned)wgs), dim3(kShThreads), 0, s, a);
-  } else {
-    static const int wgs = resident_shared(shared_common_kernel<DT, D, false>);
-    hipLaunchKernelGGL((shared_common_kernel<DT, D, false>), dim3((unsigned)wgs), dim3(kShThreads), 0, s, a);
-  }
+  const dim3 wgs((unsigned)device_cus());
+  if (a.p.pos != nullptr || a.p.cap > 0.0f)
+    hipLaunchKernelGGL((shared_rows_kernel<DT, D, true>), wgs, dim3(kShThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((shared_rows_kernel<DT, D, false>), wgs, dim3(kShThreads), 0, s, a);
   return launch_status();
 }
 
@@ -869,9 +969,9 @@ int32_t launch_merge(const SharedArgs& a, hipStream_t s) {
 }
 
 // Tables that have room for no more bytes of keys and values than this, counted once for every sequence, are decoded sequence by sequence: the
-// step over pages reads them, from the last-level cache mostly, before four launches have found out what is common.  bf16, d_h 128,
-// 8 KV heads, apart and shared: 8 sequences of 4096 rows (138 MB) 24 and 38 us, 16 (277 MB) 35 and 42, 8 of 16384 (541 MB) 57 and 43,
-// 32 of 4096 (554 MB) 54 and 44; 32 bits: 8 of 4096 (277 MB) 48 and 50, 4 of 16384 (541 MB) 80 and 76.
+// step over pages reads them, from the last-level cache mostly, before three launches have found out what is common.  bf16, d_h 128,
+// 8 KV heads, apart and shared: 8 sequences of 4096 rows (138 MB) 24 and 36 us, 16 (277 MB) 35 and 40, 8 of 16384 (541 MB) 56 and 40,
+// 4 groups of 8 of 4096 (554 MB) 55 and 41; 32 bits: 8 of 4096 (277 MB) 48 and 50, 4 of 16384 (541 MB) 80 and 76.
 constexpr long long kApartBytes = 400000000;
 
 }  // namespace
@@ -893,7 +993,12 @@ int32_t launch_shared_decode(const lava_layer_desc& d, const PagedDecodeArgs& p,
   a.n_items = reinterpret_cast<int*>(w);
   a.items = reinterpret_cast<SharedItem*>(w + l.off_items);
   a.parts = reinterpret_cast<SharedParts*>(w + l.off_parts);
+  a.own_here = own_is_here(d, p.batch) ? 1 : 0;
+  a.own_base = (int)l.own_base;
+  a.own_parts = reinterpret_cast<SharedParts*>(w + l.off_own_parts);
   a.marked = reinterpret_cast<int*>(w + l.off_marked);
+  a.own_marked = reinterpret_cast<int*>(w + l.off_own_marked);
+  a.skip = reinterpret_cast<int*>(w + l.off_skip);
   a.item_of = reinterpret_cast<int*>(w + l.off_item_of);
   a.rest_rows = reinterpret_cast<int*>(w + l.off_rest_rows);
   a.rest_table = reinterpret_cast<int*>(w + l.off_rest_table);
@@ -907,9 +1012,9 @@ int32_t launch_shared_decode(const lava_layer_desc& d, const PagedDecodeArgs& p,
   int32_t st = launch_status();
   const bool bf16 = d.dtype == LAVA_BF16, wide = d.head_dim == 128;
   if (st == LAVA_OK)
-    st = bf16 ? (wide ? launch_common<LAVA_BF16, 128>(a, s) : launch_common<LAVA_BF16, 64>(a, s))
-              : (wide ? launch_common<LAVA_F32, 128>(a, s) : launch_common<LAVA_F32, 64>(a, s));
-  if (st == LAVA_OK) {
+    st = bf16 ? (wide ? launch_rows<LAVA_BF16, 128>(a, s) : launch_rows<LAVA_BF16, 64>(a, s))
+              : (wide ? launch_rows<LAVA_F32, 128>(a, s) : launch_rows<LAVA_F32, 64>(a, s));
+  if (st == LAVA_OK && a.own_here == 0) {
     PagedDecodeArgs own = p;
     own.block_table = a.rest_table;
     own.head_rows = a.rest_rows;

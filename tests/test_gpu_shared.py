@@ -182,15 +182,19 @@ def test_every_row_counts_once(lava, G, d, dtype, page, load, kw):
     assert bool(((lse.double() - want_lse).abs() <= tol_lse + weight)[some].all())
 
 
+IDLE = pytest.mark.parametrize("idle", [0, 260], ids=["few", "many"])   # sequences that hold nothing: own rows of 512 heads and more are decoded apart
+
+
+@IDLE
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
-def test_masked_values_may_be_anything(lava, dtype, d):
+def test_masked_values_may_be_anything(lava, dtype, d, idle):
     """Infinities and NaN in rows that a window leaves out, for all of a group or for some of its sequences only, and behind last rows."""
     rng = np.random.default_rng(3)
     H, Hkv, page = 8, 2, 16
-    sizes = [4, 3]
-    table, rows, n_pages = shared_tables(rng, sizes, Hkv, page, lambda i, g: 12 + g, 1, 30)
+    sizes = [4, 3, idle]
+    table, rows, n_pages = shared_tables(rng, sizes, Hkv, page, lambda i, g: 12 + g, 1, 30, idle=range(7, 7 + idle))
     c = Case(lava, rng, H, Hkv, d, dtype, page, sizes, table, rows, n_pages, window=100, span=400)
-    c.q_pos[:] = dev(np.array([399, 399, 350, 310, 300, 300, 300], np.int32))
+    c.q_pos[:7] = dev(np.array([399, 399, 350, 310, 300, 300, 300], np.int32))
     inf = float("inf")
     low, high = c.pos < 200, c.pos >= 399                              # nobody sees the first; the last one some
     for t in (c.k, c.v):
@@ -249,9 +253,10 @@ def test_groups_that_are_none(lava):
     assert torch.equal(out, plain[0]) and torch.equal(lse, plain[1])   # alone, every sequence is decoded as it is
 
 
-def test_wrong_counts_and_pages(lava):
+@IDLE
+def test_wrong_counts_and_pages(lava, idle):
     rng = np.random.default_rng(10)
-    table, rows, n_pages = shared_tables(rng, [4, 5], 2, 16, lambda i, g: 8, 1, 20)
+    table, rows, n_pages = shared_tables(rng, [4, 5, idle], 2, 16, lambda i, g: 8, 1, 20, idle=range(9, 9 + idle))
     for what, value in (("rows", -1), ("rows", widened(table, 16, 512).shape[2] * 16 + 1), ("common", -1), ("common", n_pages), ("own", n_pages)):
         t, r = table.copy(), rows.copy()
         if what == "rows":
@@ -260,10 +265,10 @@ def test_wrong_counts_and_pages(lava):
             t[:4, 0, 5] = value
         else:
             t[6, 1, rows[6, 1] // 16 if rows[6, 1] % 16 else rows[6, 1] // 16 - 1] = value
-        c = Case(lava, np.random.default_rng(11), 8, 2, 128, "bf16", 16, [4, 5], t, r, n_pages)
+        c = Case(lava, np.random.default_rng(11), 8, 2, 128, "bf16", 16, [4, 5, idle], t, r, n_pages)
         out, lse = c.run()
-        bad = torch.isnan(lse).view(9, 2, 4).all(2).cpu().numpy()
-        want = np.zeros((9, 2), bool)
+        bad = torch.isnan(lse).view(9 + idle, 2, 4).all(2).cpu().numpy()
+        want = np.zeros((9 + idle, 2), bool)
         want[(2, 1) if what == "rows" else (slice(0, 4), 0) if what == "common" else (6, 1)] = True
         assert np.array_equal(bad, want), what
         c.check(out, lse)
@@ -271,15 +276,17 @@ def test_wrong_counts_and_pages(lava):
 
 @pytest.mark.parametrize("page,d,dtype", [(16, 128, "bf16"), (64, 64, "f32")])
 def test_little_room_is_decoded_apart(lava, launches, page, d, dtype):
-    """Which launches a step takes follows from the room its tables have and from the number of groups, never from what they hold."""
+    """Which launches a step takes follows from the room its tables have, from the number of heads and of groups, never from what they hold."""
     rng = np.random.default_rng(15)
-    table, rows, n_pages = shared_tables(rng, [3, 4], 2, page, lambda i, g: 5, 1, 20)
-    for narrow in (True, False):
-        c = Case(lava, rng, 8, 2, d, dtype, page, [3, 4], table, rows, n_pages, narrow=narrow)
+    for narrow, idle in ((True, 0), (False, 0), (False, 248), (False, 250)):
+        sizes = [3, 4, 1 + idle]
+        table, rows, n_pages = shared_tables(rng, sizes, 2, page, lambda i, g: 5, 1, 20, idle=range(8, 8 + idle))
+        c = Case(lava, rng, 8, 2, d, dtype, page, sizes, table, rows, n_pages, narrow=narrow)
         (out, lse), n = launches(c.run)
         c.check(out, lse)
-        assert n["paged_decode"] == 1 and n["shared_plan"] == n["shared_decode"] == n["shared_merge"] == (0 if narrow else 1)
-    (out, lse), n = launches(lambda: c.run(start=dev(np.arange(8, dtype=np.int32))))
+        assert n["shared_plan"] == n["shared_decode"] == n["shared_merge"] == (0 if narrow else 1)
+        assert n["paged_decode"] == (1 if narrow or 2 * (8 + idle) > 512 else 0)
+    (out, lse), n = launches(lambda: c.run(start=dev(np.arange(c.batch + 1, dtype=np.int32))))
     c.check(out, lse)
     assert n["paged_decode"] == 1 and n["shared_plan"] == 0
 
