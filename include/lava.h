@@ -756,7 +756,7 @@ size_t lava_beam_step_workspace_bytes(int32_t batch, int32_t beams, int64_t voca
  *                the `source` of a state that holds n_tables layers as sequences of their own
  * Sorted, the best first.  A place without a candidate gets parent -1, token -1, score -inf, done 1.  A beam with a NaN or +inf
  * among its logits, or with nothing but -inf, has no continuation.
- * beams, n_out <= 64, vocab < 2^31, batch <= 65535, n_tables <= 1024, batch * beams * ceil(vocab / 8192) < 2^31,
+ * beams, n_out <= 64, vocab < 2^31, batch <= 65535, n_tables <= 1024, batch * beams * ceil(vocab / 8192) < 2^24,
  * n_tables * batch * max(beams, n_out) < 2^31.  The same inputs give the same outputs bit for bit, and beams with the
  * same logits and scores the same candidates.
  */

@@ -13,7 +13,7 @@ bool good_workspace(const void* workspace, size_t bytes, size_t need) {
 int32_t check_beams(int32_t batch, int32_t beams, int64_t vocab, int32_t n_out) {
   if (batch < 1 || beams < 1 || vocab < 1 || n_out < 1) return LAVA_ERR_INVALID_ARG;
   if (batch > 65535 || beams > 64 || n_out > 64 || vocab >= (int64_t)1 << 31) return LAVA_ERR_SHAPE;
-  if ((int64_t)batch * beams * ((vocab + 8191) / 8192) >= (int64_t)1 << 31) return LAVA_ERR_SHAPE;
+  if ((int64_t)batch * beams * ((vocab + 8191) / 8192) >= (int64_t)1 << 24) return LAVA_ERR_SHAPE;   // a launch has fewer than 2^32 threads, 256 of them each
   return LAVA_OK;
 }
 

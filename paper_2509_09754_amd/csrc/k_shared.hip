@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_rows_kernel(const Shared
           if (k < S::kHalves && lane < 16) lds_write32(lds_addr(&s_pos[buffer][16 * k + lane]), __int_as_float(pos_next[x]));
         }
       }
-      if ((s + 1) * S::kStageRows > it.rows) {                 // uniform: rows behind the last one weigh nothing, whatever was there
+      if (it.rows - s * S::kStageRows < S::kStageRows) {                 // uniform: rows behind the last one weigh nothing, whatever was there
 #pragma unroll
         for (int x = 0; x < 4 * S::kTiles / kShWaves; ++x) {
           const int k = wave + kShWaves * x, hh = k % S::kHalves, left = it.rows - s * S::kStageRows - 16 * hh;
@@ -631,7 +631,7 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_rows_kernel(const Shared
             }
           }
         }
-        if (r0 + 32 > it.rows) {                               // uniform: some are behind the last row
+        if (it.rows - r0 < 32) {                               // uniform: some are behind the last row
 #pragma unroll
           for (int v = 0; v < 16; ++v) x[v] = r0 + 8 * (v / 4) + 4 * half + v % 4 < it.rows ? x[v] : -INFINITY;
         }

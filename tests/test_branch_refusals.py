@@ -35,7 +35,7 @@ def beam(**kw):
 @pytest.mark.parametrize("kw,want", [
     (dict(dtype=2), ARG), (dict(batch=0), ARG), (dict(beams=0), ARG), (dict(vocab=0), ARG), (dict(n_out=0), ARG), (dict(batch=65536), SHAPE),
     (dict(beams=65), SHAPE), (dict(n_out=65), SHAPE), (dict(vocab=1 << 31, stride=1 << 31), SHAPE),
-    (dict(batch=65535, beams=64, vocab=1 << 30, stride=1 << 30), SHAPE), (dict(logits=None), ARG), (dict(logits=FAKE + 1), ARG),
+    (dict(batch=65535, beams=64, vocab=1 << 30, stride=1 << 30), SHAPE), (dict(batch=32768, vocab=128 * 8192, stride=1 << 20), SHAPE), (dict(logits=None), ARG), (dict(logits=FAKE + 1), ARG),
     (dict(dtype=lava.LAVA_F32, logits=FAKE + 2), ARG), (dict(scores=None), ARG), (dict(parents=None), ARG), (dict(tokens=None), ARG),
     (dict(scores_out=None), ARG), (dict(pad=-1), ARG), (dict(pad=1000), ARG), (dict(stride=999), ARG), (dict(stride=-1), ARG), (dict(stride=1 << 40), SHAPE),
     (dict(n_out=3, scores_out=FAKE), ARG), (dict(n_out=3, done=FAKE, done_out=FAKE), ARG), (dict(sources=FAKE), ARG), (dict(n_tables=1), ARG),
@@ -49,6 +49,7 @@ def test_beam_step_lets_pass():
     """Odd addresses of 16-bit logits, one row of any stride, the buffers in place: refused for the missing workspace only."""
     assert beam(logits=FAKE + 2, ws=None) == SPACE
     assert beam(batch=1, beams=1, stride=0, n_out=64, ws=None) == SPACE
+    assert beam(batch=32768, beams=4, vocab=127 * 8192, stride=1 << 20, ws=None) == SPACE
     assert beam(scores_out=FAKE, done=FAKE, done_out=FAKE, ws=None) == SPACE
     size = lava.lava_beam_step_workspace_bytes
     assert size(0, 4, 10, 4) == size(1, 65, 10, 4) == size(1, 4, 0, 4) == size(1, 4, 10, 0) == size(65535, 64, 1 << 30, 1) == 0

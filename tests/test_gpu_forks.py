@@ -159,6 +159,44 @@ def test_histories(lava, batch, heads, page, blocks, dtype, d):
     assert refused < 6
 
 
+# tables that one workgroup marks (256 heads and 8192 entries at most), and the next larger ones
+@pytest.mark.parametrize("batch,heads,blocks", [(64, 4, 32), (257, 1, 4), (1, 1, 8192), (1, 1, 8193), (256, 1, 32), (127, 2, 33)])
+def test_small_changes_and_the_next_larger(lava, batch, heads, blocks):
+    print(f"edges {batch}x{heads}x{blocks}", flush=True)
+    rng, c = make(lava, batch, heads, 16, blocks, "bf16", 64, fill=0.4, spare=3 * batch * heads, seed=blocks)
+    for in_place in (True, False):
+        c.change(in_place, source=sources(rng, batch, 4))
+        counts, kept = random_lists(rng, c.now["rows"], 0.8)
+        c.change(in_place, counts=counts, kept=kept)
+
+
+def test_pool_beyond_four_gib(lava):
+    """Pages whose bytes lie beyond 2^32 of the pool's start: copied from, copied to."""
+    page, d, n_pages = 256, 128, 100_000
+    desc = lava.LayerDesc.make(2, 2, d, 1, "bf16")
+    k, v = (torch.empty(n_pages, page, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    pool = lava.PagePool(k, v, None, max_blocks=2)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    for x in (k, v):
+        x[[99_999, 70_001, 3, 80_000]] = torch.randn(4, page, d, device=DEV).to(torch.bfloat16)
+    free = torch.zeros(n_pages, dtype=torch.int32, device=DEV)
+    free[:4] = i32(99_998, 5, 99_997, 90_000)
+    state = lava.PageState(i32([[99_999, 70_001], [3, 80_000]], [[-1, -1], [-1, -1]]), i32([300, 511], [0, 0]), i32(600, 0), free, i32(4), page)
+    lava.lava_page_fork(desc, pool, state, i32(0, 0))
+    torch.cuda.synchronize()
+    assert state.block_table.tolist() == [[[99_999, 70_001], [3, 80_000]], [[99_999, 90_000], [3, 99_997]]] and int(state.n_free[0]) == 2
+    for x in (k, v):
+        assert torch.equal(x[90_000, :44], x[70_001, :44]) and torch.equal(x[99_997, :255], x[80_000, :255])
+    kept = torch.cat([torch.arange(1, 300, 2), torch.arange(511)]).to(DEV, torch.int32)[None].repeat(2, 1).contiguous()
+    lava.lava_page_compact(desc, pool, state, i32([150, 511], [150, 511]), kept, evict=i32(0, 1))
+    torch.cuda.synchronize()
+    assert state.block_table[1].tolist() == [[5, 90_000], [3, 99_997]] and state.head_rows.tolist() == [[300, 511], [150, 511]]
+    for x in (k, v):
+        old = torch.cat([x[99_999], x[70_001]])
+        assert torch.equal(x[5, :150], old[1:300:2])
+    assert int(state.n_free[0]) == 2 and state.free_pages[:2].tolist() == [99_998, 90_000]
+
+
 @pytest.mark.parametrize("in_place", [True, False])
 def test_refused_on_the_device(lava, in_place):
     """Nothing changes, the reason is in the error word; a call after it goes on."""

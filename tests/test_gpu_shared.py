@@ -314,6 +314,41 @@ def test_without_lse_and_replayed(lava):
         assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(eager[0], want)
 
 
+def test_pool_beyond_four_gib(lava):
+    """Common and own pages whose bytes lie beyond 2^32 of the pool's start."""
+    page, d, H, Hkv, n_pages = 256, 128, 8, 2, 100_000
+    desc = lava.LayerDesc.make(H, Hkv, d, 1, "bf16")
+    rng = np.random.default_rng(21)
+    table, rows, few = shared_tables(rng, [3, 2], Hkv, page, lambda i, g: 3, 1, 300)
+    high = n_pages - 1 - 37 * np.arange(few)
+    k, v = (torch.empty(n_pages, page, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    c = Case(lava, rng, H, Hkv, d, "bf16", page, [3, 2], table, rows, few)
+    k[dev(high)], v[dev(high)] = c.k, c.v
+    wide = dev(np.where(c.table.cpu().numpy() >= 0, high[np.maximum(c.table.cpu().numpy(), 0)], -1).astype(np.int32))
+    pool = lava.PagePool(k, v, None, max_blocks=wide.shape[2])
+    out, lse = lava.lava_shared_decode(desc, c.q, pool, wide, c.rows, c.start)
+    torch.cuda.synchronize()
+    c.check(out, lse)
+
+
+def test_first_call_of_a_kernel_inside_a_capture(lava):
+    """A step whose kernels are first launched while they are recorded."""
+    rng = np.random.default_rng(22)
+    table, rows, n_pages = shared_tables(rng, [5, 3], 1, 128, lambda i, g: 2, 1, 300)
+    c = Case(lava, rng, 3, 1, 128, "f32", 128, [5, 3], table, rows, n_pages, softcap=9.0)
+    ws = torch.full((lava.lava_shared_decode_workspace_bytes(c.desc, c.batch, c.table.shape[2]),), 0xFF, dtype=torch.uint8, device=DEV)
+    out, lse = torch.empty(8, 3, 128, device=DEV), torch.empty(8, 3, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        lava.lava_shared_decode(c.desc, c.q, c.pool, c.table, c.rows, c.start, c.options, out=out, lse=lse, workspace=ws)
+    for _ in range(3):
+        out.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(out, lse)
+
+
 def test_two_calls_at_once(lava):
     rng = np.random.default_rng(13)
     cases = []
