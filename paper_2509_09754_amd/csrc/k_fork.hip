@@ -6,7 +6,7 @@
 // behind them go to fresh pages, whose rows are copied.  A page is free afterwards if no new table names it.
 //
 // Who holds a page is found out by marking, two words a page: a new table's leading blocks store `alive`, an old table's blocks that
-// do not stay take the minimum with 1 + the head's number in `first`.  A page that is not alive was first named by head
+// do not stay in their places take the minimum with 1 + the head's number in `first`.  A page that is not alive was first named by head
 // first - 1, which gives it back, so that the stack's order does not depend on the order of the marks.
 //
 // Each step needs all of what the one before found: clear the marks; mark, and sum the fresh pages over the heads (a
@@ -31,7 +31,7 @@ constexpr unsigned int kNoHolder = 0xffffffffu;
 
 struct ChangeHeader {
   int error;                                  // LAVA_PAGES_* bits
-  int n_free, fresh, back;                    // free pages before, pages taken, pages given back
+  int n_free, fresh;                          // free pages before, pages taken
 };
 
 struct __attribute__((aligned(16))) HeadPlan {
@@ -77,9 +77,8 @@ ChangeLayout change_layout(int batch, int n_kv_heads, int max_blocks, long long 
 
 __device__ __forceinline__ bool is_page(const PageChangeArgs& p, int page) { return page >= 0 && page < p.n_pages; }
 
-// Rows that head h held, 0 where the count is out of range.
-__device__ __forceinline__ int rows_before(const PageChangeArgs& p, int h) {
-  const int rows = p.st.head_rows[h];
+// Rows of a head with that count, 0 where it is out of range.
+__device__ __forceinline__ int rows_of(const PageChangeArgs& p, int rows) {
   return rows < 0 || rows > (long long)p.max_blocks << p.page_shift ? 0 : rows;
 }
 
@@ -90,8 +89,8 @@ __device__ __forceinline__ int blocks_of(const PageChangeArgs& p, int rows) {
 // Does sequence b go on with the last pages of sequence s, which it is made of?  A wavefront's question.
 __device__ __forceinline__ bool is_keeper(const PageChangeArgs& p, int b, int s) {
   if (p.source == nullptr || s == b) return true;
-  if (s < 0 || p.source[s] == s) return false;
-  const int lane = threadIdx.x & 63;
+  if (s < 0) return false;
+  const int lane = threadIdx.x & 63, of_s = p.source[s];
   for (int c0 = 0; c0 < b; c0 += 512) {
     bool same = false;
 #pragma unroll
@@ -101,7 +100,7 @@ __device__ __forceinline__ bool is_keeper(const PageChangeArgs& p, int b, int s)
     }
     if (__ballot(same) != 0ull) return false;
   }
-  return true;
+  return of_s != s;
 }
 
 // The first t in [0, n) with list[t] != t, n if there is none; the list ascends.
@@ -127,14 +126,21 @@ __device__ __forceinline__ int leading_same(const int* list, int n) {
 constexpr int kLooks = 4;                     // look-ups of a thread at a time
 
 // What head h keeps, and its marks; returns the fresh pages it needs.  A wavefront's work; error bits are or-ed to `error`.
+// The kernel takes as long as its chain of look-ups, so the first blocks of both tables are loaded before it is known how
+// many count, and who keeps a last page is found out while the counts are on their way.
 __device__ __forceinline__ int mark_head(const ChangeArgs& a, int h, int& error) {
   const PageChangeArgs& p = a.p;
   const int lane = threadIdx.x & 63, G = p.heads, P = 1 << p.page_shift, b = h / G, g = h - b * G;
-  const int rows = rows_before(p, h), nb_old = blocks_of(p, rows);
-  if (p.st.head_rows[h] != rows) error |= LAVA_PAGES_INVALID;
+  const int* mine = p.st.block_table + (long long)h * p.max_blocks;
+  const int mine_first = mine[lane < p.max_blocks ? lane : 0], held = p.st.head_rows[h];
   int s = p.source != nullptr ? p.source[b] : b;
   if (s < -1 || s >= p.batch) error |= LAVA_PAGES_INVALID, s = -1;
-  const int old = s >= 0 ? rows_before(p, s * G + g) : 0;
+  const int* from = p.st.block_table + ((long long)(s >= 0 ? s : b) * G + g) * p.max_blocks;
+  const int from_first = from[lane < p.max_blocks ? lane : 0], held_from = p.st.head_rows[(s >= 0 ? s : b) * G + g];
+  const int from_pos = p.st.seq_pos[s >= 0 ? s : b];
+  const bool keeper = is_keeper(p, b, s);
+  const int rows = rows_of(p, held), nb_old = blocks_of(p, rows), old = s >= 0 ? rows_of(p, held_from) : 0;
+  if (held != rows) error |= LAVA_PAGES_INVALID;
   int n = old, same = old;
   long long begin = -1;
   if (p.head_counts != nullptr && (p.evict == nullptr || p.evict[b] != 0)) {
@@ -160,34 +166,38 @@ __device__ __forceinline__ int mark_head(const ChangeArgs& a, int h, int& error)
     }
   }
   int stay = same >> p.page_shift;
-  if ((n & (P - 1)) != 0 && same >= n && (old & (P - 1)) != 0 && n >> p.page_shift == old >> p.page_shift && is_keeper(p, b, s)) ++stay;
+  if ((n & (P - 1)) != 0 && same >= n && (old & (P - 1)) != 0 && n >> p.page_shift == old >> p.page_shift && keeper) ++stay;
   if (s >= 0) {
-    const int* from = p.st.block_table + ((long long)s * G + g) * p.max_blocks;
     for (int j0 = lane; j0 < stay; j0 += 64 * kLooks) {
       int page[kLooks];
 #pragma unroll
-      for (int u = 0; u < kLooks; ++u) page[u] = j0 + 64 * u < stay ? from[j0 + 64 * u] : 0;
+      for (int u = 0; u < kLooks; ++u) page[u] = j0 + 64 * u < 64 ? from_first : j0 + 64 * u < stay ? from[j0 + 64 * u] : 0;
 #pragma unroll
       for (int u = 0; u < kLooks; ++u) {
+        if (j0 + 64 * u >= stay) continue;
         if (!is_page(p, page[u])) error |= LAVA_PAGES_INVALID;
-        else if (j0 + 64 * u < stay) a.alive[page[u]] = 1u;
+        else a.alive[page[u]] = 1u;
       }
     }
   }
-  const int* mine = p.st.block_table + (long long)h * p.max_blocks;
   const int kept = s == b ? stay : 0;                          // leading blocks that this head marked itself
-  for (int j0 = (a.old_table != nullptr ? 0 : kept) + lane; j0 < nb_old; j0 += 64 * kLooks) {
-    int page[kLooks];
+  const int beside = s >= 0 ? stay : 0;                        // where it may have: the two tables name the same pages, as a prompt's beams do
+  for (int j0 = lane; j0 < nb_old; j0 += 64 * kLooks) {
+    int page[kLooks], other[kLooks];
 #pragma unroll
-    for (int u = 0; u < kLooks; ++u) page[u] = j0 + 64 * u < nb_old ? mine[j0 + 64 * u] : 0;
+    for (int u = 0; u < kLooks; ++u) {
+      const int j = j0 + 64 * u;
+      page[u] = j < 64 ? mine_first : j < nb_old && (j >= kept || a.old_table != nullptr) ? mine[j] : 0;
+      other[u] = j >= beside ? -1 : j < 64 ? from_first : j < nb_old ? from[j] : -1;
+    }
 #pragma unroll
     for (int u = 0; u < kLooks; ++u) {
       const int j = j0 + 64 * u;
       if (j >= nb_old) continue;
       if (a.old_table != nullptr) a.old_table[(long long)h * p.max_blocks + j] = page[u];
       if (j < kept) continue;
-      if (is_page(p, page[u])) __hip_atomic_fetch_min(&a.first[page[u]], 1u + (unsigned int)h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      else error |= LAVA_PAGES_INVALID;
+      if (!is_page(p, page[u])) error |= LAVA_PAGES_INVALID;
+      else if (page[u] != other[u]) __hip_atomic_fetch_min(&a.first[page[u]], 1u + (unsigned int)h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   }
   if (lane == 0) {
@@ -198,7 +208,7 @@ __device__ __forceinline__ int mark_head(const ChangeArgs& a, int h, int& error)
     x.from = s >= 0 ? s * G + g : -1;
     x.old = old;
     x.list = begin;
-    if (g == 0) a.seq_pos[b] = s >= 0 ? p.st.seq_pos[s] : 0;
+    if (g == 0) a.seq_pos[b] = s >= 0 ? from_pos : 0;
   }
   return blocks_of(p, n) - stay;
 }
@@ -206,13 +216,16 @@ __device__ __forceinline__ int mark_head(const ChangeArgs& a, int h, int& error)
 // Pages that head h gives back.  `use(page, how many before it)` for each, in the order of the blocks; a wavefront's work.
 template <typename F>
 __device__ __forceinline__ int for_each_gone(const ChangeArgs& a, int h, const int* table, F use) {
-  const int lane = threadIdx.x & 63, nb_old = blocks_of(a.p, a.old_rows[h]);
+  const int lane = threadIdx.x & 63, first_page = table[lane < a.p.max_blocks ? lane : 0], nb_old = blocks_of(a.p, a.old_rows[h]);
   int n = 0;
-  for (int j0 = a.plan[h].from == h ? a.plan[h].stay : 0; j0 < nb_old; j0 += 64 * kLooks) {
+  for (int j0 = a.plan[h].from == h ? a.plan[h].stay & ~63 : 0; j0 < nb_old; j0 += 64 * kLooks) {   // (what stays is alive)
     int page[kLooks];
     unsigned int first[kLooks], alive[kLooks];
 #pragma unroll
-    for (int u = 0; u < kLooks; ++u) page[u] = j0 + 64 * u + lane < nb_old ? table[j0 + 64 * u + lane] : -1;
+    for (int u = 0; u < kLooks; ++u) {
+      const int j = j0 + 64 * u + lane;
+      page[u] = j >= nb_old ? -1 : j0 + 64 * u == 0 ? first_page : table[j];
+    }
 #pragma unroll
     for (int u = 0; u < kLooks; ++u) {
       const bool there = is_page(a.p, page[u]);
@@ -245,33 +258,6 @@ __device__ __forceinline__ int2 sums_of_group(int* s_wave, int mine) {
   return r;
 }
 
-// Sums of the workgroups' totals in front of workgroup `group` (x) and of all (y), in every thread of a workgroup.
-template <int THREADS>
-__device__ __forceinline__ int2 sum_totals(const int* totals, int groups, int group, int* s_sum) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int before = 0, all = 0;
-  for (int i = threadIdx.x; i < groups; i += THREADS) {
-    const int x = totals[i];
-    before += i < group ? x : 0;
-    all += x;
-  }
-  before = (int)lane_value(wave_incl((unsigned int)before), 63);
-  all = (int)lane_value(wave_incl((unsigned int)all), 63);
-  if (lane == 0) {
-    s_sum[2 * wave] = before;
-    s_sum[2 * wave + 1] = all;
-  }
-  __syncthreads();
-  int2 r = make_int2(0, 0);
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) {
-    r.x += s_sum[2 * w];
-    r.y += s_sum[2 * w + 1];
-  }
-  __syncthreads();
-  return r;
-}
-
 // The fresh pages, off the stack: every `step`th from `from` on.  Returns error bits.
 __device__ __forceinline__ int take_pages(const ChangeArgs& a, int n_free, int fresh, int from, int step) {
   if (n_free < 0 || n_free > a.p.n_pages || fresh > n_free) return 0;    // found out again when tables are written
@@ -286,10 +272,7 @@ __device__ __forceinline__ int take_pages(const ChangeArgs& a, int n_free, int f
 
 // ---------------------------------------------------------------- 1: clear
 __global__ void __launch_bounds__(256) change_begin_kernel(const ChangeArgs a) {
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    a.head->error = 0;
-    a.head->back = 0;
-  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.head->error = 0;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < a.p.n_pages; i += (long long)gridDim.x * 256) {
     a.alive[i] = 0u;
     a.first[i] = kNoHolder;
@@ -304,48 +287,71 @@ __global__ void __launch_bounds__(kChangeThreads) change_mark_kernel(const Chang
   int error = 0, sum = 0;
   for (int h = h0; h < h1; ++h) {
     const int fresh = mark_head(a, h, error);
-    if (lane == 0) a.plan[h].fresh_at = sum;
+    if (lane == 0 && a.per > 1) a.plan[h].fresh_at = sum;
     sum += fresh;
   }
   if (error != 0) atomicOr(&a.head->error, error);
   const int2 all = sums_of_group(s_wave, sum);
   if (lane == 0)
-    for (int h = h0; h < h1; ++h) a.plan[h].fresh_at += all.x;
+    for (int h = h0; h < h1; ++h) a.plan[h].fresh_at = all.x + (a.per > 1 ? a.plan[h].fresh_at : 0);
   if (threadIdx.x == 0) a.fresh_total[blockIdx.x] = all.y;
 }
 
 // ---------------------------------------------------------------- 3: sums of what goes back; the fresh pages
 __global__ void __launch_bounds__(kChangeThreads) change_count_kernel(const ChangeArgs a) {
-  __shared__ int s_wave[kChangeWaves], s_sum[2 * kChangeWaves];
+  __shared__ int s_wave[kChangeWaves], s_before[kChangeWaves], s_fresh[kChangeWaves];
   const PageChangeArgs& p = a.p;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int h0 = (blockIdx.x * kChangeWaves + wave) * a.per, h1 = h0 + a.per < a.heads ? h0 + a.per : a.heads;
-  const int2 fresh = sum_totals<kChangeThreads>(a.fresh_total, gridDim.x, blockIdx.x, s_sum);
+  // fresh pages of the workgroups before this one, of all; they are on their way while the heads' pages are looked up
+  constexpr int kEach = kMostGroups / kChangeThreads;
+  int fresh_of[kEach], before = 0, fresh = 0, sum = 0;
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const unsigned int i = threadIdx.x + u * kChangeThreads;
+    fresh_of[u] = i < gridDim.x ? a.fresh_total[i] : 0;
+  }
   const int n_free = p.st.n_free[0];
-  const bool enough = n_free >= 0 && n_free <= p.n_pages && fresh.y <= n_free;
-  int sum = 0;
   for (int h = h0; h < h1; ++h) {
     const int n = for_each_gone(a, h, p.st.block_table + (long long)h * p.max_blocks, [](int, int) {});
-    const int at = a.plan[h].fresh_at + fresh.x, need = blocks_of(p, a.plan[h].n) - a.plan[h].stay;
-    for (int j = lane; enough && j < need; j += 64) a.owner[at + j] = h;
-    if (lane == 0) {
-      a.plan[h].back_at = sum;
-      a.plan[h].fresh_at = at;
-    }
+    if (lane == 0 && a.per > 1) a.plan[h].back_at = sum;
     sum += n;
+  }
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    before += threadIdx.x + u * kChangeThreads < blockIdx.x ? fresh_of[u] : 0;
+    fresh += fresh_of[u];
+  }
+  before = (int)lane_value(wave_incl((unsigned int)before), 63);
+  fresh = (int)lane_value(wave_incl((unsigned int)fresh), 63);
+  if (lane == 0) {
+    s_before[wave] = before;
+    s_fresh[wave] = fresh;
+  }
+  __syncthreads();
+  before = fresh = 0;
+#pragma unroll
+  for (int w = 0; w < kChangeWaves; ++w) {
+    before += s_before[w];
+    fresh += s_fresh[w];
+  }
+  const bool enough = n_free >= 0 && n_free <= p.n_pages && fresh <= n_free;
+  for (int h = h0; h < h1; ++h) {
+    const int at = a.plan[h].fresh_at + before, need = blocks_of(p, a.plan[h].n) - a.plan[h].stay;
+    for (int j = lane; enough && j < need; j += 64) a.owner[at + j] = h;
+    if (lane == 0) a.plan[h].fresh_at = at;
   }
   const int2 all = sums_of_group(s_wave, sum);
   if (lane == 0)
-    for (int h = h0; h < h1; ++h) a.plan[h].back_at += all.x;
+    for (int h = h0; h < h1; ++h) a.plan[h].back_at = all.x + (a.per > 1 ? a.plan[h].back_at : 0);
   if (threadIdx.x == 0) {
     a.back_total[blockIdx.x] = all.y;
-    if (all.y != 0) atomicAdd(&a.head->back, all.y);
     if (blockIdx.x == 0) {
       a.head->n_free = n_free;
-      a.head->fresh = fresh.y;
+      a.head->fresh = fresh;
     }
   }
-  const int error = take_pages(a, n_free, fresh.y, blockIdx.x * kChangeThreads + threadIdx.x, gridDim.x * kChangeThreads);
+  const int error = take_pages(a, n_free, fresh, blockIdx.x * kChangeThreads + threadIdx.x, gridDim.x * kChangeThreads);
   if (error != 0) atomicOr(&a.head->error, error);
 }
 
@@ -373,8 +379,8 @@ __global__ void __launch_bounds__(kOneThreads) change_one_kernel(const ChangeArg
     entry_page[u] = entry_head[u] >= 0 ? p.st.block_table[e] : -1;   // behind a head's last block whatever is there: not used
   }
   if (is_head) {
-    const int rows = rows_before(p, h);
-    if (p.st.head_rows[h] != rows) error = LAVA_PAGES_INVALID;
+    const int held = p.st.head_rows[h], rows = rows_of(p, held);
+    if (held != rows) error = LAVA_PAGES_INVALID;
     s_rows[h] = rows;
     s_count[h] = p.head_counts != nullptr ? p.head_counts[h] : 0;
     s_back[h] = 0;
@@ -449,11 +455,12 @@ __global__ void __launch_bounds__(kOneThreads) change_one_kernel(const ChangeArg
     const int x = entry_head[u], j = entry_block[u], page = entry_page[u];
     if (x < 0) continue;
     const int from = s_from[x], stay = s_stay[x];
+    int keeps = -1;
     if (from >= 0 && j < stay) {
-      const int keeps = from == x ? page : p.st.block_table[from * W + j];
+      keeps = from == x ? page : p.st.block_table[from * W + j];
       if (is_page(p, keeps)) st_dev(&a.alive[keeps], 1u);
     }
-    if (is_page(p, page) && (from != x || j >= stay))
+    if (is_page(p, page) && keeps != page)
       __hip_atomic_fetch_min(&a.first[page], 1u + (unsigned int)x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   drain_vmem();
@@ -497,13 +504,14 @@ __global__ void __launch_bounds__(kOneThreads) change_one_kernel(const ChangeArg
   if (error != 0) atomicOr(&s_error, error);
   __syncthreads();
   if (threadIdx.x == 0) {
-    *a.head = ChangeHeader{s_error, n_free, fresh, s_total[1]};
+    *a.head = ChangeHeader{s_error, n_free, fresh};
     a.back_total[0] = s_total[1];
   }
 }
 
 // ---------------------------------------------------------------- 4: tables, counts, stack; rows
-constexpr int kApplyThreads = 256, kApplyWaves = kApplyThreads / 64, kRowsInFlight = 4, kMostApply = 4096;
+constexpr int kApplyThreads = 256, kApplyWaves = kApplyThreads / 64, kMostApply = 4096;
+template <int ROWS>                           // rows of a thread at a time
 __global__ void __launch_bounds__(kApplyThreads) change_apply_kernel(const ChangeArgs a, int groups) {
   __shared__ int s_before[kMostGroups], s_wave[kApplyWaves];   // pages given back by the groups of heads before each
   const PageChangeArgs& p = a.p;
@@ -511,16 +519,43 @@ __global__ void __launch_bounds__(kApplyThreads) change_apply_kernel(const Chang
   const int first = blockIdx.x * kApplyThreads + threadIdx.x, step = gridDim.x * kApplyThreads;
   const int wave0 = blockIdx.x * kApplyWaves + wave, waves = gridDim.x * kApplyWaves;
   const ChangeHeader head = *a.head;
+  int back = 0;                                                // pages given back
+  {
+    constexpr int kEach = kMostGroups / kApplyThreads;
+    int mine[kEach], sum = 0;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int q = (int)threadIdx.x * kEach + u;
+      mine[u] = q < groups ? a.back_total[q] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) sum += mine[u];
+    const int incl = (int)wave_incl((unsigned int)sum);
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    int at = incl - sum;
+#pragma unroll
+    for (int w = 0; w < kApplyWaves; ++w) {
+      at += w < wave ? s_wave[w] : 0;
+      back += s_wave[w];
+    }
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      s_before[threadIdx.x * kEach + u] = at;
+      at += mine[u];
+    }
+    __syncthreads();
+  }
   const int n_free = head.n_free;
   int error = head.error;
   if (n_free < 0 || n_free > p.n_pages) error |= LAVA_PAGES_INVALID;
   if (error == 0 && head.fresh > n_free) error = LAVA_PAGES_EXHAUSTED;
-  if (error == 0 && (long long)n_free - head.fresh + head.back > p.n_pages) error = LAVA_PAGES_INVALID;
+  if (error == 0 && (long long)n_free - head.fresh + back > p.n_pages) error = LAVA_PAGES_INVALID;
   const int left = error != 0 ? (n_free < 0 ? 0 : n_free > p.n_pages ? (int)p.n_pages : n_free) : n_free - head.fresh;
   const bool table_apart = p.table_out != p.st.block_table;
   const int* tables = table_apart ? p.st.block_table : a.old_table;
   if (first == 0) {
-    p.st.n_free_out[0] = error != 0 ? n_free : left + head.back;
+    p.st.n_free_out[0] = error != 0 ? n_free : left + back;
     if (error != 0 && p.st.error != nullptr) atomicOr(p.st.error, error);
   }
   if (p.free_out != p.st.free_pages)
@@ -537,24 +572,24 @@ __global__ void __launch_bounds__(kApplyThreads) change_apply_kernel(const Chang
     }
     return;
   }
-  // rows: those of the fresh pages in one line, `per_row` threads a row, kRowsInFlight rows of a thread at a time
+  // rows: those of the fresh pages in one line, `per_row` threads a row, ROWS rows of a thread at a time
   const int per_row = p.row_bytes >> 4, rows_a_pass = kApplyThreads / per_row, i = threadIdx.x / per_row, x = threadIdx.x - i * per_row;
   u32x4 *k_out = reinterpret_cast<u32x4*>(p.k), *v_out = reinterpret_cast<u32x4*>(p.v);
   const u32x4 *k_in = k_out, *v_in = v_out;
-  const long long pass = (long long)rows_a_pass * kRowsInFlight, total = (long long)head.fresh << p.page_shift;
+  const long long pass = (long long)rows_a_pass * ROWS, total = (long long)head.fresh << p.page_shift;
   for (long long t0 = blockIdx.x * pass; t0 < total; t0 += gridDim.x * pass) {
-    long long src[kRowsInFlight], dst[kRowsInFlight];
-    bool on[kRowsInFlight];
-    int owner[kRowsInFlight], page[kRowsInFlight];
+    long long src[ROWS], dst[ROWS];
+    bool on[ROWS];
+    int owner[ROWS], page[ROWS];
 #pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) {
+    for (int u = 0; u < ROWS; ++u) {
       const long long at = t0 + u * rows_a_pass + i;
       const int k = (int)((at < total ? at : t0) >> p.page_shift);
       owner[u] = a.owner[k];
       page[u] = a.taken[k];
     }
 #pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) {
+    for (int u = 0; u < ROWS; ++u) {
       const long long at = t0 + u * rows_a_pass + i;
       const HeadPlan h = a.plan[owner[u]];
       const int k = (int)((at < total ? at : t0) >> p.page_shift), in_page = (int)at & (P - 1);
@@ -566,16 +601,16 @@ __global__ void __launch_bounds__(kApplyThreads) change_apply_kernel(const Chang
       src[u] = on[u] ? ((long long)tables[(long long)h.from * p.max_blocks + (r >> p.page_shift)] << p.page_shift) + (r & (P - 1)) : 0;
       dst[u] = ((long long)page[u] << p.page_shift) + in_page;
     }
-    u32x4 kx[kRowsInFlight], vx[kRowsInFlight];
-    int px[kRowsInFlight];
+    u32x4 kx[ROWS], vx[ROWS];
+    int px[ROWS];
 #pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) {                  // a row that is not there: row 0 of the pool, which is
+    for (int u = 0; u < ROWS; ++u) {                  // a row that is not there: row 0 of the pool, which is
       kx[u] = k_in[src[u] * per_row + x];
       vx[u] = v_in[src[u] * per_row + x];
       px[u] = p.pos != nullptr && x == 0 ? p.pos[src[u]] : 0;
     }
 #pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) {
+    for (int u = 0; u < ROWS; ++u) {
       if (on[u]) {
         k_out[dst[u] * per_row + x] = kx[u];
         v_out[dst[u] * per_row + x] = vx[u];
@@ -595,29 +630,8 @@ __global__ void __launch_bounds__(kApplyThreads) change_apply_kernel(const Chang
       if (h % G == 0) p.st.seq_pos_out[h / G] = a.seq_pos[h / G];
     }
   }
-  if (head.back == 0) return;                                  // uniform: the same for all
+  if (back == 0) return;                                       // uniform: the same for all
   // pages given back
-  {
-    constexpr int kEach = kMostGroups / kApplyThreads;
-    int mine[kEach], sum = 0;
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-      const int q = (int)threadIdx.x * kEach + u;
-      mine[u] = q < groups ? a.back_total[q] : 0;
-      sum += mine[u];
-    }
-    const int incl = (int)wave_incl((unsigned int)sum);
-    if (lane == 63) s_wave[wave] = incl;
-    __syncthreads();
-    int at = incl - sum;
-    for (int w = 0; w < wave; ++w) at += s_wave[w];
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-      s_before[threadIdx.x * kEach + u] = at;
-      at += mine[u];
-    }
-    __syncthreads();
-  }
   for (int h = wave0; h < a.heads; h += waves) {
     int* to = p.free_out + left + s_before[a.one != 0 ? 0 : h / (kChangeWaves * a.per)] + a.plan[h].back_at;
     for_each_gone(a, h, tables + (long long)h * p.max_blocks, [to](int page, int n) { to[n] = page; });
@@ -663,14 +677,18 @@ int32_t launch_page_change(const PageChangeArgs& p, void* ws, hipStream_t s) {
   }
   int32_t st = launch_status();
   if (st != LAVA_OK) return st;
-  // as many workgroups as there can be work for, up to two rounds of what the device holds: of a fork a head copies less than a page
-  const long long pass = (long long)kApplyThreads / (p.row_bytes >> 4) * kRowsInFlight;
+  // as many workgroups as there can be work for, up to two rounds of what the device holds: of a fork a head copies less than a page.
+  // Rows from anywhere, and few rows, are copied two at a time (32 caches evicted 21.3 -> 20.0 us, eight beams' pages 9.0 -> 8.1), long
+  // runs four (64 samples of 8 prompts 17.3 -> 16.0).
   const long long rows = (long long)a.heads * ((p.head_counts != nullptr ? p.max_blocks : 1LL) << p.page_shift);
+  const bool four = p.head_counts == nullptr && rows > 8192;
+  const long long pass = (long long)kApplyThreads / (p.row_bytes >> 4) * (four ? 4 : 2);
   long long wgs = (rows + pass - 1) / pass;
   if (wgs < (a.heads + kApplyWaves - 1) / kApplyWaves) wgs = (a.heads + kApplyWaves - 1) / kApplyWaves;
   if (wgs > kMostApply) wgs = kMostApply;
   ProfScope ps(KID_PAGE_APPLY, s);
-  hipLaunchKernelGGL(change_apply_kernel, dim3((unsigned)wgs), dim3(kApplyThreads), 0, s, a, groups);
+  if (four) hipLaunchKernelGGL(change_apply_kernel<4>, dim3((unsigned)wgs), dim3(kApplyThreads), 0, s, a, groups);
+  else hipLaunchKernelGGL(change_apply_kernel<2>, dim3((unsigned)wgs), dim3(kApplyThreads), 0, s, a, groups);
   return launch_status();
 }
 
