@@ -15,7 +15,10 @@
 // reads of buffers that it also writes was set aside before.  The first three are one launch of one workgroup where tables are few
 // and short (kOneEntries), which clears only the words of pages that are named.
 //
-// Bound by the chain of launches for a beam step (one layer of eight beams), by HBM for many rows.
+// Bound by the chain of launches and of look-ups in each for a beam step (one layer of eight beams of 4096 tokens: 7.3 us by one workgroup, 5.8 of
+// rows; 32 layers of 16 beams: 2.9, 6.0, 5.0 and 16 for 47 MB), by HBM for many rows (48 caches evicted in 32 bits, 254 MB:
+// rows 60 us, 4.3 TB/s, marks 21).  An entry that names the page it named before is no candidate for going back: with
+// atomics for the pages that all beams share the second launch of the 32 layers took 8.5 us.
 #include "common.h"
 #include "decode_parts.h"
 #include "tile_ring.h"
@@ -356,6 +359,7 @@ __global__ void __launch_bounds__(kChangeThreads) change_count_kernel(const Chan
 }
 
 // ---------------------------------------------------------------- 1 to 3 by one workgroup
+// One launch instead of three: eight beams of one layer 7.3 us instead of 14, a wavefront a head in series 25.
 // Every thread has up to kOnePer entries of the tables, whose look-ups are independent of each other.  A list's blocks stay as long as
 // their last rows are where they were, since it ascends.
 constexpr int kOneThreads = 1024, kOneHeads = 256, kOnePer = 8, kOneEntries = kOnePer * kOneThreads;

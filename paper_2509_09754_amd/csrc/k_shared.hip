@@ -75,6 +75,7 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
   const PagedDecodeArgs& p = a.p;
   const int group = blockIdx.x / p.H_kv, g = blockIdx.x - group * p.H_kv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int seqs = kShRows / p.G, P = 1 << p.page_shift;
+  const int from = a.group_start[group], to = a.group_start[group + 1];   // on their way while the others are looked at
   if (threadIdx.x == 0) s_bad = 0;
   __syncthreads();
   int before = 0, all = 0;                                     // blocks of sequences of the groups before, of all
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
     a.n_items[1] = 0;
   }
   // groups that are none: every sequence by itself
-  const int b0 = bad ? group : a.group_start[group], b1 = bad ? p.batch : a.group_start[group + 1], step = bad ? a.n_groups : 1;
+  const int b0 = bad ? group : from, b1 = bad ? p.batch : to, step = bad ? a.n_groups : 1;
   int common = 0, lead = 0x7fffffff;
   if (!bad && b1 - b0 > 1) {                                   // uniform
     auto held = [&](int b) { return p.head_rows[(long long)b * p.H_kv + g]; };
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
     }
     if (some > 1) {
       // a wavefront 64 blocks: the first one in which a sequence differs, kCompared of them at a time
-      constexpr int kCompared = 16;
+      constexpr int kCompared = 32;
       const int* first = table(lead);
       common = least;
       for (int j0 = 64 * wave; j0 < least; j0 += 64 * kPlanShWaves) {
@@ -210,9 +211,9 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
         a.own_marked[h[i]] = 0;
         a.item_of[h[i]] = skip[i] > 0 ? item0 + (b - b0) / seqs : -1;
       }
-      int* to = a.rest_table + h[i] * p.max_blocks;
-      if (lane < left[i]) to[lane] = y[i];
-      for (int j = 64 + lane; j < left[i]; j += 64) to[j] = p.block_table[h[i] * p.max_blocks + skip[i] + j];
+      int* rest = a.rest_table + h[i] * p.max_blocks;
+      if (lane < left[i]) rest[lane] = y[i];
+      for (int j = 64 + lane; j < left[i]; j += 64) rest[j] = p.block_table[h[i] * p.max_blocks + skip[i] + j];
     }
   }
 }
