@@ -12,9 +12,8 @@
 // is the least (coefficients by Remez's exchange).  15 64-bit instructions a token, at the rate of 32-bit ones on this
 // device (2.4 ns a wavefront); with the polynomial of Taylor's series to degree 10, its exponent by ldexp and bounds from 64 readlanes a
 // wavefront 64 groups of 8 beams over 131072 tokens took 85 us, now 61: rows 57 (107 MB of bf16 logits, 1.9 TB/s), pick 7.  Bound by the issue of
-// instructions: more wavefronts (64
-// registers) or the chains of two or four tokens side by side take as long or longer.  One group of 4 beams over 32000 tokens: 11.4 us, two
-// launches of dependent look-ups.
+// instructions: more wavefronts (64 registers) or the chains of two or four tokens side by side take as long or longer.  One group of 4
+// beams over 32000 tokens: 11.4 us, two launches of dependent look-ups.
 #include "common.h"
 #include "decode_parts.h"
 #include "tile_ring.h"
