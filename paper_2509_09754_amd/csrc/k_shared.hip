@@ -446,17 +446,16 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_rows_kernel(const Shared
     const int s0 = part * unit_share, s_all = stages_in(it.rows), s1 = s0 + unit_share < s_all ? s0 + unit_share : s_all;
     const int* table = p.block_table + ((long long)it.lead * p.H_kv + it.head) * p.max_blocks + it.skip;
 
-    // ---------------- the queries of this lane's column
+    // ---------------- the queries of this lane's column: a sequence that holds nothing in this head has none, whatever stands there
     const int qr = rt * 32 + col;
-    const bool real = qr < q_rows;
-    const int q_seq = it.first_seq + (real ? qr / p.G : 0), q_head = it.head * p.G + (real ? qr % p.G : 0);
+    const bool there = qr < q_rows;
+    const int q_seq = it.first_seq + (there ? qr / p.G : 0), q_head = it.head * p.G + (there ? qr % p.G : 0);
+    const bool real = there && p.head_rows[(long long)q_seq * p.H_kv + it.head] != 0;
     u32x4 qf[T::kSteps];
 #pragma unroll
-    for (int j = 0; j < T::kSteps; ++j) {
-      u32x4 x = u32x4{0u, 0u, 0u, 0u};
-      if (real) x = reinterpret_cast<const u32x4*>(p.q)[((long long)q_seq * p.H + q_head) * T::kCpr + 2 * j + half];
-      qf[j] = x;
-    }
+    for (int j = 0; j < T::kSteps; ++j) qf[j] = reinterpret_cast<const u32x4*>(p.q)[((long long)q_seq * p.H + q_head) * T::kCpr + 2 * j + half];
+#pragma unroll
+    for (int j = 0; j < T::kSteps; ++j) qf[j] = real ? qf[j] : u32x4{0u, 0u, 0u, 0u};
     const int q_pos = OPT && p.pos != nullptr ? p.q_pos[q_seq] : 0;
     const float slope = OPT && p.slopes != nullptr ? p.slopes[q_head] * kLog2e : 0.0f;
 
@@ -509,8 +508,9 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_rows_kernel(const Shared
       int lo = 0x7fffffff, hi = -0x7fffffff - 1;
       for (int i = lane; i < it.n_seq; i += 64) {
         const int y = p.q_pos[it.first_seq + i];
-        lo = min(lo, y);
-        hi = max(hi, y);
+        const bool holds = p.head_rows[(long long)(it.first_seq + i) * p.H_kv + it.head] != 0;
+        lo = holds ? min(lo, y) : lo;
+        hi = holds ? max(hi, y) : hi;
       }
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) {
