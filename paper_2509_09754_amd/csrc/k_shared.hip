@@ -19,8 +19,9 @@
 //           probabilities stay in registers.  bf16: V is read transposed from LDS, a probability is three bf16 parts (8 + 8 +
 //           8 bits), so that products are exact and sums 32 bits, as in the decode step over pages (with two parts an output
 //           would be off by 2.4e-6 of itself)
-// Rows that are masked may hold anything there.  A product cannot leave them out, so an item whose sums are not all
-// finite is marked, and merge computes its heads' outputs again, row by row.
+// Rows that are masked may hold anything there.  A product cannot leave them out, so a sequence's head whose sums are not all
+// finite is marked, and merge computes its outputs again, row by row.  (A query is a column of the products: one that is no number
+// leaves the others of its item as they are.)
 //
 // Bound by HBM for few queries: 4 groups of 4 sequences with 8 KV heads of 65536 rows (1.07 GB) 208 us a step, 5.2 TB/s.  By the matrix
 // cores for many: 64 sequences over 8 heads of 131072 rows need 275 GFLOP with the three parts, 265 us, 1.04 PFLOP/s, where a large matrix
@@ -59,7 +60,7 @@ struct SharedArgs {
   int* n_items;                                // number of items; units that were taken out of turn
   SharedItem* items;
   SharedParts *parts, *own_parts;              // [items], [batch][H_kv]
-  int *marked, *own_marked;                    // [items], [batch][H_kv] sums that are not finite
+  int *marked, *head_marked;                   // [items] 2: a page is not in the pool; [batch][H_kv] 1: sums that are not finite, 2: of own rows, a page
   int* item_of;                                // [batch][H_kv] item that has the sequence's common rows, -1: none
   int *rest_rows, *skip;                       // [batch][H_kv] rows that are left (as a unit's: -1 if there cannot be as many), blocks in common
   int* rest_table;                             // [batch][H_kv][max_blocks] where own rows are decoded by themselves
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
         const bool none = rows[i] < 0 || rows[i] > p.max_blocks << p.page_shift;
         a.rest_rows[h[i]] = a.own_here != 0 && none ? -1 : rows[i] - (skip[i] << p.page_shift);
         a.skip[h[i]] = skip[i];
-        a.own_marked[h[i]] = 0;
+        a.head_marked[h[i]] = 0;
         a.item_of[h[i]] = skip[i] > 0 ? item0 + (b - b0) / seqs : -1;
       }
       int* rest = a.rest_table + h[i] * p.max_blocks;
@@ -702,9 +703,8 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_rows_kernel(const Shared
     for (int d = 0; d < S::kDBlocks; ++d)
 #pragma unroll
       for (int v = 0; v < 16; ++v) wrong |= !(fabsf(acc[d][v]) < INFINITY);
-    wrong = wrong && real;
+    if (wrong && real) atomicOr(&a.head_marked[(long long)q_seq * p.H_kv + it.head], 1);
     __syncthreads();                                           // every wavefront is done with the stages
-    if (__ballot(wrong) != 0ull && lane == 0) atomicOr(&s_wrong, 1);
     constexpr int kChunks = D / 4;                             // 16-byte chunks of an output row
     float* s_acc = reinterpret_cast<float*>(&s_stage[0][0]);
     if (half == 0) {
@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(kShThreads, 2) shared_rows_kernel(const Shared
       }
     __syncthreads();
     if (threadIdx.x == 0) {
-      if (s_wrong != 0) atomicOr(item >= 0 ? &a.marked[item] : &a.own_marked[it.first_seq * p.H_kv + it.head], s_wrong);
+      if (s_wrong != 0) atomicOr(item >= 0 ? &a.marked[item] : &a.head_marked[it.first_seq * p.H_kv + it.head], s_wrong);
       s_next = (int)next_unit;
     }
     const long long out0 = (long long)row0 + (long long)part * q_rows;
@@ -838,7 +838,7 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
     return;
   }
   const int rest = here ? a.rest_rows[blockIdx.x] : 0;
-  const int marked = (item >= 0 ? a.marked[item] : 0) | (here ? a.own_marked[blockIdx.x] : 0);
+  const int marked = (item >= 0 ? a.marked[item] : 0) | a.head_marked[blockIdx.x];
   if (marked == 1) {                                           // no page was wrong: only values
     whole_head<DT, D>(a, b, g, s_red);
     return;
@@ -922,7 +922,7 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
 bool own_is_here(const lava_layer_desc& d, int32_t batch) { return (int64_t)batch * d.n_kv_heads <= kOwnHeads; }
 
 struct SharedLayout {
-  size_t off_items, off_parts, off_own_parts, off_marked, off_own_marked, off_item_of, off_rest_rows, off_skip, off_rest_table, off_rest_lse, off_ml, off_acc;
+  size_t off_items, off_parts, off_own_parts, off_marked, off_head_marked, off_item_of, off_rest_rows, off_skip, off_rest_table, off_rest_lse, off_ml, off_acc;
   size_t off_decode, bytes, own_base;
 };
 SharedLayout shared_layout(const lava_layer_desc& d, int32_t batch, int32_t max_blocks) {
@@ -937,8 +937,8 @@ SharedLayout shared_layout(const lava_layer_desc& d, int32_t batch, int32_t max_
   l.off_parts = l.off_items + align_up(heads * sizeof(SharedItem));
   l.off_own_parts = l.off_parts + align_up(heads * sizeof(SharedParts));
   l.off_marked = l.off_own_parts + align_up(heads * sizeof(SharedParts));
-  l.off_own_marked = l.off_marked + align_up(heads * 4);
-  l.off_item_of = l.off_own_marked + align_up(heads * 4);
+  l.off_head_marked = l.off_marked + align_up(heads * 4);
+  l.off_item_of = l.off_head_marked + align_up(heads * 4);
   l.off_rest_rows = l.off_item_of + align_up(heads * 4);
   l.off_skip = l.off_rest_rows + align_up(heads * 4);
   l.off_rest_table = l.off_skip + align_up(heads * 4);
@@ -998,7 +998,7 @@ int32_t launch_shared_decode(const lava_layer_desc& d, const PagedDecodeArgs& p,
   a.own_base = (int)l.own_base;
   a.own_parts = reinterpret_cast<SharedParts*>(w + l.off_own_parts);
   a.marked = reinterpret_cast<int*>(w + l.off_marked);
-  a.own_marked = reinterpret_cast<int*>(w + l.off_own_marked);
+  a.head_marked = reinterpret_cast<int*>(w + l.off_head_marked);
   a.skip = reinterpret_cast<int*>(w + l.off_skip);
   a.item_of = reinterpret_cast<int*>(w + l.off_item_of);
   a.rest_rows = reinterpret_cast<int*>(w + l.off_rest_rows);

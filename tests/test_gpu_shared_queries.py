@@ -43,3 +43,40 @@ def test_queries_of_sequences_that_hold_nothing(lava, dtype, d, idle, kw):
     c.check(out, lse)
 
 
+
+
+@IDLE
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("kw", [{}, dict(window=1500, softcap=20.0)], ids=["plain", "window and cap"])
+def test_one_query_that_is_no_number(lava, dtype, d, idle, kw):
+    """The sequence's own results are NaN where it sees rows.  The others' are what they are beside a query of zeros, whose logits' maximum moves no
+    more often either: at the first rows that are seen."""
+    c = case(lava, dtype, d, idle, kw)
+    c.q_pos.fill_(2000)
+    c.q[4], c.q[9, :4] = 0.0, 0.0                                      # all heads of one sequence, one KV head's of another
+    want, want_lse = c.run()
+    assert bool(torch.isfinite(want_lse[[0, 3, 4, 9]]).all())
+    c.q[4], c.q[9, :4] = float("nan"), float("nan")
+    out, lse = c.run()
+    hit = torch.zeros(c.batch, 8, dtype=torch.bool, device=out.device)
+    hit[4], hit[9, :4] = True, True
+    assert torch.equal(torch.isnan(lse), hit) and torch.equal(torch.isnan(out), hit[..., None].expand_as(out))
+    assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+
+
+def test_values_that_one_sequence_does_not_see(lava):
+    """An infinity that the window of one group member leaves out: that member is looked at row by row, and gets what it gets without it."""
+    c = case(lava, "bf16", 128, 0, dict(window=300))
+    c.pos.copy_(torch.randint(0, 200, c.pos.shape, device=c.pos.device))
+    c.q_pos.fill_(199)
+    c.q_pos[3] = 420                                                   # sees positions from 121 on
+    c.check(*c.run())
+    low = c.pos < 100
+    v = c.v.clone()
+    c.v[low] = float("inf")
+    out, lse = c.run()
+    c.v[low] = v[low]
+    want, want_lse, tol, tol_lse = c.want()
+    assert bool(((out[3].double().cpu() - want[3]).abs() <= tol[3] + 2.0 ** -22 * 6).all())
+    assert bool(((lse.double().cpu() - want_lse).abs()[want_lse.isfinite()] <= (tol_lse + want_lse.abs() * 2.0 ** -21)[want_lse.isfinite()]).all())
+    assert not bool(torch.isfinite(out[0]).all())
