@@ -64,10 +64,12 @@ def test_one_query_that_is_no_number(lava, dtype, d, idle, kw):
     assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
 
 
-def test_values_that_one_sequence_does_not_see(lava):
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("kw", [dict(window=300), dict(window=300, bias=True, softcap=20.0)], ids=["window", "all"])
+def test_values_that_one_sequence_does_not_see(lava, dtype, d, kw):
     """An infinity that the window of one group member leaves out: that member is looked at row by row, and gets what it gets without it."""
-    c = case(lava, "bf16", 128, 0, dict(window=300))
-    c.pos.copy_(torch.randint(0, 200, c.pos.shape, device=c.pos.device))
+    c = case(lava, dtype, d, 0, kw)
+    c.pos.copy_(torch.randint(0, 200, c.pos.shape, device=c.pos.device, generator=torch.Generator(c.pos.device).manual_seed(3)))
     c.q_pos.fill_(199)
     c.q_pos[3] = 420                                                   # sees positions from 121 on
     c.check(*c.run())
@@ -77,6 +79,7 @@ def test_values_that_one_sequence_does_not_see(lava):
     out, lse = c.run()
     c.v[low] = v[low]
     want, want_lse, tol, tol_lse = c.want()
+    some = want_lse.isfinite()
     assert bool(((out[3].double().cpu() - want[3]).abs() <= tol[3] + 2.0 ** -22 * 6).all())
-    assert bool(((lse.double().cpu() - want_lse).abs()[want_lse.isfinite()] <= (tol_lse + want_lse.abs() * 2.0 ** -21)[want_lse.isfinite()]).all())
+    assert bool(((lse.double().cpu() - want_lse).abs()[some] <= (tol_lse + want_lse.abs() * 2.0 ** -21)[some]).all())
     assert not bool(torch.isfinite(out[0]).all())
