@@ -295,6 +295,7 @@ struct PagedDecodeArgs {
   float scale, cap;
   float* out;
   float* lse;
+  float2* sums;                // [batch][H] or null: maximum (log2 units) and sum of every row's softmax, what its log-sum-exp is rounded from
 };
 size_t paged_decode_bytes(const lava_layer_desc& d);
 int32_t launch_paged_decode(const lava_layer_desc& d, const PagedDecodeArgs& a, void* ws, hipStream_t s);

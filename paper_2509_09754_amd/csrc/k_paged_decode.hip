@@ -74,6 +74,12 @@ __device__ __forceinline__ int head_tiles(const PagedDecodeArgs& a, int rows) {
   return (int)(((unsigned int)rows + kTileKeys - 1u) / kTileKeys);
 }
 
+// What a row's softmax sums to, in the forms that are asked for.
+__device__ __forceinline__ void write_sums(const PagedDecodeArgs& p, long long row, float M, float L) {
+  if (p.lse != nullptr) p.lse[row] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  if (p.sums != nullptr) p.sums[row] = make_float2(M, L);
+}
+
 // Two values of an output row from the maximum (log2 units), the sum and the weighted values; no row seen: zeros.
 template <int D>
 __device__ __forceinline__ void write_row(const PagedDecodeArgs& p, int b, int g, int t, int e, float M, float L, float2 sum) {
@@ -81,7 +87,7 @@ __device__ __forceinline__ void write_row(const PagedDecodeArgs& p, int b, int g
   const bool none = L == 0.0f;
   p.out[row * D + e] = none ? 0.0f : sum.x / L;
   p.out[row * D + e + 1] = none ? 0.0f : sum.y / L;
-  if (p.lse != nullptr && e == 0) p.lse[row] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  if (e == 0) write_sums(p, row, M, L);
 }
 
 // The maximum, and the sum, over the 32 lanes of this lane's half of the wavefront, in each of them.
@@ -224,7 +230,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
       const int b = h / p.H_kv;
       const long long row0 = (long long)b * p.H + (long long)(h - b * p.H_kv) * p.G;
       for (int i = threadIdx.x; i < p.G * D; i += kDecThreads) p.out[row0 * D + i] = n < 0 ? NAN : 0.0f;
-      if (p.lse != nullptr && (int)threadIdx.x < p.G) p.lse[row0 + threadIdx.x] = n < 0 ? NAN : -INFINITY;
+      if ((int)threadIdx.x < p.G) write_sums(p, row0 + threadIdx.x, -INFINITY, n < 0 ? NAN : 0.0f);
     }
   }
   if (total == 0u) return;
@@ -599,7 +605,7 @@ __global__ void __launch_bounds__(kDecThreads, (kWavesPerSimd<DT, D>)) paged_dec
         const long long row = (long long)b * p.H + (long long)g * p.G + i;
 #pragma unroll
         for (int e = 0; e < kDpl; ++e) p.out[row * D + lane * kDpl + e] = L == 0.0f ? 0.0f : acc[i][e] / L;
-        if (p.lse != nullptr && lane == 0) p.lse[row] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        if (lane == 0) write_sums(p, row, M, L);
       }
       if (last) return;
       hb = next_head;

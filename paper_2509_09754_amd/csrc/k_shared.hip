@@ -64,7 +64,7 @@ struct SharedArgs {
   int* item_of;                                // [batch][H_kv] item that has the sequence's common rows, -1: none
   int *rest_rows, *skip;                       // [batch][H_kv] rows that are left (as a unit's: -1 if there cannot be as many), blocks in common
   int* rest_table;                             // [batch][H_kv][max_blocks] where own rows are decoded by themselves
-  float* rest_lse;                             // [batch][H]
+  float2* rest_sums;                           // [batch][H] and what they sum to
   float2* part_ml;                             // [rows] maximum (log2 units) and sum
   float* part_acc;                             // [rows][D]
 };
@@ -865,10 +865,7 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
   const int item = a.item_of[blockIdx.x];
   const bool here = a.own_here != 0;
   const long long row0 = (long long)b * p.H + (long long)g * p.G;
-  if (item < 0 && !here) {                                     // nothing in common: the own rows were all
-    if (p.lse != nullptr && (int)threadIdx.x < p.G) p.lse[row0 + threadIdx.x] = a.rest_lse[row0 + threadIdx.x];
-    return;
-  }
+  if (item < 0 && !here) return;                               // nothing in common: the own rows were all
   const int rest = here ? a.rest_rows[blockIdx.x] : 0;
   const int marked = (item >= 0 ? a.marked[item] : 0) | a.head_marked[blockIdx.x];
   if (marked == 1) {                                           // no page was wrong: only values
@@ -896,8 +893,8 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // a wavefront a query: the maximum over its parts, then their weights
   for (int t = wave; t < p.G; t += kMergeThreads / 64) {
-    const float own = here ? -INFINITY : a.rest_lse[row0 + t] * kLog2e;
-    float M = own, L = 0.0f;
+    const float2 own = here ? make_float2(-INFINITY, 0.0f) : a.rest_sums[row0 + t];
+    float M = own.x, L = 0.0f;
     for (int u = lane; u < n; u += 64) M = fmaxf(M, a.part_ml[row_of(u, t)].x);
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) M = fmaxf(M, __shfl_xor(M, m));
@@ -908,9 +905,9 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) L += __shfl_xor(L, m);
-    const float wgt = fast_exp2(own - base);
+    const float wgt = fast_exp2(own.x - base) * own.y;         // NaN: a page that is not in the pool, or rows that cannot be
     L += wgt;
-    if (marked != 0 || isnan(own) || rest < 0) L = NAN;        // a page that is not in the pool, or rows that cannot be
+    if (marked != 0 || rest < 0) L = NAN;                      // the same
     if (lane == 0) {
       s_base[t] = base;
       s_own[t] = wgt;
@@ -954,7 +951,7 @@ __global__ void __launch_bounds__(kMergeThreads) shared_merge_kernel(const Share
 bool own_is_here(const lava_layer_desc& d, int32_t batch) { return (int64_t)batch * d.n_kv_heads <= kOwnHeads; }
 
 struct SharedLayout {
-  size_t off_items, off_parts, off_own_parts, off_marked, off_head_marked, off_item_of, off_rest_rows, off_skip, off_rest_table, off_rest_lse, off_ml, off_acc;
+  size_t off_items, off_parts, off_own_parts, off_marked, off_head_marked, off_item_of, off_rest_rows, off_skip, off_rest_table, off_rest_sums, off_ml, off_acc;
   size_t off_decode, bytes, own_base;
 };
 SharedLayout shared_layout(const lava_layer_desc& d, int32_t batch, int32_t max_blocks) {
@@ -974,8 +971,8 @@ SharedLayout shared_layout(const lava_layer_desc& d, int32_t batch, int32_t max_
   l.off_rest_rows = l.off_item_of + align_up(heads * 4);
   l.off_skip = l.off_rest_rows + align_up(heads * 4);
   l.off_rest_table = l.off_skip + align_up(heads * 4);
-  l.off_rest_lse = l.off_rest_table + (own_is_here(d, batch) ? 0 : align_up(heads * max_blocks * 4));
-  l.off_ml = l.off_rest_lse + align_up((size_t)batch * d.n_q_heads * 4);
+  l.off_rest_sums = l.off_rest_table + (own_is_here(d, batch) ? 0 : align_up(heads * max_blocks * 4));
+  l.off_ml = l.off_rest_sums + (own_is_here(d, batch) ? 0 : align_up((size_t)batch * d.n_q_heads * sizeof(float2)));
   l.off_acc = l.off_ml + align_up(rows * sizeof(float2));
   l.off_decode = l.off_acc + align_up(rows * d.head_dim * sizeof(float));
   l.bytes = l.off_decode + paged_decode_bytes(d);
@@ -1035,7 +1032,7 @@ int32_t launch_shared_decode(const lava_layer_desc& d, const PagedDecodeArgs& p,
   a.item_of = reinterpret_cast<int*>(w + l.off_item_of);
   a.rest_rows = reinterpret_cast<int*>(w + l.off_rest_rows);
   a.rest_table = reinterpret_cast<int*>(w + l.off_rest_table);
-  a.rest_lse = reinterpret_cast<float*>(w + l.off_rest_lse);
+  a.rest_sums = reinterpret_cast<float2*>(w + l.off_rest_sums);
   a.part_ml = reinterpret_cast<float2*>(w + l.off_ml);
   a.part_acc = reinterpret_cast<float*>(w + l.off_acc);
   {
@@ -1051,7 +1048,7 @@ int32_t launch_shared_decode(const lava_layer_desc& d, const PagedDecodeArgs& p,
     PagedDecodeArgs own = p;
     own.block_table = a.rest_table;
     own.head_rows = a.rest_rows;
-    own.lse = a.rest_lse;
+    own.sums = a.rest_sums;
     st = launch_paged_decode(d, own, w + l.off_decode, s);
   }
   if (st == LAVA_OK)

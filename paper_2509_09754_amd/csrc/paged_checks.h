@@ -69,6 +69,7 @@ inline int32_t check_paged_decode(const lava_layer_desc* desc, int32_t batch, co
   a.cap = o.softcap;
   a.out = out;
   a.lse = lse;
+  a.sums = nullptr;
   return LAVA_OK;
 }
 
