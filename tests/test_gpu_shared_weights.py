@@ -3,7 +3,7 @@ from few roundings, which the bounds count."""
 import numpy as np
 import pytest
 
-from test_gpu_shared import dev, shared_tables, widened
+from test_gpu_shared import OPTIONS, SHAPES, Case, dev, shared_tables, widened
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -52,3 +52,63 @@ def test_large_logits(lava, dtype, d, idle):
     # 4096 log2 e, its sum with a logarithm (within 2^-22 of itself), the product with ln 2: half a step each, of up to 5925 and 4107
     assert bool(((lse[:8].double() - want_lse).abs() <= 4 * STEP * 4107 + 2.0 ** -20).all()), float((lse[:8].double() - want_lse).abs().max())
     assert not bool(out[8:].any()) and bool((lse[8:] == -float("inf")).all())
+
+
+@pytest.mark.parametrize("H,Hkv,d,dtype,page", SHAPES)
+@pytest.mark.parametrize("kw", OPTIONS, ids=["plain", "cap", "bias", "window", "all"])
+@pytest.mark.parametrize("idle", [0, 520], ids=["few", "many"])
+def test_within_the_bounds_of_the_step_over_pages(lava, H, Hkv, d, dtype, page, kw, idle):
+    """Nothing is stored between the parts but maxima, sums and values in 32 bits: the bound of the decode step over pages holds, and the roundings of
+    putting two parts together."""
+    rng = np.random.default_rng(H + d + page + len(kw))
+    sizes = [7, 2, 1, idle]
+    table, rows, n_pages = shared_tables(rng, sizes, Hkv, page, lambda i, g: (150 + 16 * i) // page + g % 2, 0, 90, idle=range(10, 10 + idle))
+    c = Case(lava, rng, H, Hkv, d, dtype, page, sizes, table, rows, n_pages, **kw)
+    out, lse = c.run()
+    want, want_lse, tol, tol_lse = c.want()
+    out, lse = out.double().cpu(), lse.double().cpu()
+    some = torch.isfinite(want_lse)
+    assert torch.equal(torch.isfinite(lse), some)
+    # a part's weight: its exponential within 2^-23, a product, a sum and, of own rows by themselves, a division and a product; what
+    # three bf16 parts leave out of a probability, 2^-24.  Each of those is relative to an average of values
+    top = float(c.v.double().abs().max())
+    assert bool(((out - want).abs() <= tol + 12 * STEP * top)[some].all()), float(((out - want).abs() / (tol + 12 * STEP * top))[some].max())
+    assert bool(((lse - want_lse).abs() <= tol_lse + 8 * STEP)[some].all())
+
+
+def third_part(e):
+    """What is left of e behind two parts of 8 bits, relative to it."""
+    half = lambda x: torch.tensor(x, dtype=torch.float32).bfloat16().double().item()
+    e = torch.tensor(e, dtype=torch.float32).double().item()
+    return abs(e - half(e) - half(e - half(e))) / e
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("own", [False, True], ids=["common", "own"])
+def test_probabilities_of_24_bits(lava, d, own):
+    """One row at a logit whose probability has its largest remainder behind 16 bits, at value 1 among rows of value 0: without that remainder
+    the result would be off by more than the bound."""
+    logits = torch.arange(2, 46).double() * -2.0 ** -7                 # numbers of 8 bits
+    left = [third_part(x) for x in logits.exp().tolist()]
+    z = float(logits[int(np.argmax(left))])
+    page, Hkv, G = 16, 2, 4
+    n_own = 2 if own else 0
+    table = widened(np.arange(2 * Hkv * 2).reshape(2, Hkv, 2).astype(np.int32), page, 2 * d * 2)
+    table[1, :, 0] = table[0, :, 0]
+    rows = np.full((2, Hkv), page + n_own, np.int32)
+    k, v = (torch.zeros(2 * Hkv * 2, page, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    for page_no in (table[:, :, 1] if own else table[0, :, 0]).reshape(-1).tolist():
+        k[page_no, 1 if own else page - 1, 3] = z
+        v[page_no, 1 if own else page - 1] = 1.0
+    q = torch.zeros(2, G * Hkv, d, dtype=torch.bfloat16, device=DEV)
+    q[:, :, 3] = 1.0
+    desc = lava.LayerDesc.make(G * Hkv, Hkv, d, 1, "bf16", softmax_scale=1.0)
+    out, lse = lava.lava_shared_decode(desc, q, lava.PagePool(k, v, None, max_blocks=table.shape[2]), dev(table), dev(rows), dev(np.array([0, 2], np.int32)))
+    torch.cuda.synchronize()
+    e = float(np.exp(z))
+    want = e / (page + n_own - 1 + e)
+    # half steps: the scaled logit two, of a difference below 0.5 in log2 units (one); the exponential two; the value's three products; the sum of 16
+    # or 18 terms one each; two parts put together four; a division five
+    bound = (1 + 2 + 3 + 18 + 4 + 5) * STEP
+    assert max(left) > 1.5 * bound
+    assert bool(((out.double() - want).abs() <= bound * want).all()), float(((out.double() - want).abs() / want).max() / STEP)
