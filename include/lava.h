@@ -738,7 +738,8 @@ size_t lava_beam_step_workspace_bytes(int32_t batch, int32_t beams, int64_t voca
  *   Beam i with score s_i and logits x_i goes on with token v at  c = s_i + (x_i[v] - log sum_u exp(x_i[u])).
  *   A beam that is done has one continuation: pad_token, at its score.
  *   One candidate comes before another if its c is larger; if the beam's number is smaller; if, of one beam, the
- *   logit is larger; if the token's number is smaller.  c is formed in 64 bits.
+ *   logit is larger; if the token's number is smaller.  c is formed in 64 bits, its exponentials within 4.1e-11 of
+ *   themselves: of candidates of two beams that are no further apart either may come first.
  *
  *   dtype        LAVA_F32 or LAVA_BF16, of the logits
  *   logits       device, row b * beams + i at element (b * beams + i) * logit_stride, vocab values one after another;
@@ -748,12 +749,15 @@ size_t lava_beam_step_workspace_bytes(int32_t batch, int32_t beams, int64_t voca
  *   done         device int32 [batch][beams] or NULL (none is): non-zero, the beam is over.  Its logits are not read
  *   end_token    a continuation with it is done from now on; negative: there is none
  *   pad_token    0 <= pad_token < vocab
- *   parents      device int32 [batch][n_out]   row of the beam that goes on, b * beams + i: `source` of lava_page_fork
+ *   parents      device int32 [batch][n_out]   row of the beam that goes on, b * beams + i.  Where n_out = beams that is
+ *                the `source` of lava_page_fork.  With another n_out it is not: a source is a place of the state, of which
+ *                there are as many before as after, so the caller puts the parents, as places, where the beams that go on
+ *                are to be, and -1 into the others
  *   tokens       device int32 [batch][n_out]
  *   scores_out   device float [batch][n_out]   c, rounded once; may be `scores` itself where n_out = beams
  *   done_out     device int32 [batch][n_out] or NULL; may be `done` itself where n_out = beams
  *   sources      device int32 [n_tables][batch * n_out] or NULL (n_tables 0): parents + t * batch * beams (a parent of -1 stays),
- *                the `source` of a state that holds n_tables layers as sequences of their own
+ *                where n_out = beams the `source` of a state that holds n_tables layers as sequences of their own
  * Sorted, the best first.  A place without a candidate gets parent -1, token -1, score -inf, done 1.  A beam with a NaN or +inf
  * among its logits, or with nothing but -inf, has no continuation.
  * beams, n_out <= 64, vocab < 2^31, batch <= 65535, n_tables <= 1024, batch * beams * ceil(vocab / 8192) < 2^24,
@@ -803,6 +807,11 @@ int32_t lava_page_fork(const lava_layer_desc* desc, const lava_page_pool* pool, 
  * the head's last before); the rows behind go to fresh pages, and pages that are in no table any more go back.  seq_pos stays as it is.  Pages are
  * taken before any go back: the stack has to hold as many as the call fills.  Everything else as for lava_page_fork; counts that
  * are negative, more than a head holds or together more than kept_capacity are LAVA_PAGES_INVALID.
+ * Rows behind the first one that is not kept are a sequence's own afterwards, also where sequences that shared them keep the same ones: eviction of
+ * n of them fills up to n times the pages, and may need more than it gives back.  A prompt is best evicted before it is forked.
+ * Where the lists come from: rows in pages have no scores of their own.  A program keeps kept_scores of the selection that filled
+ * the pages, in the order of the rows (heads one after another), moves them with the sequences' sources, appends a score for every
+ * new row (+inf: it stays) and selects from them again.
  */
 int32_t lava_page_compact(const lava_layer_desc* desc, const lava_page_pool* pool, int32_t batch, const lava_page_state* state,
                           const int32_t* head_counts, const int32_t* kept_idx, int64_t kept_capacity, const int32_t* evict,
@@ -815,7 +824,7 @@ size_t lava_shared_decode_workspace_bytes(const lava_layer_desc* desc, int32_t b
 /*
  * lava_paged_decode for groups of sequences that share pages: the pages that the tables of all sequences of a group begin with are read
  * once, for the queries of all of them; then every sequence's own.  The result is lava_paged_decode's up to the order of
- * summation, whatever the tables hold.
+ * summation, whatever the tables hold.  Where a group has nothing in common the step takes up to half as long again as that one.
  *
  *   n_groups     1 .. batch
  *   group_start  device int32 [n_groups + 1]: group i is sequences group_start[i] .. group_start[i + 1] - 1; from 0, without a

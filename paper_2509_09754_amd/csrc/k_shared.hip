@@ -23,10 +23,13 @@
 // finite is marked, and merge computes its outputs again, row by row.  (A query is a column of the products: one that is no number
 // leaves the others of its item as they are.)
 //
-// Bound by HBM for few queries: 4 groups of 4 sequences with 8 KV heads of 65536 rows (1.07 GB) 208 us a step, 5.2 TB/s.  By the matrix
-// cores for many: 64 sequences over 8 heads of 131072 rows need 275 GFLOP with the three parts, 265 us, 1.04 PFLOP/s, where a large matrix
-// product of the library reaches 1.12; with own rows, 26 us by themselves, 294 in one launch.  32 bits: by the 32-bit matrix
-// instructions, which two or four of the eight wavefronts of few queries issue.
+// Bound by HBM for few queries: 4 groups of 4 sequences with 8 KV heads of 65536 rows (1.07 GB) 208 us a step, 5.2 TB/s.  For many by
+// products and the softmax between them in turn: 64 sequences over 8 heads of 131072 rows need 275 GFLOP with the three parts; rows 287 us
+// (by events, own rows among them), 0.96 PFLOP/s with the matrix cores busy for 45 % at 1.95 GHz, where a large product of the library has
+// 1.1 to 1.3 with 66 % at 1.5 to 1.7.  Plan 16, merge 13, the step 309.  Six groups of 3 to 17 sequences, 7 heads each, capped, biased and in
+// windows of 8192 of up to 65536 positions: rows 66 us, of which cap and bias take 6; neither bytes (1.3 TB/s) nor products (8 % busy),
+// but units that begin unhidden and hold unevenly many stages of the window.  32 bits: by the 32-bit matrix instructions, which two or four
+// of the eight wavefronts of few queries issue.
 #include <math.h>
 
 #include "common.h"
@@ -224,8 +227,11 @@ __global__ void __launch_bounds__(kPlanShThreads) shared_plan_kernel(const Share
 // most, and half of the tiles need no rescaling of the output (296 -> 283 us).
 constexpr float kSlack = 8.0f;
 
-// (sequence, head) pairs whose own rows are units of the same launch, at most.  A launch of their own costs more than it does (64 sequences
-// of 131072 rows 315 -> 304 us, ragged ones 90 -> 85); more are many small units, and their number is found again by every workgroup.
+// (sequence, head) pairs whose own rows are units of the same launch, at most; more are many small units, and their number is found again by
+// every workgroup.  Groups x sequences over 16384 rows and 300 own ones, bf16, 8 KV heads, us a step with own rows apart and here:
+//   256 heads   4 x 8 85.5 and 79.7, 1 x 32 64.8 and 60.8        512   8 x 8 144 and 139, 1 x 64 87.7 and 84.8 (40 own rows: 76.7 and 73.7)
+//   768 heads   12 x 8 233 and 218, 2 x 48 128 and 124 (40 own rows: 102 and 107)
+//   1024 heads  16 x 8 322 and 309, 2 x 64 136 and 145 (40: 110 and 120), 64 x 2 over 4096 rows with 100 own 230 and 241
 constexpr int kOwnHeads = 512;
 
 template <int DT, int D>
@@ -1002,7 +1008,8 @@ int32_t launch_merge(const SharedArgs& a, hipStream_t s) {
 // Tables that have room for no more bytes of keys and values than this, counted once for every sequence, are decoded sequence by sequence: the
 // step over pages reads them, from the last-level cache mostly, before three launches have found out what is common.  bf16, d_h 128,
 // 8 KV heads, apart and shared: 8 sequences of 4096 rows (138 MB) 24 and 36 us, 16 (277 MB) 35 and 40, 8 of 16384 (541 MB) 56 and 40,
-// 4 groups of 8 of 4096 (554 MB) 55 and 41; 32 bits: 8 of 4096 (277 MB) 48 and 50, 4 of 16384 (541 MB) 80 and 76.
+// 4 groups of 8 of 4096 (554 MB) 55 and 41; 32 bits: 8 of 4096 (277 MB) 48 and 50, 4 of 16384 (541 MB) 80 and 76.  Room is all that the host
+// knows: tables with room for much more than they hold (4 sequences of 1024 rows a head, room for 131072) take 24 us where narrow ones take 13.
 constexpr long long kApartBytes = 400000000;
 
 }  // namespace
