@@ -785,13 +785,15 @@ __device__ __forceinline__ void whole_head(const SharedArgs& a, int b, int g, fl
     float q[kEach], acc[kEach] = {}, M = -INFINITY, L = 0.0f;
     load(p.q, row, q);
     bool bad = false;
-    for (int r0 = 64 * wave; r0 < rows; r0 += 64 * kWaves) {
+    for (unsigned int r0 = 64u * wave; r0 < (unsigned int)rows; r0 += 64u * kWaves) {   // (a head may have 2^31 rows, nearly)
       // a lane a row: where it lies and whether it is seen
-      const int r = r0 + lane, page = r < rows ? table[r >> p.page_shift] : 0;
-      const bool there = r < rows && page >= 0 && page < p.n_pages;
-      const long long place = there ? ((long long)page << p.page_shift) + (r & ((1 << p.page_shift) - 1)) : 0;
+      const unsigned int r = r0 + lane;
+      const bool held = r < (unsigned int)rows;
+      const int page = held ? table[r >> p.page_shift] : 0;
+      const bool there = held && page >= 0 && page < p.n_pages;
+      const long long place = there ? ((long long)page << p.page_shift) + (int)(r & ((1u << p.page_shift) - 1u)) : 0;
       const unsigned int back = p.pos != nullptr && there ? (unsigned int)q_pos - (unsigned int)p.pos[place] : 0u;
-      bad |= __ballot(r < rows && !there) != 0ull;
+      bad |= __ballot(held && !there) != 0ull;
       unsigned long long todo = __ballot(there && back < window);
       while (todo != 0ull) {                                   // uniform; kAtOnce of the rows that are seen
         bool on[kAtOnce];

@@ -60,3 +60,31 @@ def test_units_of_many_stages(lava, dtype, d, stage, form):
     rows = (stages * page + own).astype(np.int32)
     print(f"{form}: {dtype} d {d}, {rows[0, 0]} rows, {stages} stages", flush=True)
     run(lava, dtype, d, 4, pages, table, rows, 350 if windowed else 0, torch.tensor([999, 950], dtype=torch.int32, device=DEV))
+
+
+@pytest.mark.parametrize("window", [0, 1000], ids=["plain", "window"])
+def test_as_many_rows_as_can_be(lava, window):
+    """2^31 - 256 rows: the first, the last and one between have a value, and one of the two queries is no number."""
+    page, d, blocks = 256, 64, (1 << 23) - 1
+    desc = lava.LayerDesc.make(1, 1, d, 1, "bf16")
+    k = torch.zeros(4, page, d, dtype=torch.bfloat16, device=DEV)
+    v = torch.ones(4, page, d, dtype=torch.bfloat16, device=DEV)
+    k[1:, ::page // 2] = 1.0                                          # two rows of page 1 to 3
+    pos = torch.zeros(4, page, dtype=torch.int32, device=DEV)
+    for i in (1, 2, 3):
+        v[i, ::page // 2] = 8.0 * i
+        pos[i, ::page // 2] = 5000
+    table = torch.zeros(2, 1, blocks, dtype=torch.int32, device=DEV)
+    table[:, 0, 0], table[:, 0, 5_000_001], table[:, 0, -1] = 1, 2, 3
+    rows = torch.full((2, 1), blocks * page, dtype=torch.int32, device=DEV)
+    q = torch.full((2, 1, d), 8.0, dtype=torch.bfloat16, device=DEV)   # logit 64 for those six rows, 0 for 2^31: e^-64 of them each, 3.4e-19 in all
+    q[1] = float("nan")
+    pool = lava.PagePool(k, v, pos, max_blocks=blocks)
+    options = lava.DecodeOptions.make(window=window) if window else None
+    q_pos = torch.full((2,), 5500, dtype=torch.int32, device=DEV)
+    start = torch.tensor([0, 2], dtype=torch.int32, device=DEV)
+    out, lse = lava.lava_shared_decode(desc, q, pool, table, rows, start, options, q_pos)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(out[1]).all()) and bool(torch.isnan(lse[1]).all())
+    assert bool(((out[0] - 16.0).abs() <= 16.0 * 2.0 ** -20).all()), out[0, 0, :4].tolist()
+    assert abs(float(lse[0, 0]) - (64.0 + np.log(6.0))) <= 66 * 2.0 ** -21
