@@ -743,7 +743,7 @@ size_t lava_beam_step_workspace_bytes(int32_t batch, int32_t beams, int64_t voca
  *
  *   dtype        LAVA_F32 or LAVA_BF16, of the logits
  *   logits       device, row b * beams + i at element (b * beams + i) * logit_stride, vocab values one after another;
- *                aligned to their size only.  -inf is a token that cannot follow
+ *                aligned to their size only; logit_stride >= vocab if there are several.  -inf is a token that cannot follow
  *   scores       device float [batch][beams].  A beam whose score is not finite has no continuation (at the first step
  *                all beams but one of a group that starts from one prompt: -inf)
  *   done         device int32 [batch][beams] or NULL (none is): non-zero, the beam is over.  Its logits are not read

@@ -1010,7 +1010,7 @@ def lava_beam_step(logits: torch.Tensor, scores: torch.Tensor, n_out: Optional[i
     parents for a state that holds n_tables layers as sequences of their own.  Returns (parents, tokens, scores_out, done_out), each
     [batch, n_out]; parents are rows b * beams + i, what lava_page_fork takes where n_out = beams (with another n_out the caller puts them where
     the beams that go on are to be in its state, and -1 elsewhere)."""
-    if logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda or logits.dim() != 3 or logits.stride(2) != 1:
+    if logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda or logits.dim() != 3 or (logits.shape[2] > 1 and logits.stride(2) != 1):
         raise ValueError("logits must be a device tensor [batch, beams, V] of float32 or bfloat16 with contiguous rows")
     batch, beams, vocab = logits.shape
     if batch > 1 and beams > 1 and logits.stride(0) != beams * logits.stride(1):

@@ -127,3 +127,13 @@ def test_fewer_beams_go_on(lava):
     assert (p // beams == np.arange(batch)[:, None]).all()
     want[:, :n_out] = 20 + p
     assert state.head_rows.view(batch, beams).cpu().numpy().tolist() == want.tolist() and int(state.error[0]) == 0
+
+
+def test_one_token(lava):
+    """A vocabulary of one, whose only column may have any stride: every beam goes on at its score."""
+    logits = torch.randn(2, 7, 3, device=DEV).transpose(1, 2)[:, :, :1]
+    assert logits.stride(2) != 1
+    logits = torch.as_strided(logits, (2, 3, 1), (3, 1, logits.stride(2)))
+    scores = torch.tensor([[-1.0, -3.0, -2.0], [-5.0, -4.0, -6.0]], device=DEV)
+    parents, tokens, out, done = lava.lava_beam_step(logits, scores)
+    assert parents.tolist() == [[0, 2, 1], [4, 3, 5]] and not tokens.any() and out.tolist() == [[-1.0, -2.0, -3.0], [-4.0, -5.0, -6.0]]
